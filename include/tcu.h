@@ -18,6 +18,8 @@
  *   - tcu_transitive_closure: the blocked transitive closure (Theorem 5).
  *   - tcu_dft: the discrete Fourier transform by Cooley-Tukey (Theorem 7).
  *   - tcu_poly_eval: batch polynomial evaluation (Theorem 11).
+ *   - tcu_rms_norm, tcu_adapter_gemm and tcu_clip_grads with their gradients:
+ *     the operators around a model layer's products.
  *
  * Throughout, s = sqrt(m) is the unit size (a machine parameter of the
  * model), n is the row count of a tall call and N the order of the square
@@ -333,6 +335,151 @@ int tcu_dft_ex(const void *x, void *y, void *work, int64_t n, int64_t batch, int
  * Errors: as tcu_dft_ex, plus TCU_ERR_SCRATCH.  Cost accounting: as tcu_dft. */
 #define TCU_DFT_NOALLOC_MAX_BYTES ((int64_t)64 << 20)
 int tcu_dft_noalloc(const void *x, void *y, int64_t n, int64_t batch, int s, void *hip_stream);
+
+/* ---- operators of an adapted layer ----
+ *
+ * The operators below surround a projection computed on the unit: the norm
+ * that feeds it (tcu_rms_norm, whose 8-bit form with a scale per row is the
+ * int8 product's left operand), low-rank adapters beside it
+ * (tcu_adapter_gemm; a rank is one or a few unit sizes, and X A^T is
+ * Corollary 1's product with a narrow right side), the gradients of both, and
+ * the clipping of gradients by their common norm (tcu_clip_grads).
+ * Their matrices follow the conventions above (device pointers, row-major,
+ * 16-byte aligned bases, pitches in elements, no alignment asked of pitches,
+ * extents below 2^40 bytes); vectors of binary32 or int32 values (scales,
+ * adapters' numbers) need only their elements' alignment.  Each call's
+ * stream is its last argument.  An output must not share a byte with any
+ * other operand, except where stated.  `work` is scratch of the size the
+ * call's tcu_*_work function gives, 16-byte aligned; its contents are
+ * overwritten, and calls that overlap in time need one each.  Nothing is
+ * allocated and the calls can be captured into a graph.  Results are the same
+ * on every call, with one exception stated at tcu_adapter_gemm. */
+
+/* Element types of the norms and of the gradients clipped. */
+typedef enum tcu_elem {
+    TCU_ELEM_F32 = 0,
+    TCU_ELEM_F16 = 1,
+    TCU_ELEM_BF16 = 2
+} tcu_elem;
+
+/* Root-mean-square norm of every row, with the residual's addition:
+ *   h = x + res                        (res NULL: h = x)
+ *   y = h * rstd * w,  rstd = 1 / sqrt(mean(h^2) + eps)
+ *   qscale = max|y| / 127,  q = y / qscale rounded to nearest even
+ * over rows of `cols` elements.  Everything is formed in binary32 from the
+ * unrounded sum h; h and y are rounded once to the element type, q is formed
+ * from the unrounded y.  Any of h, y and q may be NULL and is then not
+ * written; qscale (rows binary32 values) goes with q.  h may be exactly x or
+ * exactly res (same base and pitch): the residual is then added in place.
+ * A row of zeros has y = 0, q = 0 and qscale = 0.  A row with a value that is
+ * not finite has qscale = NaN and q = 0; no other row is affected.
+ *   0 <= rows <= TCU_MAX_RECT_DIM; 1 <= cols <= TCU_MAX_RECT_DIM (rows = 0: no-op);
+ *   eps >= 0, finite; elem: a tcu_elem, of x, res, w, h and y.
+ * Errors: TCU_ERR_NULL, TCU_ERR_SHAPE (also eps), TCU_ERR_UNSUPPORTED (elem),
+ * TCU_ERR_ALIGN, TCU_ERR_OVERLAP, TCU_ERR_POINTER, TCU_ERR_NO_DEVICE, TCU_ERR_HIP. */
+int tcu_rms_norm(const void *x, int64_t ldx, const void *res, int64_t ldr, const void *w, void *h,
+                 int64_t ldh, void *y, int64_t ldy, void *q, int64_t ldq, float *qscale,
+                 int64_t rows, int64_t cols, float eps, int elem, void *hip_stream);
+
+/* Its gradient.  With g = dy * w and rstd recomputed from h:
+ *   dx = rstd * (g - h * rstd^2 * mean(g * h)) + dh   (dh NULL: without it)
+ *   dw = sum over the rows of dy * h * rstd           (cols binary32 values)
+ * dx is the gradient of x and of res alike; dh is the gradient that reaches h
+ * by the residual stream.  Formed in binary32; dx is rounded once.  dw is
+ * overwritten (zeros for rows = 0).  dx may be exactly dy or exactly dh.
+ * Errors: as tcu_rms_norm. */
+int tcu_rms_norm_grad(const void *dy, int64_t lddy, const void *h, int64_t ldh, const void *w,
+                      const void *dh, int64_t lddh, void *dx, int64_t lddx, float *dw, void *work,
+                      int64_t rows, int64_t cols, float eps, int elem, void *hip_stream);
+/* Bytes of its work (-1: a size out of range). */
+int64_t tcu_rms_norm_grad_work(int64_t rows, int64_t cols);
+
+/* A projection with low-rank adapters, one of G for every row:
+ *   Y[m] = X[m] W + alpha[g] (X[m] A_g^T) B_g^T,   g = ids[m]
+ *   X: M x K, pitch ldx;  W: K x N, pitch ldw (as B of tcu_gemm_rect);
+ *   A: G x r x K contiguous (A_g's rows are the rank's weights over K);
+ *   B: G x N x r contiguous;  alpha: G binary32 scales;  ids: M int32 numbers.
+ *   A row whose number lies outside [0, G) has no adapter: Y[m] = X[m] W.
+ *   Y: M x N, pitch ldy, overwritten.
+ * The rows of an adapter may lie in any order.  No row's result depends on
+ * another row or on an adapter it does not name, also where those hold values
+ * that are not finite.  X A^T is summed in binary32 and enters the second
+ * product with at least 16 significant bits where Y is bfloat16 and 22
+ * otherwise; the sum of both parts is formed in binary32 and rounded once.
+ *   0 <= M, K, N <= TCU_MAX_RECT_DIM (M = 0 or N = 0: a no-op);
+ *   0 <= G <= TCU_MAX_ADAPTERS;  1 <= r <= TCU_MAX_RANK;
+ *   A, B, alpha and ids may be NULL if G = 0.
+ *   dtype: TCU_F16_F32, TCU_BF16_F32 or TCU_BF16_BF16 (X, W, A, B and Y).
+ * As for tcu_gemm, binary32 results with K >= 2048 may differ in their low
+ * bits from call to call.
+ * Errors: TCU_ERR_NULL, TCU_ERR_SHAPE, TCU_ERR_UNSUPPORTED, TCU_ERR_ALIGN,
+ * TCU_ERR_OVERLAP, TCU_ERR_POINTER, TCU_ERR_NO_DEVICE, TCU_ERR_HIP.
+ * Cost accounting, with the thread's unit size s: ceil(K/s)*ceil(N/s) calls
+ * and, with adapters, ceil(K/s)*ceil(r/s) + ceil(r/s)*ceil(N/s) more, each of
+ * M rows: every row goes through one adapter. */
+#define TCU_MAX_ADAPTERS ((int64_t)1 << 16)
+#define TCU_MAX_RANK 128
+int tcu_adapter_gemm(const void *X, int64_t ldx, const void *W, int64_t ldw, const void *A,
+                     const void *B, const float *alpha, const int32_t *ids, void *Y, int64_t ldy,
+                     void *work, int64_t M, int64_t K, int64_t N, int64_t r, int64_t G, int dtype,
+                     void *hip_stream);
+
+/* The same with an 8-bit base: Xq (M x K int8, row scales xscale, as
+ * tcu_rms_norm writes them) times Wq (K x N int8, column scales wscale):
+ *   Y[m][n] = xscale[m] wscale[n] sum_k Xq[m][k] Wq[k][n]
+ *             + alpha[g] (X[m] A_g^T) B_g^T [n]
+ * X, A, B and Y are bfloat16; X (M x K) may be NULL if G = 0.  The int8 sum is
+ * exact (K < 2^17); the rest as tcu_adapter_gemm. */
+int tcu_adapter_gemm_q8(const void *Xq, int64_t ldxq, const float *xscale, const void *Wq,
+                        int64_t ldwq, const float *wscale, const void *X, int64_t ldx,
+                        const void *A, const void *B, const float *alpha, const int32_t *ids,
+                        void *Y, int64_t ldy, void *work, int64_t M, int64_t K, int64_t N,
+                        int64_t r, int64_t G, void *hip_stream);
+
+/* The adapters' gradients for the gradient dY (M x N) of Y:
+ *   dA_g = sum over g's rows of alpha[g] (dY[m] B_g)^T X[m]     (G x r x K)
+ *   dB_g = sum over g's rows of alpha[g] dY[m]^T (X[m] A_g^T)   (G x N x r)
+ * binary32, contiguous, overwritten; an adapter without rows gets zeros.  The
+ * inputs are 16-bit (elem TCU_ELEM_F16 or TCU_ELEM_BF16); everything from
+ * there on is binary32, summed in an order that depends on the sizes and ids
+ * alone.  K and N at least 1.  Errors and accounting as tcu_adapter_gemm (each
+ * of the four products is counted, of M rows). */
+int tcu_adapter_grad(const void *X, int64_t ldx, const void *dY, int64_t lddy, const void *A,
+                     const void *B, const float *alpha, const int32_t *ids, float *dA, float *dB,
+                     void *work, int64_t M, int64_t K, int64_t N, int64_t r, int64_t G, int elem,
+                     void *hip_stream);
+
+/* The input's gradient:
+ *   dX[m] = dY[m] W^T + alpha[g] (dY[m] B_g) A_g
+ * Wt: W^T, N x K, pitch ldwt (the frozen W laid out once for this call);
+ * dX: M x K.  Contract, types and errors as tcu_adapter_gemm, whose product
+ * it is with the adapters' factors exchanged. */
+int tcu_adapter_input_grad(const void *dY, int64_t lddy, const void *Wt, int64_t ldwt,
+                           const void *A, const void *B, const float *alpha, const int32_t *ids,
+                           void *dX, int64_t lddx, void *work, int64_t M, int64_t K, int64_t N,
+                           int64_t r, int64_t G, int dtype, void *hip_stream);
+/* Bytes of work that any of the four takes (-1: a size out of range). */
+int64_t tcu_adapter_work(int64_t M, int64_t K, int64_t N, int64_t r, int64_t G);
+
+/* Clipping of gradients by their common norm:
+ *   norm = sqrt(sum over all tensors of g^2),  coef = min(1, max_norm / (norm + 1e-6))
+ *   out_t[i] = g_t[i] * coef,  result[0] = norm, result[1] = coef
+ *   grads, outs, counts, elems: HOST arrays of `tensors` device pointers, element
+ *     counts and element types (tcu_elem); they are read during the call only.
+ *     out_t has g_t's type and may be exactly g_t (in place); the tensors need
+ *     only their elements' alignment.  A tensor of no elements may be NULL.
+ *   result: 2 binary32 values on the device.
+ * Squares are summed in binary64: a norm inside binary32's range is found also
+ * where its square is not.  With a value that is not finite the formula's
+ * result stands: norm = inf gives coef = 0, NaN gives NaN.
+ *   0 <= tensors <= 2^20; max_norm >= 0 (may be infinite).
+ * Errors as above; TCU_ERR_OVERLAP also where an output shares a byte with
+ * another tensor. */
+int tcu_clip_grads(const void *const *grads, void *const *outs, const int64_t *counts,
+                   const int32_t *elems, int64_t tensors, float max_norm, float *result,
+                   void *work, void *hip_stream);
+/* Bytes of its work. */
+int64_t tcu_clip_grads_work(void);
 
 /* ---- cost accounting (Theorem 2 proof; Section 5 weak model) ----
  * tcu_calls:        logical tensor-unit calls issued (1 per tall call,

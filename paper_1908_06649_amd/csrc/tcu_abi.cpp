@@ -13,6 +13,7 @@
 #include <utility>
 
 #include "tcu.h"
+#include "tcu_host.h"
 #include "tcu_launch.h"
 
 #define TCU_EXPORT extern "C" __attribute__((visibility("default")))
@@ -56,11 +57,15 @@ bool unit_ok(int s) { return s == 16 || s == 32; }
 bool dtype_ok(int dt) { return dt >= TCU_F16_F32 && dt <= TCU_I8_I32; }
 int64_t in_size(int dt) { return dt == TCU_I8_I32 ? 1 : 2; }
 int64_t out_size(int dt) { return dt == TCU_BF16_BF16 ? 2 : 4; }
-bool misaligned(const void *p) { return (reinterpret_cast<uintptr_t>(p) & 15u) != 0; }
+using tcu::misaligned;
 bool overlap(const void *a, int64_t na, const void *b, int64_t nb) {
   const uintptr_t x = reinterpret_cast<uintptr_t>(a), y = reinterpret_cast<uintptr_t>(b);
   return x < y + (uintptr_t)nb && y < x + (uintptr_t)na;
 }
+
+}  // namespace
+
+namespace tcu {
 
 // Resolve the current device and check it is a gfx950; fills its CU count.
 int device_ready(int *num_cus) {
@@ -120,40 +125,17 @@ int device_range(const void *p, int64_t bytes) {
   return TCU_OK;
 }
 
+bool checks_on() {
+  return g_knob[TCU_KNOB_CHECK_POINTERS].load(std::memory_order_relaxed) != 0;
+}
+
 // With pointer checks on, every operand extent (pointer, bytes) in turn.
 int check_ranges(std::initializer_list<std::pair<const void *, int64_t>> ranges) {
-  if (g_knob[TCU_KNOB_CHECK_POINTERS].load(std::memory_order_relaxed) == 0) return TCU_OK;
+  if (!checks_on()) return TCU_OK;
   for (const auto &r : ranges) {
     const int rc = device_range(r.first, r.second);
     if (rc != TCU_OK) return rc;
   }
-  return TCU_OK;
-}
-
-int validate_tall(const void *A, int64_t n, int s, const void *B, const void *C, int dt) {
-  if (!A || !B || !C) return TCU_ERR_NULL;
-  if (!unit_ok(s) || !dtype_ok(dt)) return TCU_ERR_UNSUPPORTED;
-  // The model requires n >= sqrt(m) rows for a call (Section 3).
-  if (n < s || n > TCU_MAX_ROWS) return TCU_ERR_SHAPE;
-  if (misaligned(A) || misaligned(B) || misaligned(C)) return TCU_ERR_ALIGN;
-  const int64_t a_bytes = n * s * in_size(dt);
-  const int64_t b_bytes = (int64_t)s * s * in_size(dt);
-  const int64_t c_bytes = n * s * out_size(dt);
-  if (overlap(C, c_bytes, A, a_bytes) || overlap(C, c_bytes, B, b_bytes)) return TCU_ERR_OVERLAP;
-  return TCU_OK;
-}
-
-int validate_gemm(const void *A, const void *B, const void *C, int64_t N, int s, int dt) {
-  if (!A || !B || !C) return TCU_ERR_NULL;
-  if (!unit_ok(s) || !dtype_ok(dt)) return TCU_ERR_UNSUPPORTED;
-  // Theorem 2 takes N a multiple of s (the strips and blocks tile A and B).
-  if (N < s || N % s != 0 || N > TCU_MAX_ORDER) return TCU_ERR_SHAPE;
-  // int32 sums of N products of magnitude <= 2^14 stay exact while N < 2^17.
-  if (dt == TCU_I8_I32 && N >= ((int64_t)1 << 17)) return TCU_ERR_SHAPE;
-  if (misaligned(A) || misaligned(B) || misaligned(C)) return TCU_ERR_ALIGN;
-  const int64_t in_bytes = N * N * in_size(dt);
-  const int64_t c_bytes = N * N * out_size(dt);
-  if (overlap(C, c_bytes, A, in_bytes) || overlap(C, c_bytes, B, in_bytes)) return TCU_ERR_OVERLAP;
   return TCU_OK;
 }
 
@@ -199,6 +181,39 @@ bool views_overlap(const void *a, int64_t ar, int64_t aw, int64_t ap, const void
   return c + bw > P && hits(q + 1, 0, c + bw - P);
 }
 
+}  // namespace tcu
+
+namespace {
+
+using namespace tcu;
+
+int validate_tall(const void *A, int64_t n, int s, const void *B, const void *C, int dt) {
+  if (!A || !B || !C) return TCU_ERR_NULL;
+  if (!unit_ok(s) || !dtype_ok(dt)) return TCU_ERR_UNSUPPORTED;
+  // The model requires n >= sqrt(m) rows for a call (Section 3).
+  if (n < s || n > TCU_MAX_ROWS) return TCU_ERR_SHAPE;
+  if (misaligned(A) || misaligned(B) || misaligned(C)) return TCU_ERR_ALIGN;
+  const int64_t a_bytes = n * s * in_size(dt);
+  const int64_t b_bytes = (int64_t)s * s * in_size(dt);
+  const int64_t c_bytes = n * s * out_size(dt);
+  if (overlap(C, c_bytes, A, a_bytes) || overlap(C, c_bytes, B, b_bytes)) return TCU_ERR_OVERLAP;
+  return TCU_OK;
+}
+
+int validate_gemm(const void *A, const void *B, const void *C, int64_t N, int s, int dt) {
+  if (!A || !B || !C) return TCU_ERR_NULL;
+  if (!unit_ok(s) || !dtype_ok(dt)) return TCU_ERR_UNSUPPORTED;
+  // Theorem 2 takes N a multiple of s (the strips and blocks tile A and B).
+  if (N < s || N % s != 0 || N > TCU_MAX_ORDER) return TCU_ERR_SHAPE;
+  // int32 sums of N products of magnitude <= 2^14 stay exact while N < 2^17.
+  if (dt == TCU_I8_I32 && N >= ((int64_t)1 << 17)) return TCU_ERR_SHAPE;
+  if (misaligned(A) || misaligned(B) || misaligned(C)) return TCU_ERR_ALIGN;
+  const int64_t in_bytes = N * N * in_size(dt);
+  const int64_t c_bytes = N * N * out_size(dt);
+  if (overlap(C, c_bytes, A, in_bytes) || overlap(C, c_bytes, B, in_bytes)) return TCU_ERR_OVERLAP;
+  return TCU_OK;
+}
+
 int validate_rect(const void *A, int64_t lda, const void *B, int64_t ldb, const void *C,
                   int64_t ldc, int64_t M, int64_t K, int64_t N, int flags, int s, int dt) {
   if (!unit_ok(s) || !dtype_ok(dt) || (flags & ~TCU_ACCUMULATE) != 0) return TCU_ERR_UNSUPPORTED;
@@ -209,7 +224,6 @@ int validate_rect(const void *A, int64_t lda, const void *B, int64_t ldb, const 
   if ((!A && M * K > 0) || (!B && K * N > 0) || (!C && M * N > 0)) return TCU_ERR_NULL;
   // int32 sums of K products of magnitude <= 2^14 stay exact while K < 2^17.
   if (dt == TCU_I8_I32 && K >= ((int64_t)1 << 17)) return TCU_ERR_SHAPE;
-  constexpr int64_t kMaxExtent = (int64_t)1 << 40;
   if (lda < K || ldb < N || ldc < N || lda >= kMaxExtent || ldb >= kMaxExtent ||
       ldc >= kMaxExtent)
     return TCU_ERR_SHAPE;
@@ -385,11 +399,7 @@ TCU_EXPORT int tcu_gemm_rect_ex(const void *A, int64_t lda, const void *B, int64
   // Corollary 1 via Theorem 2 on the zero-padded operands: ceil(K/s) strips
   // times ceil(N/s) blocks per strip, one call each, every call on all
   // ceil(M/s)*s padded rows.
-  const int64_t calls = ((K + s - 1) / s) * ((N + s - 1) / s);
-  const int64_t row_blocks = (M + s - 1) / s;
-  g_calls.fetch_add(calls, std::memory_order_relaxed);
-  g_square_calls.fetch_add(calls * row_blocks, std::memory_order_relaxed);
-  g_work.fetch_add(calls * row_blocks * s * s, std::memory_order_relaxed);
+  tcu::count_tall(((K + s - 1) / s) * ((N + s - 1) / s), M, s);
   return TCU_OK;
 }
 
@@ -534,6 +544,16 @@ TCU_EXPORT int tcu_get_knob(int knob) {
 }
 
 namespace tcu {
+int unit_size() { return g_cfg.s; }
+
+// Corollary 1's accounting: the calls are on all ceil(M/s)*s padded rows.
+void count_tall(int64_t calls, int64_t M, int s) {
+  const int64_t row_blocks = (M + s - 1) / s;
+  g_calls.fetch_add(calls, std::memory_order_relaxed);
+  g_square_calls.fetch_add(calls * row_blocks, std::memory_order_relaxed);
+  g_work.fetch_add(calls * row_blocks * s * s, std::memory_order_relaxed);
+}
+
 int knob(int which) {
   return which >= 0 && which < kKnobs ? g_knob[which].load(std::memory_order_relaxed) : 0;
 }

@@ -1,0 +1,474 @@
+// Root-mean-square norm of rows, with the residual's addition and an 8-bit
+// output, and its gradient (tcu_rms_norm, tcu_rms_norm_grad).
+//
+//   h = x + res,  y = h rstd w,  rstd = 1 / sqrt(mean(h^2) + eps)
+//   dx = rstd (g - h rstd^2 mean(g h)) + dh,  g = dy w;   dw = sum_rows dy h rstd
+//
+// Both are bound by memory: a row is read once, kept in registers while its
+// sums are formed, and written once.  A row of up to 1024 elements is one
+// wave's, up to 16384 a workgroup's of four waves (kV vectors of eight
+// elements per lane, the smallest number that holds the row); longer rows are
+// read twice.  Sums are binary32.
+#include "tcu_elem.h"
+#include "tcu_layer.h"
+
+namespace tcu {
+namespace {
+
+constexpr int kWaveCols = 1024, kBlockCols = 16384;
+constexpr unsigned kInfBits = 0x7f800000u;
+
+// Sum and unsigned maximum over the kT threads of a row (64: a wave, else the
+// workgroup, through LDS).
+template <int kT>
+__device__ __forceinline__ float row_sum(float v, float *lds) {
+  v = wave_sum(v);
+  if constexpr (kT > 64) {
+    const int w = threadIdx.x >> 6;
+    if ((threadIdx.x & 63) == 0) lds[w] = v;
+    __syncthreads();
+    v = 0.f;
+#pragma unroll
+    for (int i = 0; i < kT / 64; ++i) v += lds[i];
+    __syncthreads();   // read before the next sum overwrites
+  }
+  return v;
+}
+template <int kT>
+__device__ __forceinline__ unsigned row_max(unsigned v, float *lds) {
+  v = wave_max(v);
+  if constexpr (kT > 64) {
+    unsigned *u = (unsigned *)lds;
+    const int w = threadIdx.x >> 6;
+    if ((threadIdx.x & 63) == 0) u[w] = v;
+    __syncthreads();
+    v = 0u;
+#pragma unroll
+    for (int i = 0; i < kT / 64; ++i) v = u[i] > v ? u[i] : v;
+    __syncthreads();
+  }
+  return v;
+}
+
+// What the 8-bit output of a row needs: the largest |h w| as bits, which order
+// like the values, NaN above infinity.
+struct Quant {
+  float pre, inv, scale;   // q = rint(y * pre * inv)
+};
+__device__ __forceinline__ Quant quant_of(unsigned max_hw, float rstd) {
+  const float amax = __builtin_bit_cast(float, max_hw) * rstd;
+  Quant k;
+  // 127 / amax stays finite down to the smallest maxima
+  k.pre = amax < 0x1p-96f ? 0x1p96f : 1.f;
+  k.scale = amax / 127.f;
+  k.inv = amax > 0.f ? 127.f / (amax * k.pre) : 0.f;
+  if (max_hw >= kInfBits) {
+    k.scale = __builtin_nanf("");
+    k.inv = 0.f;
+  }
+  return k;
+}
+__device__ __forceinline__ void store_q8(unsigned char *p, const float (&y)[8], const Quant &k,
+                                         int valid) {
+  unsigned b[2] = {0u, 0u};
+#pragma unroll
+  for (int e = 0; e < 8; ++e) {
+    float f = rintf(y[e] * k.pre * k.inv);
+    f = k.inv > 0.f ? fminf(fmaxf(f, -127.f), 127.f) : 0.f;
+    b[e >> 2] |= ((unsigned)(int)f & 0xffu) << (8 * (e & 3));
+  }
+  if (valid >= 8) {
+    typedef u32x2 u32x2_any __attribute__((aligned(1)));
+    *(u32x2_any *)p = u32x2{b[0], b[1]};
+  } else {
+#pragma unroll
+    for (int e = 0; e < 8; ++e)
+      if (e < valid) p[e] = (unsigned char)(b[e >> 2] >> (8 * (e & 3)));
+  }
+}
+
+__device__ __forceinline__ float rstd_of(float sum_sq, int64_t cols, float eps) {
+  return 1.f / sqrtf(sum_sq / (float)cols + eps);
+}
+
+// x + res, eight elements.
+template <int ELEM>
+__device__ __forceinline__ void load_h(const unsigned char *x, const unsigned char *res, int valid,
+                                       float (&h)[8]) {
+  const Raw8<ELEM> rx = load8<ELEM>(x, valid);
+  if (res) {
+    const Raw8<ELEM> rr = load8<ELEM>(res, valid);
+    float b[8];
+    unpack8<ELEM>(rx, h);
+    unpack8<ELEM>(rr, b);
+#pragma unroll
+    for (int e = 0; e < 8; ++e) h[e] += b[e];
+  } else {
+    unpack8<ELEM>(rx, h);
+  }
+}
+
+// The outputs of eight elements of a row.
+template <int ELEM>
+__device__ __forceinline__ void finish8(const NormArgs &a, int64_t row, int64_t col, int valid,
+                                        const float (&h)[8], const float (&w)[8], float rstd,
+                                        const Quant &k) {
+  constexpr int ES = elem_bytes<ELEM>;
+  if (a.h) store8<ELEM>((unsigned char *)a.h + (row * a.ldh + col) * ES, h, valid);
+  if (!a.y && !a.q) return;
+  float y[8];
+#pragma unroll
+  for (int e = 0; e < 8; ++e) y[e] = h[e] * rstd * w[e];
+  if (a.y) store8<ELEM>((unsigned char *)a.y + (row * a.ldy + col) * ES, y, valid);
+  if (a.q) store_q8((unsigned char *)a.q + row * a.ldq + col, y, k, valid);
+}
+
+template <int ELEM, int kT, int kV>
+__global__ __launch_bounds__(256) void rms_norm_kernel(NormArgs a) {
+  constexpr int ES = elem_bytes<ELEM>, kRows = 256 / kT;
+  __shared__ float lds[4];
+  const int t = threadIdx.x % kT;
+  const int64_t step = (int64_t)gridDim.x * kRows;
+  for (int64_t row = (int64_t)blockIdx.x * kRows + threadIdx.x / kT; row < a.rows; row += step) {
+    const unsigned char *x = (const unsigned char *)a.x + row * a.ldx * ES;
+    const unsigned char *res = a.res ? (const unsigned char *)a.res + row * a.ldr * ES : nullptr;
+    float h[kV][8];
+    Raw8<ELEM> w[kV];
+    float ss = 0.f;
+#pragma unroll
+    for (int i = 0; i < kV; ++i) {
+      const int col = (t + i * kT) * 8, valid = (int)a.cols - col;
+      if (valid > 0) {
+        load_h<ELEM>(x + (int64_t)col * ES, res ? res + (int64_t)col * ES : nullptr, valid, h[i]);
+        w[i] = load8<ELEM>((const unsigned char *)a.w + (int64_t)col * ES, valid);
+      } else {
+        w[i] = Raw8<ELEM>{};
+#pragma unroll
+        for (int e = 0; e < 8; ++e) h[i][e] = 0.f;
+      }
+    }
+#pragma unroll
+    for (int i = 0; i < kV; ++i)
+#pragma unroll
+      for (int e = 0; e < 8; ++e) ss += h[i][e] * h[i][e];
+    const float rstd = rstd_of(row_sum<kT>(ss, lds), a.cols, a.eps);
+    Quant k{};
+    if (a.q) {
+      unsigned m = 0u;
+#pragma unroll
+      for (int i = 0; i < kV; ++i) {
+        float f[8];
+        unpack8<ELEM>(w[i], f);
+#pragma unroll
+        for (int e = 0; e < 8; ++e) {
+          const unsigned b = __builtin_bit_cast(unsigned, h[i][e] * f[e]) & 0x7fffffffu;
+          m = b > m ? b : m;
+        }
+      }
+      k = quant_of(row_max<kT>(m, lds), rstd);
+      if (t == 0) a.qscale[row] = k.scale;
+    }
+#pragma unroll
+    for (int i = 0; i < kV; ++i) {
+      const int col = (t + i * kT) * 8, valid = (int)a.cols - col;
+      if (valid <= 0) continue;
+      float f[8];
+      unpack8<ELEM>(w[i], f);
+      finish8<ELEM>(a, row, col, valid, h[i], f, rstd, k);
+    }
+  }
+}
+
+// Rows of any length: read once for the sums, once more for the outputs.
+template <int ELEM>
+__global__ __launch_bounds__(1024) void rms_norm_long_kernel(NormArgs a) {
+  constexpr int ES = elem_bytes<ELEM>, kT = 1024;
+  __shared__ float lds[16];
+  for (int64_t row = blockIdx.x; row < a.rows; row += gridDim.x) {
+    const unsigned char *x = (const unsigned char *)a.x + row * a.ldx * ES;
+    const unsigned char *res = a.res ? (const unsigned char *)a.res + row * a.ldr * ES : nullptr;
+    const unsigned char *w = (const unsigned char *)a.w;
+    float ss = 0.f;
+    unsigned m = 0u;
+    float h[8], f[8];
+    for (int64_t col = 8 * threadIdx.x; col < a.cols; col += 8 * kT) {
+      const int valid = (int)(a.cols - col < 8 ? a.cols - col : 8);
+      load_h<ELEM>(x + col * ES, res ? res + col * ES : nullptr, valid, h);
+      if (a.q) unpack8<ELEM>(load8<ELEM>(w + col * ES, valid), f);
+#pragma unroll
+      for (int e = 0; e < 8; ++e) {
+        ss += h[e] * h[e];
+        if (a.q) {
+          const unsigned b = __builtin_bit_cast(unsigned, h[e] * f[e]) & 0x7fffffffu;
+          m = b > m ? b : m;
+        }
+      }
+    }
+    const float rstd = rstd_of(row_sum<kT>(ss, lds), a.cols, a.eps);
+    Quant k{};
+    if (a.q) {
+      k = quant_of(row_max<kT>(m, lds), rstd);
+      if (threadIdx.x == 0) a.qscale[row] = k.scale;
+    }
+    for (int64_t col = 8 * threadIdx.x; col < a.cols; col += 8 * kT) {
+      const int valid = (int)(a.cols - col < 8 ? a.cols - col : 8);
+      load_h<ELEM>(x + col * ES, res ? res + col * ES : nullptr, valid, h);
+      unpack8<ELEM>(load8<ELEM>(w + col * ES, valid), f);
+      finish8<ELEM>(a, row, col, valid, h, f, rstd, k);
+    }
+  }
+}
+
+// The gradient.  A workgroup takes every gridDim.x'th row (kT = 64: every wave
+// a row) and sums its rows' part of dw in registers; the parts, one per
+// workgroup, are added in their order by norm_dw_kernel.
+template <int ELEM, int kT, int kV>
+__global__ __launch_bounds__(256) void rms_norm_grad_kernel(NormGradArgs a) {
+  constexpr int ES = elem_bytes<ELEM>, kRows = 256 / kT;
+  __shared__ float lds[kT == 64 ? 4 * kV * 512 : 8];
+  const int t = threadIdx.x % kT;
+  const unsigned char *dyp = (const unsigned char *)a.dy, *hp = (const unsigned char *)a.h;
+  const unsigned char *dhp = (const unsigned char *)a.dh, *wp = (const unsigned char *)a.w;
+  Raw8<ELEM> w[kV];
+  float dw[kV][8];
+#pragma unroll
+  for (int i = 0; i < kV; ++i) {
+    const int col = (t + i * kT) * 8, valid = (int)a.cols - col;
+    w[i] = valid > 0 ? load8<ELEM>(wp + (int64_t)col * ES, valid) : Raw8<ELEM>{};
+#pragma unroll
+    for (int e = 0; e < 8; ++e) dw[i][e] = 0.f;
+  }
+  const int64_t step = (int64_t)gridDim.x * kRows;
+  for (int64_t row = (int64_t)blockIdx.x * kRows + threadIdx.x / kT; row < a.rows; row += step) {
+    Raw8<ELEM> dy[kV], h[kV], dh[kV];
+#pragma unroll
+    for (int i = 0; i < kV; ++i) {
+      const int col = (t + i * kT) * 8, valid = (int)a.cols - col;
+      dy[i] = h[i] = dh[i] = Raw8<ELEM>{};
+      if (valid > 0) {
+        dy[i] = load8<ELEM>(dyp + (row * a.lddy + col) * ES, valid);
+        h[i] = load8<ELEM>(hp + (row * a.ldh + col) * ES, valid);
+        if (dhp) dh[i] = load8<ELEM>(dhp + (row * a.lddh + col) * ES, valid);
+      }
+    }
+    float ss = 0.f, gh = 0.f;
+#pragma unroll
+    for (int i = 0; i < kV; ++i) {
+      float d[8], x[8], f[8];
+      unpack8<ELEM>(dy[i], d);
+      unpack8<ELEM>(h[i], x);
+      unpack8<ELEM>(w[i], f);
+#pragma unroll
+      for (int e = 0; e < 8; ++e) {
+        ss += x[e] * x[e];
+        gh += d[e] * f[e] * x[e];
+      }
+    }
+    ss = row_sum<kT>(ss, lds);
+    gh = row_sum<kT>(gh, lds + (kT > 64 ? 4 : 0));
+    const float rstd = rstd_of(ss, a.cols, a.eps);
+    const float c = rstd * rstd * (gh / (float)a.cols);
+#pragma unroll
+    for (int i = 0; i < kV; ++i) {
+      const int col = (t + i * kT) * 8, valid = (int)a.cols - col;
+      if (valid <= 0) continue;
+      float d[8], x[8], f[8], r[8];
+      unpack8<ELEM>(dy[i], d);
+      unpack8<ELEM>(h[i], x);
+      unpack8<ELEM>(w[i], f);
+      unpack8<ELEM>(dh[i], r);
+#pragma unroll
+      for (int e = 0; e < 8; ++e) {
+        dw[i][e] += d[e] * (x[e] * rstd);
+        r[e] += rstd * (d[e] * f[e] - x[e] * c);
+      }
+      store8<ELEM>((unsigned char *)a.dx + (row * a.lddx + col) * ES, r, valid);
+    }
+  }
+  float *part = a.work + (int64_t)blockIdx.x * a.cols;
+  if constexpr (kT == 64) {
+    // the four waves' sums, in their order
+#pragma unroll
+    for (int i = 0; i < kV; ++i)
+#pragma unroll
+      for (int e = 0; e < 8; ++e)
+        lds[((threadIdx.x >> 6) * kV + i) * 512 + t * 8 + e] = dw[i][e];
+    __syncthreads();
+    for (int col = threadIdx.x; col < a.cols; col += 256) {
+      float v = 0.f;
+#pragma unroll
+      for (int q = 0; q < 4; ++q) v += lds[q * kV * 512 + col];
+      part[col] = v;
+    }
+  } else {
+#pragma unroll
+    for (int i = 0; i < kV; ++i) {
+      const int col = (t + i * kT) * 8, valid = (int)a.cols - col;
+      if (valid > 0) store8<TCU_ELEM_F32>((unsigned char *)(part + col), dw[i], valid);
+    }
+  }
+}
+
+// Rows of any length; a workgroup's part of dw is kept in memory.
+template <int ELEM>
+__global__ __launch_bounds__(1024) void rms_norm_grad_long_kernel(NormGradArgs a) {
+  constexpr int ES = elem_bytes<ELEM>, kT = 1024;
+  __shared__ float lds[32];
+  const unsigned char *wp = (const unsigned char *)a.w;
+  float *part = a.work + (int64_t)blockIdx.x * a.cols;
+  for (int64_t row = blockIdx.x; row < a.rows; row += gridDim.x) {
+    const unsigned char *dyp = (const unsigned char *)a.dy + row * a.lddy * ES;
+    const unsigned char *hp = (const unsigned char *)a.h + row * a.ldh * ES;
+    const unsigned char *dhp =
+        a.dh ? (const unsigned char *)a.dh + row * a.lddh * ES : nullptr;
+    float d[8], x[8], f[8], r[8];
+    float ss = 0.f, gh = 0.f;
+    for (int64_t col = 8 * threadIdx.x; col < a.cols; col += 8 * kT) {
+      const int valid = (int)(a.cols - col < 8 ? a.cols - col : 8);
+      unpack8<ELEM>(load8<ELEM>(dyp + col * ES, valid), d);
+      unpack8<ELEM>(load8<ELEM>(hp + col * ES, valid), x);
+      unpack8<ELEM>(load8<ELEM>(wp + col * ES, valid), f);
+#pragma unroll
+      for (int e = 0; e < 8; ++e) {
+        ss += x[e] * x[e];
+        gh += d[e] * f[e] * x[e];
+      }
+    }
+    ss = row_sum<kT>(ss, lds);
+    gh = row_sum<kT>(gh, lds + 16);
+    const float rstd = rstd_of(ss, a.cols, a.eps);
+    const float c = rstd * rstd * (gh / (float)a.cols);
+    const bool first = row == blockIdx.x;
+    for (int64_t col = 8 * threadIdx.x; col < a.cols; col += 8 * kT) {
+      const int valid = (int)(a.cols - col < 8 ? a.cols - col : 8);
+      unpack8<ELEM>(load8<ELEM>(dyp + col * ES, valid), d);
+      unpack8<ELEM>(load8<ELEM>(hp + col * ES, valid), x);
+      unpack8<ELEM>(load8<ELEM>(wp + col * ES, valid), f);
+      unpack8<ELEM>(dhp ? load8<ELEM>(dhp + col * ES, valid) : Raw8<ELEM>{}, r);
+      float s[8] = {};
+      if (!first)
+        unpack8<TCU_ELEM_F32>(load8<TCU_ELEM_F32>((unsigned char *)(part + col), valid), s);
+#pragma unroll
+      for (int e = 0; e < 8; ++e) {
+        s[e] += d[e] * (x[e] * rstd);
+        r[e] += rstd * (d[e] * f[e] - x[e] * c);
+      }
+      store8<TCU_ELEM_F32>((unsigned char *)(part + col), s, valid);
+      store8<ELEM>((unsigned char *)a.dx + (row * a.lddx + col) * ES, r, valid);
+    }
+  }
+}
+
+// dw = the sum of `parts` rows of partial sums: a workgroup takes 64 columns,
+// its 16 waves every 16th part.
+__global__ __launch_bounds__(1024) void norm_dw_kernel(const float *__restrict__ work,
+                                                       float *__restrict__ dw, int parts,
+                                                       int64_t cols) {
+  __shared__ float lds[16][64];
+  const int lane = threadIdx.x & 63, w = threadIdx.x >> 6;
+  const int64_t col = (int64_t)blockIdx.x * 64 + lane;
+  float v = 0.f;
+  if (col < cols)
+    for (int p = w; p < parts; p += 16) v += work[p * cols + col];
+  lds[w][lane] = v;
+  __syncthreads();
+  if (w == 0 && col < cols) {
+    v = 0.f;
+#pragma unroll
+    for (int i = 0; i < 16; ++i) v += lds[i][lane];
+    dw[col] = v;
+  }
+}
+
+int vectors(int64_t cols, int threads) {
+  return (int)((cols + 8 * threads - 1) / (8 * threads));
+}
+
+// f(integral_constant) with the smallest number of vectors per lane.
+template <typename F>
+void with_vectors(int v, F f) {
+  switch (v) {
+    case 1: f(std::integral_constant<int, 1>{}); break;
+    case 2: f(std::integral_constant<int, 2>{}); break;
+    case 3: f(std::integral_constant<int, 3>{}); break;
+    case 4: f(std::integral_constant<int, 4>{}); break;
+    case 5: f(std::integral_constant<int, 5>{}); break;
+    case 6: f(std::integral_constant<int, 6>{}); break;
+    case 7: f(std::integral_constant<int, 7>{}); break;
+    default: f(std::integral_constant<int, 8>{}); break;
+  }
+}
+
+// Workgroups of a grid over `n` pieces of work: a launch counts its work items
+// in 32 bits, and the kernels walk on from there.
+unsigned grid_for(int64_t n) { return (unsigned)(n < (1 << 20) ? n : 1 << 20); }
+
+template <int ELEM>
+hipError_t norm_go(const NormArgs &a, hipStream_t stream) {
+  if (a.cols <= kWaveCols) {
+    const dim3 grid(grid_for((a.rows + 3) / 4));
+    if (vectors(a.cols, 64) == 1)
+      hipLaunchKernelGGL((rms_norm_kernel<ELEM, 64, 1>), grid, dim3(256), 0, stream, a);
+    else
+      hipLaunchKernelGGL((rms_norm_kernel<ELEM, 64, 2>), grid, dim3(256), 0, stream, a);
+  } else if (a.cols <= kBlockCols) {
+    with_vectors(vectors(a.cols, 256), [&](auto v) {
+      hipLaunchKernelGGL((rms_norm_kernel<ELEM, 256, decltype(v)::value>), dim3(grid_for(a.rows)),
+                         dim3(256), 0, stream, a);
+    });
+  } else {
+    hipLaunchKernelGGL(rms_norm_long_kernel<ELEM>, dim3(grid_for(a.rows)), dim3(1024), 0, stream,
+                       a);
+  }
+  return hipGetLastError();
+}
+
+template <int ELEM>
+hipError_t grad_go(const NormGradArgs &a, hipStream_t stream) {
+  int parts = (int)(a.rows < kNormParts ? a.rows : kNormParts);
+  if (a.rows > 0) {
+    if (a.cols <= kWaveCols) {
+      if (parts > (a.rows + 3) / 4) parts = (int)((a.rows + 3) / 4);
+      if (vectors(a.cols, 64) == 1)
+        hipLaunchKernelGGL((rms_norm_grad_kernel<ELEM, 64, 1>), dim3(parts), dim3(256), 0, stream,
+                           a);
+      else
+        hipLaunchKernelGGL((rms_norm_grad_kernel<ELEM, 64, 2>), dim3(parts), dim3(256), 0, stream,
+                           a);
+    } else if (a.cols <= kBlockCols) {
+      with_vectors(vectors(a.cols, 256), [&](auto v) {
+        hipLaunchKernelGGL((rms_norm_grad_kernel<ELEM, 256, decltype(v)::value>), dim3(parts),
+                           dim3(256), 0, stream, a);
+      });
+    } else {
+      hipLaunchKernelGGL(rms_norm_grad_long_kernel<ELEM>, dim3(parts), dim3(1024), 0, stream, a);
+    }
+    const hipError_t e = hipGetLastError();
+    if (e != hipSuccess) return e;
+  }
+  hipLaunchKernelGGL(norm_dw_kernel, dim3((unsigned)((a.cols + 63) / 64)), dim3(1024), 0, stream,
+                     a.work, a.dw, parts, a.cols);
+  return hipGetLastError();
+}
+
+}  // namespace
+
+hipError_t launch_rms_norm(int elem, const NormArgs &a, hipStream_t stream, int) {
+  switch (elem) {
+    case TCU_ELEM_F32: return norm_go<TCU_ELEM_F32>(a, stream);
+    case TCU_ELEM_F16: return norm_go<TCU_ELEM_F16>(a, stream);
+    case TCU_ELEM_BF16: return norm_go<TCU_ELEM_BF16>(a, stream);
+  }
+  return hipErrorInvalidValue;
+}
+
+hipError_t launch_rms_norm_grad(int elem, const NormGradArgs &a, hipStream_t stream, int) {
+  switch (elem) {
+    case TCU_ELEM_F32: return grad_go<TCU_ELEM_F32>(a, stream);
+    case TCU_ELEM_F16: return grad_go<TCU_ELEM_F16>(a, stream);
+    case TCU_ELEM_BF16: return grad_go<TCU_ELEM_BF16>(a, stream);
+  }
+  return hipErrorInvalidValue;
+}
+
+}  // namespace tcu

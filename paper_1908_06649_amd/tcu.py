@@ -15,6 +15,21 @@ fallback: if ``libtcu.so`` is missing or fails to load, every call raises.
                                  C (M x N) = [C +] A (M x K) @ B (K x N); A, B and C
                                  may be row-strided 2-D views (row pitch = ld)
 
+and the operators around a layer's products:
+
+    tcu_rms_norm(x, ldx, res, ldr, w, h, ldh, y, ldy, q, ldq, qscale, rows, cols, eps)
+                                 h = x + res, y = its RMS norm, q = y in 8 bits
+    tcu_rms_norm_grad(dy, lddy, h, ldh, w, dh, lddh, dx, lddx, dw, work, rows, cols, eps)
+    tcu_adapter_gemm(X, ldx, W, ldw, A, B, alpha, ids, Y, ldy, work, M, K, N, r, G)
+                                 Y[m] = X[m] W + alpha[g] (X[m] A[g]^T) B[g]^T, g = ids[m]
+    tcu_adapter_gemm_q8(Xq, ldxq, xscale, Wq, ldwq, wscale, X, ldx, A, B, alpha, ids, Y, ldy,
+                        work, M, K, N, r, G)
+                                 the same with an int8 base and scales
+    tcu_adapter_grad(X, ldx, dY, lddy, A, B, alpha, ids, dA, dB, work, M, K, N, r, G)
+    tcu_adapter_input_grad(dY, lddy, Wt, ldwt, A, B, alpha, ids, dX, lddx, work, M, K, N, r, G)
+    tcu_clip_grads(grads, outs, max_norm, result, work)
+                                 outs = grads * min(1, max_norm / (norm + 1e-6))
+
 The element types are taken from the tensors: (float16 -> float32),
 (bfloat16 -> float32), (bfloat16 -> bfloat16) or (int8 -> int32).  Calls are
 issued on torch's current stream and are asynchronous.
@@ -81,6 +96,22 @@ SIGNATURES = {
     "tcu_dft": (_int, [_vp, _vp, _vp, _i64, _i64]),
     "tcu_dft_ex": (_int, [_vp, _vp, _vp, _i64, _i64, _int, _vp]),
     "tcu_dft_noalloc": (_int, [_vp, _vp, _i64, _i64, _int, _vp]),
+    "tcu_rms_norm": (_int, [_vp, _i64, _vp, _i64, _vp, _vp, _i64, _vp, _i64, _vp, _i64, _vp, _i64,
+                            _i64, ctypes.c_float, _int, _vp]),
+    "tcu_rms_norm_grad": (_int, [_vp, _i64, _vp, _i64, _vp, _vp, _i64, _vp, _i64, _vp, _vp, _i64,
+                                 _i64, ctypes.c_float, _int, _vp]),
+    "tcu_rms_norm_grad_work": (_i64, [_i64, _i64]),
+    "tcu_adapter_gemm": (_int, [_vp, _i64, _vp, _i64, _vp, _vp, _vp, _vp, _vp, _i64, _vp, _i64,
+                                _i64, _i64, _i64, _i64, _int, _vp]),
+    "tcu_adapter_gemm_q8": (_int, [_vp, _i64, _vp, _vp, _i64, _vp, _vp, _i64, _vp, _vp, _vp, _vp,
+                                   _vp, _i64, _vp, _i64, _i64, _i64, _i64, _i64, _vp]),
+    "tcu_adapter_grad": (_int, [_vp, _i64, _vp, _i64, _vp, _vp, _vp, _vp, _vp, _vp, _vp, _i64,
+                                _i64, _i64, _i64, _i64, _int, _vp]),
+    "tcu_adapter_input_grad": (_int, [_vp, _i64, _vp, _i64, _vp, _vp, _vp, _vp, _vp, _i64, _vp,
+                                      _i64, _i64, _i64, _i64, _i64, _int, _vp]),
+    "tcu_adapter_work": (_i64, [_i64, _i64, _i64, _i64, _i64]),
+    "tcu_clip_grads": (_int, [_vp, _vp, _vp, _vp, _i64, ctypes.c_float, _vp, _vp, _vp]),
+    "tcu_clip_grads_work": (_i64, []),
     "tcu_calls": (_i64, []),
     "tcu_square_calls": (_i64, []),
     "tcu_work": (_i64, []),
@@ -428,6 +459,240 @@ def tcu_dft_noalloc(x, y, n: int, batch: int, s: int, stream_ptr: int | None = N
     dev, px, py, _ = _dft_args("tcu_dft_noalloc", x, y, None, n, batch)
     st = _stream_ptr(dev) if stream_ptr is None else stream_ptr
     _check(lib().tcu_dft_noalloc(px, py, int(n), int(batch), int(s), st), "tcu_dft_noalloc")
+
+
+# ------------------------------------------------ operators around a layer's products
+TCU_ELEM_F32 = 0
+TCU_ELEM_F16 = 1
+TCU_ELEM_BF16 = 2
+TCU_MAX_ADAPTERS = 1 << 16
+TCU_MAX_RANK = 128
+
+_ELEMS = {}
+_F32 = _I32 = _I8 = None
+
+
+def _elem_code(where: str, dtype) -> int:
+    global _F32, _I32, _I8
+    if not _ELEMS:
+        import torch
+        _F32, _I32, _I8 = torch.float32, torch.int32, torch.int8
+        _ELEMS.update({torch.float32: TCU_ELEM_F32, torch.float16: TCU_ELEM_F16,
+                       torch.bfloat16: TCU_ELEM_BF16})
+    code = _ELEMS.get(dtype)
+    if code is None:
+        raise TcuError(TCU_ERR_UNSUPPORTED, f"{where}: element type {dtype}")
+    return code
+
+
+def _dtypes(where: str, want, *tensors) -> None:
+    for t in tensors:
+        if t is not None and t.dtype != want:
+            raise ValueError(f"{where}: expected {want}, got {t.dtype}")
+
+
+def _addresses(where: str, views, vectors, work, nbytes: int):
+    """Checks of an operator's tensors: views (tensor, rows, cols, ld) are 2-D
+    with unit column stride and row pitch ld, vectors (tensor, elements) are
+    contiguous, all on the current HIP device, and work holds nbytes.  A tensor
+    may be None where the call allows it.  Returns the device index and the
+    addresses (None for absent tensors), work's last."""
+    dev, ptrs = -1, []
+    for t, rows, cols, ld in views:
+        if t is None:
+            ptrs.append(None)
+            continue
+        if t.shape != (rows, cols):
+            raise ValueError(f"{where}: expected a {rows} x {cols} view, got {tuple(t.shape)}")
+        st = t.stride()
+        if rows and cols and ((st[1] != 1 and cols > 1) or (st[0] != ld and rows > 1)):
+            raise ValueError(f"{where}: strides {st} do not match rows of pitch {ld}")
+        d = t.get_device()
+        if d < 0 or (dev >= 0 and d != dev):
+            raise ValueError(f"{where}: all tensors must be on the same HIP device")
+        dev = d
+        ptrs.append(t.data_ptr() or None)
+    for t, n in vectors:
+        if t is None:
+            ptrs.append(None)
+            continue
+        if t.numel() != n or not t.is_contiguous():
+            raise ValueError(f"{where}: expected {n} contiguous elements, got {tuple(t.shape)}")
+        d = t.get_device()
+        if d < 0 or (dev >= 0 and d != dev):
+            raise ValueError(f"{where}: all tensors must be on the same HIP device")
+        dev = d
+        ptrs.append(t.data_ptr() or None)
+    if work is not None:
+        if nbytes < 0:
+            raise TcuError(TCU_ERR_SHAPE, where)
+        if work.get_device() != dev or not work.is_contiguous() or \
+                work.numel() * work.element_size() < nbytes:
+            raise ValueError(f"{where}: work needs {nbytes} contiguous bytes on the same device")
+        ptrs.append(work.data_ptr() or None)
+    if dev != _current_device():
+        _check_current_device(where, dev)
+    return dev, ptrs
+
+
+def _stream_of(dev: int, stream_ptr):
+    return _stream_ptr(dev) if stream_ptr is None else stream_ptr
+
+
+def tcu_rms_norm(x, ldx: int, res, ldr: int, w, h, ldh: int, y, ldy: int, q, ldq: int, qscale,
+                 rows: int, cols: int, eps: float, stream_ptr: int | None = None) -> None:
+    """h = x + res, y = h / sqrt(mean(h^2) + eps) * w and y in 8 bits (q int8, qscale
+    float32 per row); res, h, y and (q, qscale) may be None."""
+    elem = _elem_code("tcu_rms_norm", x.dtype)
+    _dtypes("tcu_rms_norm", x.dtype, res, w, h, y)
+    _dtypes("tcu_rms_norm", _I8, q)
+    _dtypes("tcu_rms_norm", _F32, qscale)
+    dev, (px, pr, ph, py, pq, pw, ps) = _addresses(
+        "tcu_rms_norm", ((x, rows, cols, ldx), (res, rows, cols, ldr), (h, rows, cols, ldh),
+                         (y, rows, cols, ldy), (q, rows, cols, ldq)),
+        ((w, cols), (qscale, rows)), None, 0)
+    _check((_lib or lib()).tcu_rms_norm(px, ldx, pr, ldr, pw, ph, ldh, py, ldy, pq, ldq, ps, rows,
+                                        cols, eps, elem, _stream_of(dev, stream_ptr)),
+           "tcu_rms_norm")
+
+
+def tcu_rms_norm_grad_work(rows: int, cols: int) -> int:
+    """Bytes of tcu_rms_norm_grad's work (-1: a size out of range)."""
+    return (_lib or lib()).tcu_rms_norm_grad_work(rows, cols)
+
+
+def tcu_rms_norm_grad(dy, lddy: int, h, ldh: int, w, dh, lddh: int, dx, lddx: int, dw, work,
+                      rows: int, cols: int, eps: float, stream_ptr: int | None = None) -> None:
+    """The norm's gradients: dx (dh, if any, added) and dw (float32), from h."""
+    where = "tcu_rms_norm_grad"
+    elem = _elem_code(where, dy.dtype)
+    _dtypes(where, dy.dtype, h, w, dh, dx)
+    _dtypes(where, _F32, dw)
+    L = _lib or lib()
+    dev, (pdy, ph, pdh, pdx, pw, pdw, pwork) = _addresses(
+        where, ((dy, rows, cols, lddy), (h, rows, cols, ldh), (dh, rows, cols, lddh),
+                (dx, rows, cols, lddx)),
+        ((w, cols), (dw, cols)), work, L.tcu_rms_norm_grad_work(rows, cols))
+    _check(L.tcu_rms_norm_grad(pdy, lddy, ph, ldh, pw, pdh, lddh, pdx, lddx, pdw, pwork, rows,
+                               cols, eps, elem, _stream_of(dev, stream_ptr)), where)
+
+
+def tcu_adapter_work(M: int, K: int, N: int, r: int, G: int) -> int:
+    """Bytes of work of the adapter calls (-1: a size out of range)."""
+    return (_lib or lib()).tcu_adapter_work(M, K, N, r, G)
+
+
+def tcu_adapter_gemm(X, ldx: int, W, ldw: int, A, B, alpha, ids, Y, ldy: int, work, M: int, K: int,
+                     N: int, r: int, G: int, stream_ptr: int | None = None) -> None:
+    """Y[m] = X[m] @ W + alpha[g] * (X[m] @ A[g].T) @ B[g].T with g = ids[m] (no adapter
+    outside [0, G)); A: G x r x K, B: G x N x r, alpha float32, ids int32."""
+    where = "tcu_adapter_gemm"
+    dt = _dtype_code(X.dtype, Y.dtype, _POLY_DTYPES)
+    _elem_code(where, X.dtype)
+    _dtypes(where, X.dtype, W, A, B)
+    _dtypes(where, _F32, alpha)
+    _dtypes(where, _I32, ids)
+    L = _lib or lib()
+    dev, (px, pw, py, pa, pb, pal, pid, pwork) = _addresses(
+        where, ((X, M, K, ldx), (W, K, N, ldw), (Y, M, N, ldy)),
+        ((A, G * r * K), (B, G * N * r), (alpha, G), (ids, M)), work,
+        L.tcu_adapter_work(M, K, N, r, G))
+    _check(L.tcu_adapter_gemm(px, ldx, pw, ldw, pa, pb, pal, pid, py, ldy, pwork, M, K, N, r, G,
+                              dt, _stream_of(dev, stream_ptr)), where)
+
+
+def tcu_adapter_gemm_q8(Xq, ldxq: int, xscale, Wq, ldwq: int, wscale, X, ldx: int, A, B, alpha,
+                        ids, Y, ldy: int, work, M: int, K: int, N: int, r: int, G: int,
+                        stream_ptr: int | None = None) -> None:
+    """tcu_adapter_gemm with an 8-bit base: (Xq @ Wq) * xscale[:, None] * wscale; X, A,
+    B and Y bfloat16."""
+    import torch
+    where = "tcu_adapter_gemm_q8"
+    _elem_code(where, Y.dtype)
+    _dtypes(where, torch.bfloat16, X, A, B, Y)
+    _dtypes(where, _I8, Xq, Wq)
+    _dtypes(where, _F32, xscale, wscale, alpha)
+    _dtypes(where, _I32, ids)
+    L = _lib or lib()
+    dev, (pxq, pwq, px, py, pxs, pws, pa, pb, pal, pid, pwork) = _addresses(
+        where, ((Xq, M, K, ldxq), (Wq, K, N, ldwq), (X, M, K, ldx), (Y, M, N, ldy)),
+        ((xscale, M), (wscale, N), (A, G * r * K), (B, G * N * r), (alpha, G), (ids, M)), work,
+        L.tcu_adapter_work(M, K, N, r, G))
+    _check(L.tcu_adapter_gemm_q8(pxq, ldxq, pxs, pwq, ldwq, pws, px, ldx, pa, pb, pal, pid, py,
+                                 ldy, pwork, M, K, N, r, G, _stream_of(dev, stream_ptr)), where)
+
+
+def tcu_adapter_grad(X, ldx: int, dY, lddy: int, A, B, alpha, ids, dA, dB, work, M: int, K: int,
+                     N: int, r: int, G: int, stream_ptr: int | None = None) -> None:
+    """The adapters' gradients dA (G x r x K) and dB (G x N x r), float32."""
+    where = "tcu_adapter_grad"
+    elem = _elem_code(where, X.dtype)
+    _dtypes(where, X.dtype, dY, A, B)
+    _dtypes(where, _F32, alpha, dA, dB)
+    _dtypes(where, _I32, ids)
+    L = _lib or lib()
+    dev, (px, pdy, pa, pb, pal, pid, pda, pdb, pwork) = _addresses(
+        where, ((X, M, K, ldx), (dY, M, N, lddy)),
+        ((A, G * r * K), (B, G * N * r), (alpha, G), (ids, M), (dA, G * r * K), (dB, G * N * r)),
+        work, L.tcu_adapter_work(M, K, N, r, G))
+    _check(L.tcu_adapter_grad(px, ldx, pdy, lddy, pa, pb, pal, pid, pda, pdb, pwork, M, K, N, r, G,
+                              elem, _stream_of(dev, stream_ptr)), where)
+
+
+def tcu_adapter_input_grad(dY, lddy: int, Wt, ldwt: int, A, B, alpha, ids, dX, lddx: int, work,
+                           M: int, K: int, N: int, r: int, G: int,
+                           stream_ptr: int | None = None) -> None:
+    """dX[m] = dY[m] @ Wt + alpha[g] * (dY[m] @ B[g]) @ A[g]; Wt: N x K."""
+    where = "tcu_adapter_input_grad"
+    dt = _dtype_code(dY.dtype, dX.dtype, _POLY_DTYPES)
+    _elem_code(where, dY.dtype)
+    _dtypes(where, dY.dtype, Wt, A, B)
+    _dtypes(where, _F32, alpha)
+    _dtypes(where, _I32, ids)
+    L = _lib or lib()
+    dev, (pdy, pw, pdx, pa, pb, pal, pid, pwork) = _addresses(
+        where, ((dY, M, N, lddy), (Wt, N, K, ldwt), (dX, M, K, lddx)),
+        ((A, G * r * K), (B, G * N * r), (alpha, G), (ids, M)), work,
+        L.tcu_adapter_work(M, K, N, r, G))
+    _check(L.tcu_adapter_input_grad(pdy, lddy, pw, ldwt, pa, pb, pal, pid, pdx, lddx, pwork, M, K,
+                                    N, r, G, dt, _stream_of(dev, stream_ptr)), where)
+
+
+def tcu_clip_grads_work() -> int:
+    """Bytes of tcu_clip_grads' work."""
+    return (_lib or lib()).tcu_clip_grads_work()
+
+
+def tcu_clip_grads(grads, outs, max_norm: float, result, work,
+                   stream_ptr: int | None = None) -> None:
+    """outs[t] = grads[t] * min(1, max_norm / (norm + 1e-6)) with the norm over all tensors;
+    result (2 float32): the norm and the factor.  Contiguous tensors of any shape,
+    float32, float16 or bfloat16 each; outs[t] may be grads[t]."""
+    where = "tcu_clip_grads"
+    n = len(grads)
+    if len(outs) != n:
+        raise ValueError(f"{where}: {n} gradients and {len(outs)} outputs")
+    _elem_code(where, result.dtype)
+    _dtypes(where, _F32, result)
+    L = _lib or lib()
+    dev, (pres, pwork) = _addresses(where, (), ((result, 2),), work, L.tcu_clip_grads_work())
+    elems, counts = [], []
+    for g, o in zip(grads, outs):
+        code = _ELEMS.get(g.dtype)
+        if code is None:
+            raise TcuError(TCU_ERR_UNSUPPORTED, f"{where}: element type {g.dtype}")
+        if o.dtype != g.dtype or o.numel() != g.numel():
+            raise ValueError(f"{where}: an output differs from its gradient in type or size")
+        if g.get_device() != dev or o.get_device() != dev:
+            raise ValueError(f"{where}: all tensors must be on the same HIP device")
+        if not (g.is_contiguous() and o.is_contiguous()):
+            raise ValueError(f"{where}: tensors must be contiguous")
+        elems.append(code)
+        counts.append(g.numel())
+    _check(L.tcu_clip_grads((_vp * n)(*[g.data_ptr() for g in grads]),
+                            (_vp * n)(*[o.data_ptr() for o in outs]), (_i64 * n)(*counts),
+                            (ctypes.c_int32 * n)(*elems), n, max_norm, pres, pwork,
+                            _stream_of(dev, stream_ptr)), where)
 
 
 # --------------------------------------------------------- cost accounting
