@@ -6,8 +6,8 @@
 //   dA_g = sum_m alpha[g] (dY[m] B_g)^T X[m],  dB_g = sum_m alpha[g] dY[m]^T (X[m] A_g^T)
 //
 // The projection is the blocked product (launch_rect) into scratch, the
-// narrow product T = alpha X A^T is formed a row per wave, and a last pass adds
-// T B^T and rounds.
+// narrow product T = alpha X A^T is formed by narrow_kernel, and a last pass
+// adds T B^T and rounds.
 #include "tcu_elem.h"
 #include "tcu_launch.h"
 #include "tcu_layer.h"
@@ -17,55 +17,179 @@ namespace {
 
 constexpr int64_t round256(int64_t n) { return (n + 255) / 256 * 256; }
 
-// Scratch: the projection's sums, T of X and of dY, the adapters transposed.
-struct Scratch {
-  unsigned char *base;
-  float *t, *dt;
-  unsigned char *at, *bt;
-  int64_t bytes;
-};
-Scratch scratch(void *work, int64_t M, int64_t K, int64_t N, int64_t r, int64_t G) {
-  Scratch s;
-  int64_t at = 0;
-  auto take = [&](int64_t n) {
-    unsigned char *p = (unsigned char *)work + at;
-    at += round256(n);
-    return p;
-  };
-  s.base = take(M * (N > K ? N : K) * 4);
-  s.t = (float *)take(M * r * 4);
-  s.dt = (float *)take(M * r * 4);
-  s.at = take(G * r * K * 2);
-  s.bt = take(G * r * N * 2);
-  s.bytes = at;
-  return s;
+// Ranks of T's rows: one or an even number of blocks of 16.
+__host__ __device__ constexpr int64_t rank_pad(int64_t r) { return r <= 16 ? 16 : (r + 31) / 32 * 32; }
+
+// ---------------------------------------------------------------------------
+// The rows in the order of their adapters, the rows of one in their own order:
+// order[start[g] .. start[g + 1]) are g's, start[G] the rows that have one.
+// Workgroup g counts the rows of smaller numbers, then places its own: 1024
+// lanes by ballots, so the order is fixed.
+// ---------------------------------------------------------------------------
+constexpr int kGroupThreads = 1024;
+__global__ __launch_bounds__(kGroupThreads) void group_kernel(const int *__restrict__ ids,
+                                                              int *__restrict__ start,
+                                                              int *__restrict__ order, int M,
+                                                              int G) {
+  constexpr int kWaves = kGroupThreads / 64;
+  __shared__ int part[kWaves];
+  const int lane = threadIdx.x & 63, w = threadIdx.x >> 6, g = blockIdx.x;
+  int below = 0, own = 0;
+  for (int m = threadIdx.x; m < M; m += kGroupThreads) {
+    const int id = ids[m];
+    below += id >= 0 && id < g;
+    own += id == g;
+  }
+#pragma unroll
+  for (int s = 32; s > 0; s >>= 1) below += __shfl_xor(below, s);
+  own = __any(own > 0);
+  if (lane == 0) part[w] = below;
+  const int some = __syncthreads_or(own);
+  below = 0;
+#pragma unroll
+  for (int i = 0; i < kWaves; ++i) below += part[i];
+  if (threadIdx.x == 0) start[g] = below;
+  int at = below;
+  if (some) {
+    for (int m0 = 0; m0 < M; m0 += kGroupThreads) {
+      const int m = m0 + threadIdx.x;
+      const bool mine = m < M && ids[m] == g;
+      const unsigned long long votes = __ballot(mine);
+      __syncthreads();   // part has been read
+      if (lane == 0) part[w] = __popcll(votes);
+      __syncthreads();
+      int before = __popcll(votes & ((1ull << lane) - 1)), total = 0;
+#pragma unroll
+      for (int i = 0; i < kWaves; ++i) {
+        before += i < w ? part[i] : 0;
+        total += part[i];
+      }
+      if (mine) order[at + before] = m;
+      at += total;
+    }
+  }
+  if (g == G - 1 && threadIdx.x == 0) start[G] = at;
 }
 
-// T[m][j] = alpha[g] sum_k X[m][k] F_g(j, k), zeros without an adapter; F_g(j, k)
-// lies at F + g r K + j fj + k fk.  A wave per row.
-template <int ELEM>
-__global__ __launch_bounds__(256) void narrow_kernel(const unsigned char *__restrict__ X,
-                                                     int64_t ldx,
-                                                     const unsigned char *__restrict__ F,
-                                                     int64_t fj, int64_t fk,
+// ---------------------------------------------------------------------------
+// T[m][j] = alpha[g] sum_k X[m][k] F_g[j][k] (F_g: r x K, rows contiguous), zeros
+// from rank r on to rank_pad.  A workgroup takes 16 kRows rows (of `order` if
+// given, else as they lie) and all ranks; its 8 waves take every eighth 64
+// elements of K, and their sums are added in their order.  Both operands are
+// loaded as the matrix cores take them, 16 bytes of a row per lane: X from
+// memory once, F from the caches.  Rows of several adapters are multiplied by
+// each of them, a row keeping its own adapter's result.
+// ---------------------------------------------------------------------------
+struct Narrow {
+  const unsigned char *X, *F;
+  float *T;
+  int64_t ldx;
+  int K;
+};
+template <int ELEM, int kRows, int kBlocks>
+__global__ __launch_bounds__(512) void narrow_kernel(Narrow n0, Narrow n1,
                                                      const float *__restrict__ alpha,
                                                      const int *__restrict__ ids,
-                                                     float *__restrict__ T, int64_t M, int64_t K,
-                                                     int r, int G) {
-  const int lane = threadIdx.x & 63;
-  const int64_t step = (int64_t)gridDim.x * 4;
-  for (int64_t m = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6); m < M; m += step) {
-    const int g = ids[m];
-    const bool has = g >= 0 && g < G;
-    for (int j = 0; j < r; ++j) {
-      float s = 0.f;
-      if (has) {
-        const unsigned char *f = F + 2 * ((int64_t)g * r * K + j * fj);
-        for (int64_t k = lane; k < K; k += 64)
-          s += elem_to_f32<ELEM>(X + 2 * (m * ldx + k)) * elem_to_f32<ELEM>(f + 2 * k * fk);
-        s = wave_sum(s) * alpha[g];
+                                                     const int *__restrict__ order,
+                                                     const int *__restrict__ start, int M, int r,
+                                                     int rp, int G) {
+  constexpr int DT = ELEM == TCU_ELEM_F16 ? TCU_F16_F32 : TCU_BF16_F32;
+  constexpr int kWaves = 8, kStep = 64;
+  __shared__ f32x4 sums[kWaves][kRows * kBlocks][64];
+  const Narrow n = blockIdx.y == 0 ? n0 : n1;
+  const int lane = threadIdx.x & 63, w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int c = lane & 15, q = lane >> 4;
+  const int count = order ? start[G] : M;
+  const int first = blockIdx.x * (16 * kRows);
+  if (first >= count) return;
+  int row[kRows], id[kRows];
+  unsigned left = 0u;
+#pragma unroll
+  for (int i = 0; i < kRows; ++i) {
+    const int at = first + 16 * i + c;
+    row[i] = order ? order[at < count ? at : count - 1] : (at < count ? at : count - 1);
+    id[i] = at < count ? ids[row[i]] : -1;
+    if (id[i] >= G || id[i] < 0) id[i] = -1;
+    left |= (unsigned)(__ballot(id[i] >= 0) & 0xffffu) << (16 * i);
+  }
+  const unsigned char *x[kRows];
+#pragma unroll
+  for (int i = 0; i < kRows; ++i) x[i] = n.X + 2 * ((int64_t)row[i] * n.ldx + 8 * q);
+  while (left != 0u) {
+    // the adapter of the first row left, and its rows
+    const int lead = __builtin_ctz(left);
+    int g = 0;
+    unsigned mine = 0u;
+#pragma unroll
+    for (int i = 0; i < kRows; ++i)
+      if (lead >> 4 == i) g = __builtin_amdgcn_readlane(id[i], lead & 15);
+#pragma unroll
+    for (int i = 0; i < kRows; ++i)
+      mine |= (unsigned)(__ballot(id[i] == g) & 0xffffu) << (16 * i);
+    left &= ~mine;
+    const unsigned char *fg = n.F + 2 * ((int64_t)g * r * n.K + 8 * q);
+    const float al = alpha[g];
+    for (int j0 = 0; j0 < rp; j0 += 16 * kBlocks) {
+      const unsigned char *f[kBlocks];
+      f32x4 acc[kRows][kBlocks];
+#pragma unroll
+      for (int b = 0; b < kBlocks; ++b) {
+        const int j = j0 + 16 * b + c;
+        f[b] = fg + 2 * (int64_t)(j < r ? j : r - 1) * n.K;
+#pragma unroll
+        for (int i = 0; i < kRows; ++i) acc[i][b] = f32x4{0.f, 0.f, 0.f, 0.f};
       }
-      if (lane == 0) T[m * r + j] = s;
+      // kU chunks of 64 elements, their loads in flight together
+      auto step = [&](int k, auto chunks, auto whole) __attribute__((always_inline)) {
+        constexpr int kU = decltype(chunks)::value;
+        u32x4 xv[kU][2][kRows], fv[kU][2][kBlocks];
+#pragma unroll
+        for (int u = 0; u < kU; ++u)
+#pragma unroll
+          for (int h = 0; h < 2; ++h) {
+            const int at = k + u * kWaves * kStep + 32 * h;
+            const int valid = decltype(whole)::value ? 8 : n.K - at - 8 * q;
+#pragma unroll
+            for (int i = 0; i < kRows; ++i) xv[u][h][i] = load8<ELEM>(x[i] + 2 * at, valid).v[0];
+#pragma unroll
+            for (int b = 0; b < kBlocks; ++b) fv[u][h][b] = load8<ELEM>(f[b] + 2 * at, valid).v[0];
+          }
+#pragma unroll
+        for (int u = 0; u < kU; ++u)
+#pragma unroll
+          for (int h = 0; h < 2; ++h)
+#pragma unroll
+            for (int i = 0; i < kRows; ++i)
+#pragma unroll
+              for (int b = 0; b < kBlocks; ++b)
+                acc[i][b] = mfma_k32(DT, fv[u][h][b], xv[u][h][i], acc[i][b]);
+      };
+      int k = w * kStep;
+      constexpr int kU = kRows == 1 ? 4 : 2, kFar = (kU - 1) * kWaves * kStep;
+      for (; k + kFar + kStep <= n.K; k += kU * kWaves * kStep)
+        step(k, std::integral_constant<int, kU>{}, std::true_type{});
+      for (; k + kStep <= n.K; k += kWaves * kStep)
+        step(k, std::integral_constant<int, 1>{}, std::true_type{});
+      if (k < n.K) step(k, std::integral_constant<int, 1>{}, std::false_type{});
+#pragma unroll
+      for (int i = 0; i < kRows; ++i)
+#pragma unroll
+        for (int b = 0; b < kBlocks; ++b) sums[w][i * kBlocks + b][lane] = acc[i][b];
+      __syncthreads();
+      for (int s = w; s < kRows * kBlocks; s += kWaves) {
+        f32x4 v = sums[0][s][lane];
+#pragma unroll
+        for (int u = 1; u < kWaves; ++u) v += sums[u][s][lane];
+        // ranks j .. j + 3 of row c of the block
+        const int i = s / kBlocks, j = j0 + 16 * (s % kBlocks) + 4 * q;
+        int m = row[0];
+#pragma unroll
+        for (int u = 1; u < kRows; ++u) m = i == u ? row[u] : m;
+#pragma unroll
+        for (int e = 0; e < 4; ++e) v[e] = j + e < r ? v[e] * al : 0.f;
+        if (mine >> (16 * i + c) & 1u) *(f32x4 *)(n.T + (int64_t)m * rp + j) = v;
+      }
+      __syncthreads();   // read before the next sums overwrite
     }
   }
 }
@@ -83,53 +207,264 @@ __global__ __launch_bounds__(256) void join_kernel(AdapterArgs a, const void *ba
     const int g = a.G > 0 ? a.ids[m] : -1;
     if (g >= 0 && g < a.G) {
       const unsigned char *b = (const unsigned char *)a.B + 2 * (((int64_t)g * a.N + n) * a.r);
-      for (int j = 0; j < a.r; ++j) v += T[m * a.r + j] * elem_to_f32<ELEM>(b + 2 * j);
+      const float *t = T + m * rank_pad(a.r);
+      for (int j = 0; j < a.r; ++j) v += t[j] * elem_to_f32<ELEM>(b + 2 * j);
     }
     f32_to_elem<OUT>((unsigned char *)a.Y + (m * a.ldy + n) * elem_bytes<OUT>, v);
   }
 }
 
-// out (cols x rows) of every adapter = in (rows x cols), 16-bit values.
+// out (cols x rows) of every adapter = in (rows x cols), 16-bit values, in
+// tiles of 32 x 32.
 __global__ __launch_bounds__(256) void transpose_kernel(const unsigned short *__restrict__ in,
                                                         unsigned short *__restrict__ out,
-                                                        int64_t rows, int64_t cols, int64_t total) {
-  for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < total;
-       i += (int64_t)gridDim.x * 256) {
-    const int64_t g = i / (rows * cols), e = i - g * rows * cols;
-    const int64_t c = e / rows, r = e - c * rows;
-    out[i] = in[g * rows * cols + r * cols + c];
+                                                        int64_t rows, int64_t cols,
+                                                        int64_t tiles) {
+  __shared__ unsigned short tile[32][33];
+  const int64_t tc = (cols + 31) / 32, per = tc * ((rows + 31) / 32);
+  const int x = threadIdx.x & 31, y = threadIdx.x >> 5;
+  for (int64_t t = blockIdx.x; t < tiles; t += gridDim.x) {
+    const int64_t g = t / per, r0 = (t - g * per) / tc * 32, c0 = (t - g * per) % tc * 32;
+    const int64_t base = g * rows * cols;
+#pragma unroll
+    for (int i = y; i < 32; i += 8)
+      if (r0 + i < rows && c0 + x < cols) tile[i][x] = in[base + (r0 + i) * cols + c0 + x];
+    __syncthreads();
+#pragma unroll
+    for (int i = y; i < 32; i += 8)
+      if (c0 + i < cols && r0 + x < rows) out[base + (c0 + i) * rows + r0 + x] = tile[x][i];
+    __syncthreads();
   }
 }
 
-// D_g(j, c) = sum over g's rows of T[m][j] X[m][c], at D + g r C + j dj + c dc.
-template <int ELEM>
-__global__ __launch_bounds__(256) void factor_grad_kernel(const unsigned char *__restrict__ X,
-                                                          int64_t ldx,
-                                                          const float *__restrict__ T,
-                                                          const int *__restrict__ ids,
-                                                          float *__restrict__ D, int64_t dj,
-                                                          int64_t dc, int64_t M, int64_t C,
-                                                          int r) {
-  const int64_t c = (int64_t)blockIdx.x * 256 + threadIdx.x;
-  const int g = blockIdx.y, j = blockIdx.z;
-  if (c >= C) return;
-  float s = 0.f;
-  for (int64_t m = 0; m < M; ++m)
-    if (ids[m] == g) s += T[m * r + j] * elem_to_f32<ELEM>(X + 2 * (m * ldx + c));
-  D[(int64_t)g * r * C + j * dj + c * dc] = s;
+// ---------------------------------------------------------------------------
+// D_g(j, c) = sum over g's rows of T[m][j] X[m][c], the rows in the order of
+// group_kernel cut into chunks.  A workgroup takes one chunk and 128 columns,
+// its 4 waves every fourth group of 4 rows: binary32 matrix products over 4 rows,
+// a lane holding 8 columns of one of them (16 bytes), value e of the 16 lanes
+// being columns e, 8 + e, .. of product e.  An adapter whose rows lie in one
+// chunk is written at once; the parts of the others (those a chunk begins with,
+// and those it ends with) go to scratch and are added by finish_kernel in the
+// order of the chunks.
+// ---------------------------------------------------------------------------
+struct Factor {
+  const unsigned char *X;
+  const float *T;
+  float *D, *parts;      // parts: chunk, first or last, r, C
+  int64_t ldx, dj, dc;   // D_g(j, c) at D + g r C + j dj + c dc
+  int C;
+};
+constexpr int kFactorCols = 128;
+
+template <int ELEM, int kBlocks>
+__global__ __launch_bounds__(256) void factor_kernel(Factor f0, Factor f1,
+                                                     const int *__restrict__ ids,
+                                                     const int *__restrict__ order,
+                                                     const int *__restrict__ start, int r, int rp,
+                                                     int G, int chunk, int cols0) {
+  __shared__ f32x4 sums[4][8][64];
+  const bool second = (int)blockIdx.x >= cols0;
+  const Factor f = second ? f1 : f0;
+  const int c0 = ((int)blockIdx.x - (second ? cols0 : 0)) * kFactorCols;
+  const int lane = threadIdx.x & 63, w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int c = lane & 15, q = lane >> 4;
+  const int begin = blockIdx.y * chunk, count = start[G];
+  const int end = begin + chunk < count ? begin + chunk : count;
+  const int col = c0 + 8 * c, valid = f.C - col;
+  const int64_t rc = (int64_t)r * f.C;
+  for (int at = begin; at < end;) {
+    const int g = ids[order[at]];
+    const int s0 = start[g], s1 = start[g + 1], to = s1 < end ? s1 : end;
+    float *out;
+    int64_t dj = f.dj, dc = f.dc;
+    if (s0 >= begin && s1 <= end) {
+      out = f.D + g * rc;
+    } else {
+      out = f.parts + (2 * (int64_t)blockIdx.y + (s0 >= begin)) * rc;
+      dj = f.C;
+      dc = 1;
+    }
+    for (int j0 = 0; j0 < rp; j0 += 16 * kBlocks) {
+      f32x4 acc[kBlocks][8];
+#pragma unroll
+      for (int b = 0; b < kBlocks; ++b)
+#pragma unroll
+        for (int e = 0; e < 8; ++e) acc[b][e] = f32x4{0.f, 0.f, 0.f, 0.f};
+      // kU groups of 4 rows, their loads in flight together; past the run's end
+      // (not `whole`) zeros
+      constexpr int kU = 4;
+      auto rows = [&](int m0, auto whole) __attribute__((always_inline)) {
+        constexpr bool kWhole = decltype(whole)::value;
+        Raw8<ELEM> xr[kU];
+        float t[kU][kBlocks];
+        int m[kU];
+#pragma unroll
+        for (int u = 0; u < kU; ++u) {
+          const int i = m0 + 16 * u + q;
+          m[u] = order[kWhole || i < to ? i : to - 1];
+        }
+#pragma unroll
+        for (int u = 0; u < kU; ++u) {
+          const bool in = kWhole || m0 + 16 * u + q < to;
+          xr[u] = load8<ELEM>(f.X + 2 * ((int64_t)m[u] * f.ldx + col),
+                              kWhole ? 8 : in ? valid : 0);
+#pragma unroll
+          for (int b = 0; b < kBlocks; ++b)
+            t[u][b] = in ? f.T[(int64_t)m[u] * rp + j0 + 16 * b + c] : 0.f;
+        }
+#pragma unroll
+        for (int u = 0; u < kU; ++u) {
+          float x[8];
+          unpack8<ELEM>(xr[u], x);
+#pragma unroll
+          for (int b = 0; b < kBlocks; ++b)
+#pragma unroll
+            for (int e = 0; e < 8; ++e)
+              acc[b][e] = __builtin_amdgcn_mfma_f32_16x16x4f32(t[u][b], x[e], acc[b][e], 0, 0, 0);
+        }
+      };
+      int m0 = at + 4 * w;
+      if (c0 + kFactorCols <= f.C)
+        for (; m0 + 16 * (kU - 1) + 4 <= to; m0 += 16 * kU) rows(m0, std::true_type{});
+      for (; m0 < to; m0 += 16 * kU) rows(m0, std::false_type{});
+      // the waves' sums, 16 ranks at a time: lane holds ranks 4 q .. of column 8 c + e
+#pragma unroll
+      for (int b = 0; b < kBlocks; ++b) {
+        __syncthreads();
+#pragma unroll
+        for (int e = 0; e < 8; ++e) sums[w][e][lane] = acc[b][e];
+        __syncthreads();
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+          const int e = 2 * w + h;
+          f32x4 v = sums[0][e][lane];
+#pragma unroll
+          for (int u = 1; u < 4; ++u) v += sums[u][e][lane];
+          const int cc = col + e, j = j0 + 16 * b + 4 * q;
+          if (cc < f.C) {
+#pragma unroll
+            for (int k = 0; k < 4; ++k)
+              if (j + k < r) out[(j + k) * dj + cc * dc] = v[k];
+          }
+        }
+      }
+    }
+    at = to;
+  }
+}
+
+// Adapters without rows: zeros.  Adapters whose rows lie in several chunks: the
+// sum of their parts.
+__global__ __launch_bounds__(256) void finish_kernel(Factor f0, Factor f1,
+                                                     const int *__restrict__ start, int r, int G,
+                                                     int chunk) {
+  const Factor f = blockIdx.y == 0 ? f0 : f1;
+  const int64_t rc = (int64_t)r * f.C;
+  for (int g = blockIdx.z; g < G; g += gridDim.z) {
+    const int s0 = start[g], s1 = start[g + 1];
+    const int first = s0 / chunk, last = s1 > s0 ? (s1 - 1) / chunk : first;
+    if (s1 > s0 && first == last) continue;
+    for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < rc;
+         i += (int64_t)gridDim.x * 256) {
+      float v = 0.f;
+      if (s1 > s0) {
+        v = f.parts[(2 * (int64_t)first + 1) * rc + i];
+        for (int k = first + 1; k <= last; ++k) v += f.parts[2 * (int64_t)k * rc + i];
+      }
+      const int64_t j = i / f.C, c = i - j * f.C;
+      f.D[g * rc + j * f.dj + c * f.dc] = v;
+    }
+  }
+}
+
+// Rows of a chunk: enough workgroups of 128 columns for the chip, and
+// parts that stay small beside what is read.
+int chunk_rows(int64_t M, int64_t K, int64_t N) {
+  const int64_t strips = (K + kFactorCols - 1) / kFactorCols + (N + kFactorCols - 1) / kFactorCols;
+  int64_t rows = M * strips / 1024;
+  rows = (rows + 63) / 64 * 64;
+  return (int)(rows < 64 ? 64 : rows > 8192 ? 8192 : rows);
+}
+
+// Scratch: the projection's sums, T of X and of dY, the rows in their adapters'
+// order, the adapters transposed, the parts of the factors' gradients.
+struct Scratch {
+  unsigned char *base, *at, *bt;
+  float *t, *dt, *parts_a, *parts_b;
+  int *start, *order;
+  int64_t bytes;
+};
+Scratch scratch(void *work, int64_t M, int64_t K, int64_t N, int64_t r, int64_t G) {
+  Scratch s;
+  int64_t at = 0;
+  auto take = [&](int64_t n) {
+    unsigned char *p = (unsigned char *)work + at;
+    at += round256(n);
+    return p;
+  };
+  s.t = (float *)take(M * rank_pad(r) * 4);
+  s.dt = (float *)take(M * rank_pad(r) * 4);
+  s.start = (int *)take((G + 1) * 4);
+  s.order = (int *)take(M * 4);
+  s.at = take(G * r * K * 2);
+  s.bt = take(G * r * N * 2);
+  const int64_t chunk = chunk_rows(M, K, N), chunks = (M + chunk - 1) / chunk;
+  s.base = take(M * (N > K ? N : K) * 4);
+  s.parts_a = (float *)s.base;      // not of the same call
+  const int64_t a = round256(2 * chunks * r * K * 4), b = round256(2 * chunks * r * N * 4);
+  s.parts_b = (float *)(s.base + a);
+  const int64_t more = a + b - round256(M * (N > K ? N : K) * 4);
+  s.bytes = at + (more > 0 ? more : 0);
+  return s;
 }
 
 unsigned grid_for(int64_t n) { return (unsigned)(n < 1 ? 1 : n < (1 << 16) ? n : 1 << 16); }
 
-template <int ELEM>
-hipError_t narrow(const void *X, int64_t ldx, const void *F, int64_t fj, int64_t fk,
-                  const float *alpha, const int32_t *ids, float *T, int64_t M, int64_t K,
-                  int64_t r, int64_t G, hipStream_t stream) {
-  hipLaunchKernelGGL(narrow_kernel<ELEM>, dim3(grid_for((M + 3) / 4)), dim3(256), 0, stream,
-                     (const unsigned char *)X, ldx, (const unsigned char *)F, fj, fk, alpha, ids,
-                     T, M, K, (int)r, (int)G);
+hipError_t group(const int32_t *ids, const Scratch &s, int64_t M, int64_t G, hipStream_t stream) {
+  hipLaunchKernelGGL(group_kernel, dim3((unsigned)G), dim3(kGroupThreads), 0, stream, ids, s.start,
+                     s.order, (int)M, (int)G);
   return hipGetLastError();
 }
+
+// T of one product, or of two (n1.X not null).
+template <int ELEM>
+hipError_t narrow(const Narrow &n0, const Narrow &n1, const float *alpha, const int32_t *ids,
+                  const int *order, const int *start, int64_t M, int64_t r, int64_t G,
+                  hipStream_t stream) {
+  const int rp = (int)rank_pad(r);
+  auto go = [&](auto rows, auto blocks) {
+    constexpr int kRows = decltype(rows)::value, kBlocks = decltype(blocks)::value;
+    hipLaunchKernelGGL((narrow_kernel<ELEM, kRows, kBlocks>),
+                       dim3((unsigned)((M + 16 * kRows - 1) / (16 * kRows)), n1.X ? 2 : 1),
+                       dim3(512), 0, stream, n0, n1, alpha, ids, order, start, (int)M, (int)r, rp,
+                       (int)G);
+  };
+  auto by_blocks = [&](auto rows) {
+    if (rp == 16)
+      go(rows, std::integral_constant<int, 1>{});
+    else
+      go(rows, std::integral_constant<int, 2>{});
+  };
+  // 32 rows read the factors half as often as 16, as long as they fill the chip
+  if (M >= 8192)
+    by_blocks(std::integral_constant<int, 2>{});
+  else
+    by_blocks(std::integral_constant<int, 1>{});
+  return hipGetLastError();
+}
+
+hipError_t transpose(const void *in, void *out, int64_t G, int64_t rows, int64_t cols,
+                     hipStream_t stream) {
+  const int64_t tiles = G * ((rows + 31) / 32) * ((cols + 31) / 32);
+  if (tiles == 0) return hipSuccess;
+  hipLaunchKernelGGL(transpose_kernel, dim3(grid_for(tiles)), dim3(256), 0, stream,
+                     (const unsigned short *)in, (unsigned short *)out, rows, cols, tiles);
+  return hipGetLastError();
+}
+
+// From how many rows on they are taken in their adapters' order: an order of
+// mixed rows costs a block of 16 rows one product for each of its adapters.
+constexpr int64_t kOrderRows = 1024;
 
 template <int ELEM, int OUT, bool kQ8>
 hipError_t project(int product, const AdapterArgs &a, const Scratch &s, hipStream_t stream,
@@ -139,7 +474,12 @@ hipError_t project(int product, const AdapterArgs &a, const Scratch &s, hipStrea
   hipError_t e = launch_rect(product, 0, p, stream, num_cus);
   if (e != hipSuccess) return e;
   if (a.G > 0) {
-    e = narrow<ELEM>(a.X, a.ldx, a.A, a.K, 1, a.alpha, a.ids, s.t, a.M, a.K, a.r, a.G, stream);
+    const bool ordered = a.M > kOrderRows && a.G > 1;
+    if (ordered) e = group(a.ids, s, a.M, a.G, stream);
+    if (e != hipSuccess) return e;
+    const Narrow n{(const unsigned char *)a.X, (const unsigned char *)a.A, s.t, a.ldx, (int)a.K};
+    e = narrow<ELEM>(n, Narrow{}, a.alpha, a.ids, ordered ? s.order : nullptr, s.start, a.M, a.r,
+                     a.G, stream);
     if (e != hipSuccess) return e;
   }
   hipLaunchKernelGGL((join_kernel<ELEM, OUT, kQ8>), dim3(grid_for((a.M * a.N + 255) / 256)),
@@ -165,21 +505,35 @@ hipError_t project_dt(int dtype, const AdapterArgs &a, const Scratch &s, hipStre
 template <int ELEM>
 hipError_t grad_go(const AdapterGradArgs &a, hipStream_t stream) {
   const Scratch s = scratch(a.work, a.M, a.K, a.N, a.r, a.G);
+  const int rp = (int)rank_pad(a.r);
+  hipError_t e = group(a.ids, s, a.M, a.G, stream);
+  if (e == hipSuccess) e = transpose(a.B, s.bt, a.G, a.N, a.r, stream);
+  if (e != hipSuccess) return e;
+  const unsigned char *X = (const unsigned char *)a.X, *dY = (const unsigned char *)a.dY;
+  const int chunk = chunk_rows(a.M, a.K, a.N);
+  const Factor fa{X, s.dt, a.dA, s.parts_a, a.ldx, a.K, 1, (int)a.K};
+  const Factor fb{dY, s.t, a.dB, s.parts_b, a.lddy, 1, a.r, (int)a.N};
   if (a.M > 0) {
-    hipError_t e = narrow<ELEM>(a.X, a.ldx, a.A, a.K, 1, a.alpha, a.ids, s.t, a.M, a.K, a.r, a.G,
-                                stream);
+    e = narrow<ELEM>(Narrow{X, (const unsigned char *)a.A, s.t, a.ldx, (int)a.K},
+                     Narrow{dY, s.bt, s.dt, a.lddy, (int)a.N}, a.alpha, a.ids, s.order, s.start,
+                     a.M, a.r, a.G, stream);
     if (e != hipSuccess) return e;
-    e = narrow<ELEM>(a.dY, a.lddy, a.B, 1, a.r, a.alpha, a.ids, s.dt, a.M, a.N, a.r, a.G, stream);
+    const int ca = (int)((a.K + kFactorCols - 1) / kFactorCols);
+    const int cb = (int)((a.N + kFactorCols - 1) / kFactorCols);
+    const dim3 grid(ca + cb, (unsigned)((a.M + chunk - 1) / chunk));
+    if (rp == 16)
+      hipLaunchKernelGGL((factor_kernel<ELEM, 1>), grid, dim3(256), 0, stream, fa, fb, a.ids,
+                         s.order, s.start, (int)a.r, rp, (int)a.G, chunk, ca);
+    else
+      hipLaunchKernelGGL((factor_kernel<ELEM, 2>), grid, dim3(256), 0, stream, fa, fb, a.ids,
+                         s.order, s.start, (int)a.r, rp, (int)a.G, chunk, ca);
+    e = hipGetLastError();
     if (e != hipSuccess) return e;
   }
-  hipLaunchKernelGGL(factor_grad_kernel<ELEM>, dim3((unsigned)((a.K + 255) / 256), a.G, a.r),
-                     dim3(256), 0, stream, (const unsigned char *)a.X, a.ldx, (const float *)s.dt,
-                     a.ids, a.dA, a.K, (int64_t)1, a.M, a.K, (int)a.r);
-  hipError_t e = hipGetLastError();
-  if (e != hipSuccess) return e;
-  hipLaunchKernelGGL(factor_grad_kernel<ELEM>, dim3((unsigned)((a.N + 255) / 256), a.G, a.r),
-                     dim3(256), 0, stream, (const unsigned char *)a.dY, a.lddy,
-                     (const float *)s.t, a.ids, a.dB, (int64_t)1, a.r, a.M, a.N, (int)a.r);
+  const int64_t most = a.r * (a.K > a.N ? a.K : a.N);
+  hipLaunchKernelGGL(finish_kernel, dim3(most < 64 * 256 ? (unsigned)((most + 255) / 256) : 64, 2,
+                                         (unsigned)(a.G < 1024 ? a.G : 1024)),
+                     dim3(256), 0, stream, fa, fb, s.start, (int)a.r, (int)a.G, chunk);
   return hipGetLastError();
 }
 
@@ -196,20 +550,13 @@ hipError_t launch_adapter(int dtype, const AdapterArgs &a, hipStream_t stream, i
 hipError_t launch_adapter_input_grad(int dtype, const AdapterArgs &a, hipStream_t stream,
                                      int num_cus) {
   // The adapters' factors change places: A' = B^T (r x K here), B' = A^T (N x r).
-  const Scratch s = scratch(a.work, a.M, a.N, a.K, a.r, a.G);
+  const Scratch s = scratch(a.work, a.M, a.K, a.N, a.r, a.G);
   AdapterArgs b = a;
-  if (a.G > 0) {
-    hipLaunchKernelGGL(transpose_kernel, dim3(1024), dim3(256), 0, stream,
-                       (const unsigned short *)a.B, (unsigned short *)s.bt, a.K, a.r,
-                       a.G * a.K * a.r);
-    hipLaunchKernelGGL(transpose_kernel, dim3(1024), dim3(256), 0, stream,
-                       (const unsigned short *)a.A, (unsigned short *)s.at, a.r, a.N,
-                       a.G * a.r * a.N);
-    const hipError_t e = hipGetLastError();
-    if (e != hipSuccess) return e;
-  }
-  b.A = s.bt;
-  b.B = s.at;
+  hipError_t e = transpose(a.B, s.at, a.G, a.K, a.r, stream);
+  if (e == hipSuccess) e = transpose(a.A, s.bt, a.G, a.r, a.N, stream);
+  if (e != hipSuccess) return e;
+  b.A = s.at;
+  b.B = s.bt;
   return project_dt(dtype, b, s, stream, num_cus);
 }
 
