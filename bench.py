@@ -76,7 +76,7 @@ PROFILES = os.path.join(ROOT, "profiles")
 
 
 def kernel_sources(kind: str):
-    main = {"gemm": ["tcu_gemm.hip"], "rect": ["tcu_gemm.hip"],
+    main = {"gemm": ["tcu_gemm.hip", "tcu_gemm_tiles.h"], "rect": ["tcu_gemm.hip", "tcu_gemm_tiles.h"],
             "poly": ["tcu_poly.hip", "tcu_split.h"],
             "tc": ["tcu_tc.hip", "tcu_tc_diag.h"],
             "dft": ["tcu_dft.hip", "tcu_split.h"],

@@ -5,11 +5,10 @@
 //   Y[m] = X[m] W + alpha[g] (X[m] A_g^T) B_g^T,  g = ids[m]
 //   dA_g = sum_m alpha[g] (dY[m] B_g)^T X[m],  dB_g = sum_m alpha[g] dY[m]^T (X[m] A_g^T)
 //
-// The projection is the blocked product (launch_rect) into scratch, the
-// narrow product T = alpha X A^T is formed by narrow_kernel, and a last pass
-// adds T B^T and rounds.
+// T = alpha X A^T is formed by narrow_kernel; the projection is the blocked
+// product's kernels, T B^T added to their sums before these are stored.
 #include "tcu_elem.h"
-#include "tcu_launch.h"
+#include "tcu_gemm_tiles.h"
 #include "tcu_layer.h"
 
 namespace tcu {
@@ -194,23 +193,204 @@ __global__ __launch_bounds__(512) void narrow_kernel(Narrow n0, Narrow n1,
   }
 }
 
-// Y = base (scaled, 8-bit) + T B^T, rounded once.
+// ---------------------------------------------------------------------------
+// The adapters' part of a product's tile, added to its sums before they are
+// rounded and stored: T B^T for the adapter of every row, after the scales of an
+// 8-bit base.  The sums lie as the matrix cores hold them, 16 columns of 16 rows
+// a block, a lane one row; T (binary32) enters as words of the adapters' type,
+// bfloat16: T = hi + lo (+ lo2 where the output is binary32: 24 bits), binary16:
+// T 2^-e = hi + lo with 2^e the row's largest value, so that no size of T
+// leaves the type's range.  With 16 ranks both words of a rank share one
+// product of 32.  Every adapter's product is formed apart and added by its own
+// rows alone, so that no row sees another adapter's values (a block costs one
+// product per distinct adapter of its 16 rows; summing in place where there is
+// one made the 256 x 256 tiles spill 175 registers).  B's fragments are loaded
+// from the caches, again only where the adapter changes from block to block.
+// ---------------------------------------------------------------------------
 template <int ELEM, int OUT, bool kQ8>
-__global__ __launch_bounds__(256) void join_kernel(AdapterArgs a, const void *base,
-                                                   const float *__restrict__ T) {
-  const int64_t total = a.M * a.N;
+struct AdapterTail {
+  static constexpr bool kOn = true;
+  template <int DT>
+  static constexpr int kOut = OUT;
+  static constexpr int kWords = ELEM == TCU_ELEM_BF16 && OUT != TCU_BF16_BF16 ? 3 : 2;
+
+  const float *T, *xscale, *wscale;
+  const unsigned char *B;      // N x rp of every adapter, at this part's first column
+  const int *ids;
+  int64_t bstride;             // bytes from one adapter's B to the next
+  int rp, G;
+
+  AdapterTail at(int64_t row, int64_t col) const {
+    AdapterTail t = *this;
+    if (G > 0) {
+      t.T += row * rp;
+      t.B += col * rp * 2;
+      t.ids += row;
+    }
+    if (kQ8) {
+      t.xscale += row;
+      t.wscale += col;
+    }
+    return t;
+  }
+
+  // Eight values of T (ranks 8 k .. of a row) as words of the adapters' type;
+  // e: the row's binary exponent (binary16).
+  __device__ __forceinline__ static void words(const float (&t)[8], int e, u32x4 (&w)[kWords]) {
+    float rest[8];
+#pragma unroll
+    for (int i = 0; i < 8; ++i) rest[i] = ELEM == TCU_ELEM_F16 ? ldexpf(t[i], -e) : t[i];
+#pragma unroll
+    for (int k = 0; k < kWords; ++k) {
+      const Raw8<ELEM> r = pack8<ELEM>(rest);
+      float back[8];
+      unpack8<ELEM>(r, back);
+      w[k] = r.v[0];
+#pragma unroll
+      for (int i = 0; i < 8; ++i) {
+        // nothing is left of a value that is not finite
+        const bool fine = (bitcast<unsigned>(back[i]) & 0x7f800000u) != 0x7f800000u;
+        rest[i] = fine ? rest[i] - back[i] : 0.f;
+      }
+    }
+  }
+
+  template <typename Acc, int FN, int FM>
+  __device__ __forceinline__ void apply(Acc (&acc)[FN][FM], int row0, int col0, int M,
+                                        int N) const {
+    const int lane = threadIdx.x & 63, c = lane & 15, q = lane >> 4;
+    constexpr int DT = ELEM == TCU_ELEM_F16 ? TCU_F16_F32 : TCU_BF16_F32;
+    int id[FM];
+    unsigned long long any = 0;
+#pragma unroll
+    for (int fm = 0; fm < FM; ++fm) {
+      const int m = row0 + 16 * fm + c;
+      id[fm] = m < M && G > 0 ? ids[m] : -1;
+      if (id[fm] >= G || id[fm] < 0) id[fm] = -1;
+      any |= __ballot(id[fm] >= 0);
+    }
+    if constexpr (kQ8) {
+      float ws[FN][4];
+#pragma unroll
+      for (int fn = 0; fn < FN; ++fn)
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+          const int n = col0 + 16 * fn + 4 * q + e;
+          ws[fn][e] = wscale[n < N ? n : N - 1];
+        }
+#pragma unroll
+      for (int fm = 0; fm < FM; ++fm) {
+        const int m = row0 + 16 * fm + c;
+        const float xs = xscale[m < M ? m : M - 1];
+#pragma unroll
+        for (int fn = 0; fn < FN; ++fn) {
+          f32x4 v;
+#pragma unroll
+          for (int e = 0; e < 4; ++e) v[e] = (float)bitcast<i32x4>(acc[fn][fm])[e] * xs * ws[fn][e];
+          acc[fn][fm] = bitcast<Acc>(v);
+        }
+      }
+    }
+    if (any == 0) return;
+    // binary16: 2^e brings the row's largest |T| to [2^14, 2^15)
+    int ex[FM];
+    if constexpr (ELEM == TCU_ELEM_F16) {
+#pragma unroll
+      for (int fm = 0; fm < FM; ++fm) {
+        const int m = row0 + 16 * fm + c;
+        unsigned top = 0u;
+        if (id[fm] >= 0)
+          for (int j = 4 * q; j < rp; j += 16) {
+            const u32x4 v = *(const u32x4 *)(T + (int64_t)m * rp + j);
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+              const unsigned b = v[i] & 0x7fffffffu;
+              top = b > top ? b : top;
+            }
+          }
+#pragma unroll
+        for (int s = 16; s <= 32; s <<= 1) {
+          const unsigned o = __shfl_xor(top, s);
+          top = o > top ? o : top;
+        }
+        ex[fm] = top == 0u || top >= 0x7f800000u
+                     ? 0
+                     : __builtin_amdgcn_frexp_expf(bitcast<float>(top)) - 15;
+      }
+    }
+    const bool narrow = rp == 16;
+    const int steps = narrow ? 1 : rp / 32;
+    for (int s = 0; s < steps; ++s) {
+      const int rank = 32 * s + 8 * (narrow ? q & 1 : q);
+      int held = -1;
+      u32x4 wf[FN];
+#pragma unroll
+      for (int fn = 0; fn < FN; ++fn) wf[fn] = u32x4{0u, 0u, 0u, 0u};
+#pragma unroll
+      for (int fm = 0; fm < FM; ++fm) {
+        unsigned left = (unsigned)(__ballot(id[fm] >= 0) & 0xffffu);
+        if (left == 0u) continue;
+        const int m = row0 + 16 * fm + c;
+        float t[8];
+        unpack8<TCU_ELEM_F32>(
+            load8<TCU_ELEM_F32>((const unsigned char *)(T + (int64_t)(m < M ? m : M - 1) * rp + rank),
+                                8),
+            t);
+        u32x4 w[kWords];
+        words(t, ELEM == TCU_ELEM_F16 ? ex[fm] : 0, w);
+        if (narrow) {
+          // lanes of the upper ranks' places take the second word, and of a
+          // third word's product nothing
+          const u32x4 none = {0u, 0u, 0u, 0u};
+          w[0] = q < 2 ? w[0] : w[1];
+          if constexpr (kWords == 3) w[1] = q < 2 ? w[2] : none;
+        }
+        while (left != 0u) {
+          const int g = __builtin_amdgcn_readlane(id[fm], __builtin_ctz(left));
+          const unsigned mine = (unsigned)(__ballot(id[fm] == g) & 0xffffu);
+          left &= ~mine;
+          if (g != held) {
+            held = g;
+#pragma unroll
+            for (int fn = 0; fn < FN; ++fn) {
+              const int n = col0 + 16 * fn + c;
+              wf[fn] = *(const u32x4 *)(B + (int64_t)g * bstride +
+                                        2 * ((int64_t)(n < N ? n : N - 1) * rp + rank));
+            }
+          }
+          auto product = [&](int fn, f32x4 d) __attribute__((always_inline)) {
+            d = mfma_k32(DT, wf[fn], w[0], d);
+            if (kWords == 3 || !narrow) d = mfma_k32(DT, wf[fn], w[1], d);
+            if constexpr (kWords == 3)
+              if (!narrow) d = mfma_k32(DT, wf[fn], w[2], d);
+            return d;
+          };
+          const bool own = id[fm] == g;
+#pragma unroll
+          for (int fn = 0; fn < FN; ++fn) {
+            const f32x4 d = product(fn, f32x4{0.f, 0.f, 0.f, 0.f});
+            f32x4 v = bitcast<f32x4>(acc[fn][fm]);
+#pragma unroll
+            for (int e = 0; e < 4; ++e)
+              v[e] = own ? v[e] + (ELEM == TCU_ELEM_F16 ? ldexpf(d[e], ex[fm]) : d[e]) : v[e];
+            acc[fn][fm] = bitcast<Acc>(v);
+          }
+        }
+      }
+    }
+  }
+};
+
+// B of every adapter with rows of rp ranks, zeros from rank r on.
+__global__ __launch_bounds__(256) void pad_ranks_kernel(const unsigned short *__restrict__ B,
+                                                        unsigned short *__restrict__ out,
+                                                        int64_t rows, int r, int rp) {
+  const int64_t total = rows * rp;
   for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < total;
        i += (int64_t)gridDim.x * 256) {
-    const int64_t m = i / a.N, n = i - m * a.N;
-    float v = kQ8 ? (float)((const int *)base)[i] * a.xscale[m] * a.wscale[n]
-                  : ((const float *)base)[i];
-    const int g = a.G > 0 ? a.ids[m] : -1;
-    if (g >= 0 && g < a.G) {
-      const unsigned char *b = (const unsigned char *)a.B + 2 * (((int64_t)g * a.N + n) * a.r);
-      const float *t = T + m * rank_pad(a.r);
-      for (int j = 0; j < a.r; ++j) v += t[j] * elem_to_f32<ELEM>(b + 2 * j);
-    }
-    f32_to_elem<OUT>((unsigned char *)a.Y + (m * a.ldy + n) * elem_bytes<OUT>, v);
+    const int64_t row = i / rp;
+    const int j = (int)(i - row * rp);
+    out[i] = j < r ? B[row * r + j] : (unsigned short)0;
   }
 }
 
@@ -386,10 +566,10 @@ int chunk_rows(int64_t M, int64_t K, int64_t N) {
   return (int)(rows < 64 ? 64 : rows > 8192 ? 8192 : rows);
 }
 
-// Scratch: the projection's sums, T of X and of dY, the rows in their adapters'
-// order, the adapters transposed, the parts of the factors' gradients.
+// Scratch: T of X and of dY, the rows in their adapters' order, the adapters
+// transposed or with padded ranks, the parts of the factors' gradients.
 struct Scratch {
-  unsigned char *base, *at, *bt;
+  unsigned char *at, *bt, *padded;
   float *t, *dt, *parts_a, *parts_b;
   int *start, *order;
   int64_t bytes;
@@ -409,12 +589,13 @@ Scratch scratch(void *work, int64_t M, int64_t K, int64_t N, int64_t r, int64_t 
   s.at = take(G * r * K * 2);
   s.bt = take(G * r * N * 2);
   const int64_t chunk = chunk_rows(M, K, N), chunks = (M + chunk - 1) / chunk;
-  s.base = take(M * (N > K ? N : K) * 4);
-  s.parts_a = (float *)s.base;      // not of the same call
-  const int64_t a = round256(2 * chunks * r * K * 4), b = round256(2 * chunks * r * N * 4);
-  s.parts_b = (float *)(s.base + a);
-  const int64_t more = a + b - round256(M * (N > K ? N : K) * 4);
-  s.bytes = at + (more > 0 ? more : 0);
+  // padded ranks and the gradients' parts are not of the same call
+  const int64_t pad = round256(G * (N > K ? N : K) * rank_pad(r) * 2);
+  const int64_t pa = round256(2 * chunks * r * K * 4), pb = round256(2 * chunks * r * N * 4);
+  s.padded = take(pad > pa + pb ? pad : pa + pb);
+  s.parts_a = (float *)s.padded;
+  s.parts_b = (float *)(s.padded + pa);
+  s.bytes = at;
   return s;
 }
 
@@ -466,14 +647,21 @@ hipError_t transpose(const void *in, void *out, int64_t G, int64_t rows, int64_t
 // mixed rows costs a block of 16 rows one product for each of its adapters.
 constexpr int64_t kOrderRows = 1024;
 
-template <int ELEM, int OUT, bool kQ8>
-hipError_t project(int product, const AdapterArgs &a, const Scratch &s, hipStream_t stream,
-                   int num_cus) {
-  const RectArgs p{kQ8 ? a.Xq : a.X, kQ8 ? a.ldxq : a.ldx, a.W, a.ldw, s.base, a.N,
-                   a.M, a.K, a.N, false};
-  hipError_t e = launch_rect(product, 0, p, stream, num_cus);
-  if (e != hipSuccess) return e;
+template <int ELEM, int DT, int OUT, bool kQ8>
+hipError_t project(const AdapterArgs &a, const Scratch &s, hipStream_t stream, int num_cus) {
+  const int64_t rp = rank_pad(a.r);
+  const void *B = a.B;
+  hipError_t e = hipSuccess;
   if (a.G > 0) {
+    if (rp != a.r) {
+      const int64_t rows = a.G * a.N;
+      hipLaunchKernelGGL(pad_ranks_kernel, dim3(grid_for((rows * rp + 255) / 256)), dim3(256), 0,
+                         stream, (const unsigned short *)a.B, (unsigned short *)s.padded, rows,
+                         (int)a.r, (int)rp);
+      e = hipGetLastError();
+      if (e != hipSuccess) return e;
+      B = s.padded;
+    }
     const bool ordered = a.M > kOrderRows && a.G > 1;
     if (ordered) e = group(a.ids, s, a.M, a.G, stream);
     if (e != hipSuccess) return e;
@@ -482,22 +670,24 @@ hipError_t project(int product, const AdapterArgs &a, const Scratch &s, hipStrea
                      a.G, stream);
     if (e != hipSuccess) return e;
   }
-  hipLaunchKernelGGL((join_kernel<ELEM, OUT, kQ8>), dim3(grid_for((a.M * a.N + 255) / 256)),
-                     dim3(256), 0, stream, a, (const void *)s.base, (const float *)s.t);
-  return hipGetLastError();
+  const AdapterTail<ELEM, OUT, kQ8> tail{s.t, a.xscale, a.wscale, (const unsigned char *)B,
+                                         a.ids, a.N * rp * 2, (int)rp, (int)a.G};
+  const RectArgs p{kQ8 ? a.Xq : a.X, kQ8 ? a.ldxq : a.ldx, a.W, a.ldw, a.Y, a.ldy,
+                   a.M, a.K, a.N, false};
+  return launch_dt<DT>(p, stream, num_cus, tail);
 }
 
 hipError_t project_dt(int dtype, const AdapterArgs &a, const Scratch &s, hipStream_t stream,
                       int num_cus) {
   switch (dtype) {
     case TCU_F16_F32:
-      return project<TCU_ELEM_F16, TCU_ELEM_F32, false>(TCU_F16_F32, a, s, stream, num_cus);
+      return project<TCU_ELEM_F16, TCU_F16_F32, TCU_F16_F32, false>(a, s, stream, num_cus);
     case TCU_BF16_F32:
-      return project<TCU_ELEM_BF16, TCU_ELEM_F32, false>(TCU_BF16_F32, a, s, stream, num_cus);
+      return project<TCU_ELEM_BF16, TCU_BF16_F32, TCU_BF16_F32, false>(a, s, stream, num_cus);
     case TCU_BF16_BF16:
-      return project<TCU_ELEM_BF16, TCU_ELEM_BF16, false>(TCU_BF16_F32, a, s, stream, num_cus);
+      return project<TCU_ELEM_BF16, TCU_BF16_BF16, TCU_BF16_BF16, false>(a, s, stream, num_cus);
     case TCU_I8_I32:
-      return project<TCU_ELEM_BF16, TCU_ELEM_BF16, true>(TCU_I8_I32, a, s, stream, num_cus);
+      return project<TCU_ELEM_BF16, TCU_I8_I32, TCU_BF16_BF16, true>(a, s, stream, num_cus);
   }
   return hipErrorInvalidValue;
 }
