@@ -21,7 +21,8 @@ PROBE_SRC = "tcu_probe.hip"
 PROBE_LIB = os.path.join(HERE, "libtcu_probe.so")
 BUILD_DIR = os.path.join(ROOT, "_build")
 SOURCES = ["tcu_abi.cpp", "tcu_tall.hip", "tcu_gemm.hip", "tcu_poly.hip", "tcu_tc.hip",
-           "tcu_dft.hip", "tcu_layer_abi.cpp", "tcu_norm.hip", "tcu_adapter.hip", "tcu_clip.hip"]
+           "tcu_dft.hip", "tcu_layer_abi.cpp", "tcu_norm.hip", "tcu_adapter.hip", "tcu_few.hip",
+           "tcu_clip.hip"]
 ARCH = "gfx950"
 
 COMMON = ["-O3", "-std=c++17", "-fPIC", "-fvisibility=hidden",

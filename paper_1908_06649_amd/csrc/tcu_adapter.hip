@@ -572,6 +572,7 @@ struct Scratch {
   unsigned char *at, *bt, *padded;
   float *t, *dt, *parts_a, *parts_b;
   int *start, *order;
+  void *few;
   int64_t bytes;
 };
 Scratch scratch(void *work, int64_t M, int64_t K, int64_t N, int64_t r, int64_t G) {
@@ -595,6 +596,8 @@ Scratch scratch(void *work, int64_t M, int64_t K, int64_t N, int64_t r, int64_t 
   s.padded = take(pad > pa + pb ? pad : pa + pb);
   s.parts_a = (float *)s.padded;
   s.parts_b = (float *)(s.padded + pa);
+  const int64_t fa = few_work_bytes(M, K, N, r), fb = few_work_bytes(M, N, K, r);
+  s.few = take(fa > fb ? fa : fb);
   s.bytes = at;
   return s;
 }
@@ -679,6 +682,11 @@ hipError_t project(const AdapterArgs &a, const Scratch &s, hipStream_t stream, i
 
 hipError_t project_dt(int dtype, const AdapterArgs &a, const Scratch &s, hipStream_t stream,
                       int num_cus) {
+  if (few_ok(dtype, a)) {
+    AdapterArgs b = a;
+    b.work = s.few;
+    return launch_few(dtype, b, stream);
+  }
   switch (dtype) {
     case TCU_F16_F32:
       return project<TCU_ELEM_F16, TCU_F16_F32, TCU_F16_F32, false>(a, s, stream, num_cus);

@@ -1,0 +1,348 @@
+// A projection with low-rank adapters for few rows (single tokens of a batch of
+// requests): bound by the weights' bytes, read once.
+//
+// few_kernel forms the product's partial sums and T = alpha X A^T in one launch,
+// join_kernel adds the partial sums and T B^T and rounds.
+//   * A workgroup's 16 or 8 waves share a strip of W's columns (64 of 16 bits, 128 of
+//     8) over one of `splits` ranges of the contracted index, about one workgroup
+//     per CU in all; the waves take the steps of 64 bytes of it in turn, for all
+//     rows.  A lane loads 8 bytes of each of a step's 8 (16) rows of W that it
+//     holds, 16 lanes a whole row of the strip, and exchanges bytes in its own
+//     registers to the runs along the contracted index that the matrix cores
+//     take: W goes through neither LDS nor another lane.  The next step's loads
+//     are in flight under a step's products.
+//   * The waves' sums are added in LDS in their order, the ranges' by join_kernel.
+//   * The other workgroups form T, one row each, a rank per wave: every row has an
+//     adapter of its own, and both operands lie along the contracted index.
+#include "tcu_elem.h"
+#include "tcu_layer.h"
+
+namespace tcu {
+namespace {
+
+// A workgroup's waves: 16 where a wave's sums and two steps of W fit 128
+// registers (16-bit W, up to 32 rows), else 8.
+__host__ __device__ constexpr int few_waves(int es, int row_blocks) {
+  return es == 2 && row_blocks <= 2 ? 16 : 8;
+}
+
+// How a step of W lies: ES bytes per element, kRun elements of the contracted
+// index per lane, kCols columns per lane (8 bytes).
+template <int ES>
+struct Step {
+  static constexpr int kRun = 16 / ES, kElems = 4 * kRun, kCols = 8 / ES, kStrip = 16 * kCols;
+};
+
+__device__ __forceinline__ u32x2 load8_any(const unsigned char *p) {
+  typedef u32x2 u32x2_any __attribute__((aligned(1)));
+  return *(const u32x2_any *)p;
+}
+
+// A lane's kRun rows of 8 bytes -> its columns' runs of 16 bytes.
+template <int ES>
+__device__ __forceinline__ void to_runs(const u32x2 (&w)[16 / ES], u32x4 (&run)[8 / ES]) {
+  if constexpr (ES == 2) {
+#pragma unroll
+    for (int j = 0; j < 4; ++j)
+#pragma unroll
+      for (int d = 0; d < 4; ++d)
+        run[j][d] = __builtin_amdgcn_perm(w[2 * d + 1][j >> 1], w[2 * d][j >> 1],
+                                          j & 1 ? 0x07060302u : 0x05040100u);
+  } else {
+#pragma unroll
+    for (int h = 0; h < 2; ++h)
+#pragma unroll
+      for (int d = 0; d < 4; ++d) {
+        // 4 x 4 bytes: rows 4 d .. of columns 4 h ..
+        const unsigned a = w[4 * d][h], b = w[4 * d + 1][h], c = w[4 * d + 2][h],
+                       e = w[4 * d + 3][h];
+        const unsigned ab0 = __builtin_amdgcn_perm(b, a, 0x05010400u);
+        const unsigned ab2 = __builtin_amdgcn_perm(b, a, 0x07030602u);
+        const unsigned ce0 = __builtin_amdgcn_perm(e, c, 0x05010400u);
+        const unsigned ce2 = __builtin_amdgcn_perm(e, c, 0x07030602u);
+        run[4 * h][d] = __builtin_amdgcn_perm(ce0, ab0, 0x05040100u);
+        run[4 * h + 1][d] = __builtin_amdgcn_perm(ce0, ab0, 0x07060302u);
+        run[4 * h + 2][d] = __builtin_amdgcn_perm(ce2, ab2, 0x05040100u);
+        run[4 * h + 3][d] = __builtin_amdgcn_perm(ce2, ab2, 0x07060302u);
+      }
+  }
+}
+
+struct FewArgs {
+  const unsigned char *X, *W;      // the product's operands
+  const unsigned char *XA, *A;     // the adapters'
+  const float *alpha;
+  const int *ids;
+  unsigned *parts;                 // splits x M x N sums (binary32 or int32)
+  float *T;                        // M x r
+  int64_t ldx, ldw, ldxa;
+  int M, K, N, r, G, strips, splits;
+};
+
+// T of one row.
+template <int ELEM, int kWaves>
+__device__ __forceinline__ void narrow_row(const FewArgs &a, int m) {
+  const int g = a.ids[m];
+  if (g < 0 || g >= a.G) return;
+  const int lane = threadIdx.x & 63, w = threadIdx.x >> 6;
+  const unsigned char *x = a.XA + 2 * ((int64_t)m * a.ldxa + 8 * lane);
+  for (int j = w; j < a.r; j += kWaves) {
+    const unsigned char *f = a.A + 2 * (((int64_t)g * a.r + j) * a.K + 8 * lane);
+    float s = 0.f;
+    auto add = [&](const Raw8<ELEM> &xr, const Raw8<ELEM> &fr) {
+      float xv[8], fv[8];
+      unpack8<ELEM>(xr, xv);
+      unpack8<ELEM>(fr, fv);
+#pragma unroll
+      for (int e = 0; e < 8; ++e) s += xv[e] * fv[e];
+    };
+    int k = 0;
+    constexpr int kU = 4;
+    for (; k + 512 * kU <= a.K; k += 512 * kU) {
+      Raw8<ELEM> xr[kU], fr[kU];
+#pragma unroll
+      for (int u = 0; u < kU; ++u) {
+        xr[u].v[0] = load16_any(x + 2 * (k + 512 * u));
+        fr[u].v[0] = load16_any(f + 2 * (k + 512 * u));
+      }
+#pragma unroll
+      for (int u = 0; u < kU; ++u) add(xr[u], fr[u]);
+    }
+    for (; k < a.K; k += 512) {
+      const int valid = a.K - k - 8 * lane;
+      if (valid > 0) add(load8<ELEM>(x + 2 * k, valid), load8<ELEM>(f + 2 * k, valid));
+    }
+    s = wave_sum(s);
+    if (lane == 0) a.T[(int64_t)m * a.r + j] = s * a.alpha[g];
+  }
+}
+
+// DT: the product's types; ELEM: the adapters'; kMB: blocks of 16 rows.
+template <int DT, int ELEM, int kMB>
+__global__ __launch_bounds__(64 * few_waves(in_bytes(DT), kMB)) void few_kernel(FewArgs a) {
+  constexpr int ES = in_bytes(DT), kWaves = few_waves(ES, kMB);
+  constexpr bool kI8 = ES == 1;
+  typedef Step<ES> S;
+  typedef typename std::conditional<kI8, i32x4, f32x4>::type Acc;
+  constexpr int kRowLds = S::kStrip + 4;
+  __shared__ unsigned sums[kWaves][16 * kRowLds];
+  const int product = a.strips * a.splits;
+  if ((int)blockIdx.x >= product) {
+    narrow_row<ELEM, kWaves>(a, blockIdx.x - product);
+    return;
+  }
+  const int split = blockIdx.x / a.strips, n0 = (blockIdx.x - split * a.strips) * S::kStrip;
+  const int lane = threadIdx.x & 63, w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int c = lane & 15, q = lane >> 4;
+  const int steps = (a.K + S::kElems - 1) / S::kElems;
+  const int s_begin = (int)((int64_t)steps * split / a.splits);
+  const int s_end = (int)((int64_t)steps * (split + 1) / a.splits);
+  // columns past N repeat the last ones inside and are not stored
+  const int col = min(n0 + S::kCols * c, a.N - S::kCols);
+  const unsigned char *wp = a.W + ((int64_t)S::kRun * q * a.ldw + col) * ES;
+  const unsigned char *xp[kMB];
+#pragma unroll
+  for (int b = 0; b < kMB; ++b)
+    xp[b] = a.X + ((int64_t)min(16 * b + c, a.M - 1) * a.ldx + S::kRun * q) * ES;
+  Acc acc[kMB][S::kCols];
+#pragma unroll
+  for (int b = 0; b < kMB; ++b)
+#pragma unroll
+    for (int j = 0; j < S::kCols; ++j) acc[b][j] = Acc{0, 0, 0, 0};
+
+  auto load = [&](int s, u32x2 (&wr)[S::kRun], u32x4 (&xr)[kMB]) __attribute__((always_inline)) {
+    const int k = s * S::kElems, left = a.K - k;
+    if (left >= S::kElems) {
+      const unsigned char *p = wp + (int64_t)k * a.ldw * ES;
+#pragma unroll
+      for (int i = 0; i < S::kRun; ++i) wr[i] = load8_any(p + (int64_t)i * a.ldw * ES);
+#pragma unroll
+      for (int b = 0; b < kMB; ++b) xr[b] = load16_any(xp[b] + (int64_t)k * ES);
+    } else {
+      // the last step: zeros past K
+#pragma unroll
+      for (int i = 0; i < S::kRun; ++i) {
+        const int row = S::kRun * q + i;
+        wr[i] = load8_any(wp + ((int64_t)(min(row, left - 1) - S::kRun * q) + k) * a.ldw * ES);
+        if (row >= left) wr[i] = u32x2{0u, 0u};
+      }
+#pragma unroll
+      for (int b = 0; b < kMB; ++b)
+        xr[b] = load_chunk<ES>(xp[b] + (int64_t)k * ES, max(min(left - S::kRun * q, S::kRun), 0));
+    }
+  };
+  auto multiply = [&](const u32x2 (&wr)[S::kRun], const u32x4 (&xr)[kMB])
+      __attribute__((always_inline)) {
+    u32x4 run[S::kCols];
+    to_runs<ES>(wr, run);
+#pragma unroll
+    for (int j = 0; j < S::kCols; ++j)
+#pragma unroll
+      for (int b = 0; b < kMB; ++b) {
+        if constexpr (kI8)
+          acc[b][j] = mfma_i8_k64(run[j], xr[b], acc[b][j]);
+        else
+          acc[b][j] = mfma_k32(DT, run[j], xr[b], acc[b][j]);
+      }
+  };
+  u32x2 w0[S::kRun], w1[S::kRun];
+  u32x4 x0[kMB], x1[kMB];
+  int s = s_begin + w;
+  if (s < s_end) load(s, w0, x0);
+  for (; s < s_end; s += 2 * kWaves) {
+    if (s + kWaves < s_end) load(s + kWaves, w1, x1);
+    multiply(w0, x0);
+    if (s + kWaves >= s_end) break;
+    if (s + 2 * kWaves < s_end) load(s + 2 * kWaves, w0, x0);
+    multiply(w1, x1);
+  }
+  // The waves' sums, 16 rows at a time: a lane holds column kCols (4 q + e) + j
+  // of the strip and row c of the block.
+#pragma unroll
+  for (int b = 0; b < kMB; ++b) {
+    if (16 * b >= a.M) break;
+    if (b > 0) __syncthreads();   // read before the next sums overwrite
+#pragma unroll
+    for (int j = 0; j < S::kCols; ++j)
+#pragma unroll
+      for (int e = 0; e < 4; ++e)
+        sums[w][c * kRowLds + S::kCols * (4 * q + e) + j] = bitcast<u32x4>(acc[b][j])[e];
+    __syncthreads();
+#pragma unroll
+    for (int i = threadIdx.x; i < 16 * S::kStrip; i += 64 * kWaves) {
+      const int m = i / S::kStrip, at = i % S::kStrip;
+      unsigned v = sums[0][m * kRowLds + at];
+#pragma unroll
+      for (int u = 1; u < kWaves; ++u) {
+        const unsigned o = sums[u][m * kRowLds + at];
+        v = kI8 ? v + o : bitcast<unsigned>(bitcast<float>(v) + bitcast<float>(o));
+      }
+      const int first = n0 + at / S::kCols * S::kCols;
+      const int n = min(first, a.N - S::kCols) + at % S::kCols;
+      if (16 * b + m < a.M && n >= first)
+        a.parts[((int64_t)split * a.M + 16 * b + m) * a.N + n] = v;
+    }
+  }
+}
+
+// Y = the ranges' sums (scaled, 8-bit) + T B^T, rounded once.
+template <int ELEM, int OUT, bool kQ8>
+__global__ __launch_bounds__(256) void join_kernel(FewArgs f, const unsigned char *__restrict__ B,
+                                                   const float *__restrict__ xscale,
+                                                   const float *__restrict__ wscale,
+                                                   unsigned char *__restrict__ Y, int64_t ldy) {
+  const int n = blockIdx.x * 256 + threadIdx.x, m = blockIdx.y;
+  if (n >= f.N) return;
+  const unsigned *p = f.parts + (int64_t)m * f.N + n;
+  const int64_t range = (int64_t)f.M * f.N;
+  float v;
+  if constexpr (kQ8) {
+    int sum = 0;
+    for (int s = 0; s < f.splits; ++s) sum += (int)p[s * range];
+    v = (float)sum * xscale[m] * wscale[n];
+  } else {
+    v = 0.f;
+    for (int s = 0; s < f.splits; ++s) v += bitcast<float>(p[s * range]);
+  }
+  const int g = f.G > 0 ? f.ids[m] : -1;
+  if (g >= 0 && g < f.G) {
+    const unsigned char *b = B + 2 * (((int64_t)g * f.N + n) * f.r);
+    const float *t = f.T + (int64_t)m * f.r;
+    float low = 0.f;
+    for (int j = 0; j < f.r; j += 8) {
+      float x[8];
+      const int valid = f.r - j;
+      unpack8<ELEM>(load8<ELEM>(b + 2 * j, valid), x);
+#pragma unroll
+      for (int e = 0; e < 8; ++e)
+        if (e < valid) low += t[j + e] * x[e];
+    }
+    v += low;
+  }
+  f32_to_elem<OUT>(Y + ((int64_t)m * ldy + n) * elem_bytes<OUT>, v);
+}
+
+int row_blocks(int64_t M) { return M <= 16 ? 1 : M <= 32 ? 2 : 4; }
+
+int strip_cols(bool q8) { return q8 ? Step<1>::kStrip : Step<2>::kStrip; }
+
+// Ranges of the contracted index: about one workgroup per compute unit, and a
+// step at least for every wave.
+int few_splits(int64_t M, int64_t K, int64_t N, bool q8) {
+  const int64_t strips = N > 0 ? (N + strip_cols(q8) - 1) / strip_cols(q8) : 1;
+  const int64_t wave_elems = (int64_t)(q8 ? 64 : 32) * few_waves(q8 ? 1 : 2, row_blocks(M));
+  int64_t n = (256 + strips / 2) / strips;
+  const int64_t most = (K + wave_elems - 1) / wave_elems;
+  if (n > most) n = most;
+  return (int)(n < 1 ? 1 : n > 16 ? 16 : n);
+}
+
+int64_t parts_bytes(int64_t M, int64_t K, int64_t N, bool q8) {
+  return (few_splits(M, K, N, q8) * M * N * 4 + 255) / 256 * 256;
+}
+
+template <int DT, int ELEM, int OUT, bool kQ8>
+hipError_t few(const AdapterArgs &a, hipStream_t stream) {
+  const int strips = (int)((a.N + strip_cols(kQ8) - 1) / strip_cols(kQ8));
+  const int splits = few_splits(a.M, a.K, a.N, kQ8);
+  const FewArgs f{(const unsigned char *)(kQ8 ? a.Xq : a.X),
+                  (const unsigned char *)a.W,
+                  (const unsigned char *)a.X,
+                  (const unsigned char *)a.A,
+                  a.alpha,
+                  a.ids,
+                  (unsigned *)a.work,
+                  (float *)((unsigned char *)a.work + parts_bytes(a.M, a.K, a.N, kQ8)),
+                  kQ8 ? a.ldxq : a.ldx,
+                  a.ldw,
+                  a.ldx,
+                  (int)a.M,
+                  (int)a.K,
+                  (int)a.N,
+                  (int)a.r,
+                  (int)a.G,
+                  strips,
+                  splits};
+  const dim3 grid(strips * splits + (a.G > 0 ? (unsigned)a.M : 0u));
+  auto go = [&](auto blocks) {
+    constexpr int kMB = decltype(blocks)::value;
+    hipLaunchKernelGGL((few_kernel<DT, ELEM, kMB>), grid,
+                       dim3(64 * few_waves(kQ8 ? 1 : 2, kMB)), 0, stream, f);
+  };
+  switch (row_blocks(a.M)) {
+    case 1: go(std::integral_constant<int, 1>{}); break;
+    case 2: go(std::integral_constant<int, 2>{}); break;
+    default: go(std::integral_constant<int, 4>{});
+  }
+  const hipError_t e = hipGetLastError();
+  if (e != hipSuccess) return e;
+  hipLaunchKernelGGL((join_kernel<ELEM, OUT, kQ8>),
+                     dim3((unsigned)((a.N + 255) / 256), (unsigned)a.M), dim3(256), 0, stream, f,
+                     (const unsigned char *)a.B, a.xscale, a.wscale, (unsigned char *)a.Y, a.ldy);
+  return hipGetLastError();
+}
+
+}  // namespace
+
+// A strip's loads take 8 columns at least; a launch's blocks count in 31 bits.
+bool few_ok(int dtype, const AdapterArgs &a) {
+  return a.M <= kFewRows && a.K > 0 && a.N >= (dtype == TCU_I8_I32 ? 8 : 4);
+}
+
+int64_t few_work_bytes(int64_t M, int64_t K, int64_t N, int64_t r) {
+  if (M > kFewRows) return 0;
+  const int64_t a = parts_bytes(M, K, N, false), b = parts_bytes(M, K, N, true);
+  return (a > b ? a : b) + M * r * 4;
+}
+
+hipError_t launch_few(int dtype, const AdapterArgs &a, hipStream_t stream) {
+  switch (dtype) {
+    case TCU_F16_F32: return few<TCU_F16_F32, TCU_ELEM_F16, TCU_ELEM_F32, false>(a, stream);
+    case TCU_BF16_F32: return few<TCU_BF16_F32, TCU_ELEM_BF16, TCU_ELEM_F32, false>(a, stream);
+    case TCU_BF16_BF16: return few<TCU_BF16_BF16, TCU_ELEM_BF16, TCU_ELEM_BF16, false>(a, stream);
+    case TCU_I8_I32: return few<TCU_I8_I32, TCU_ELEM_BF16, TCU_ELEM_BF16, true>(a, stream);
+  }
+  return hipErrorInvalidValue;
+}
+
+}  // namespace tcu

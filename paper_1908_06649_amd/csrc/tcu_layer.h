@@ -58,6 +58,12 @@ hipError_t launch_adapter_grad(int elem, const AdapterGradArgs &a, hipStream_t s
 // the product dY Wt (its contracted index and columns).
 hipError_t launch_adapter_input_grad(int dtype, const AdapterArgs &a, hipStream_t stream,
                                      int num_cus);
+// The same for few rows (see tcu_few.hip), with work of few_work_bytes; the
+// sizes it takes, by few_ok.
+constexpr int64_t kFewRows = 64;
+bool few_ok(int dtype, const AdapterArgs &a);
+hipError_t launch_few(int dtype, const AdapterArgs &a, hipStream_t stream);
+int64_t few_work_bytes(int64_t M, int64_t K, int64_t N, int64_t r);
 int64_t adapter_work_bytes(int64_t M, int64_t K, int64_t N, int64_t r, int64_t G);
 
 hipError_t launch_clip(const void *const *grads, void *const *outs, const int64_t *counts,

@@ -108,7 +108,8 @@ def test_work_sizes():
     assert lib.tcu_rms_norm_grad_work(-1, 4) == -1 and lib.tcu_rms_norm_grad_work(4, 0) == -1
     assert lib.tcu_adapter_work(-1, 4, 4, 4, 4) == -1 and lib.tcu_adapter_work(4, 4, 4, 129, 4) == -1
     assert lib.tcu_adapter_work(BIG, BIG, BIG, 16, 4) >= -1
-    for size in ((1, 1, 1, 1, 0), (0, 64, 64, 16, 2), (5000, 4096, 4096, 16, 8)):
+    for size in ((1, 1, 1, 1, 0), (0, 64, 64, 16, 2), (5, 0, 64, 16, 2), (5, 64, 0, 16, 2),
+                 (0, 0, 0, 1, 0), (64, 8192, 8192, 128, 65536), (5000, 4096, 4096, 16, 8)):
         assert 0 <= lib.tcu_adapter_work(*size) < 1 << 40
     assert lib.tcu_clip_grads_work() > 0
 
