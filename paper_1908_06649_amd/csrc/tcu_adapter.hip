@@ -22,62 +22,80 @@ __host__ __device__ constexpr int64_t rank_pad(int64_t r) { return r <= 16 ? 16 
 // ---------------------------------------------------------------------------
 // The rows in the order of their adapters, the rows of one in their own order:
 // order[start[g] .. start[g + 1]) are g's, start[G] the rows that have one.
-// Workgroup g counts the rows of smaller numbers, then places its own: 1024
-// lanes by ballots, so the order is fixed.
+// Workgroup g counts the rows of smaller numbers, then places its own; every
+// lane a run of consecutive rows, so the order is fixed.
 // ---------------------------------------------------------------------------
-constexpr int kGroupThreads = 1024;
+constexpr int kGroupThreads = 1024, kGroupHeld = 8;
 __global__ __launch_bounds__(kGroupThreads) void group_kernel(const int *__restrict__ ids,
                                                               int *__restrict__ start,
                                                               int *__restrict__ order, int M,
                                                               int G) {
   constexpr int kWaves = kGroupThreads / 64;
-  __shared__ int part[kWaves];
+  __shared__ int below_of[kWaves], own_of[kWaves];
   const int lane = threadIdx.x & 63, w = threadIdx.x >> 6, g = blockIdx.x;
+  const int per = (M + kGroupThreads - 1) / kGroupThreads;
+  const int64_t first = (int64_t)threadIdx.x * per;
+  const int mine = first < M ? (M - first < per ? (int)(M - first) : per) : 0;
+  // up to kGroupHeld numbers a lane stay in registers between the two passes
+  int held[kGroupHeld];
   int below = 0, own = 0;
-  for (int m = threadIdx.x; m < M; m += kGroupThreads) {
-    const int id = ids[m];
-    below += id >= 0 && id < g;
-    own += id == g;
-  }
+  if (per <= kGroupHeld) {
 #pragma unroll
-  for (int s = 32; s > 0; s >>= 1) below += __shfl_xor(below, s);
-  own = __any(own > 0);
-  if (lane == 0) part[w] = below;
-  const int some = __syncthreads_or(own);
-  below = 0;
+    for (int i = 0; i < kGroupHeld; ++i) held[i] = i < mine ? ids[first + i] : -1;
 #pragma unroll
-  for (int i = 0; i < kWaves; ++i) below += part[i];
-  if (threadIdx.x == 0) start[g] = below;
-  int at = below;
-  if (some) {
-    for (int m0 = 0; m0 < M; m0 += kGroupThreads) {
-      const int m = m0 + threadIdx.x;
-      const bool mine = m < M && ids[m] == g;
-      const unsigned long long votes = __ballot(mine);
-      __syncthreads();   // part has been read
-      if (lane == 0) part[w] = __popcll(votes);
-      __syncthreads();
-      int before = __popcll(votes & ((1ull << lane) - 1)), total = 0;
-#pragma unroll
-      for (int i = 0; i < kWaves; ++i) {
-        before += i < w ? part[i] : 0;
-        total += part[i];
-      }
-      if (mine) order[at + before] = m;
-      at += total;
+    for (int i = 0; i < kGroupHeld; ++i) {
+      below += held[i] >= 0 && held[i] < g;
+      own += held[i] == g;
+    }
+  } else {
+    for (int i = 0; i < mine; ++i) {
+      const int id = ids[first + i];
+      below += id >= 0 && id < g;
+      own += id == g;
     }
   }
-  if (g == G - 1 && threadIdx.x == 0) start[G] = at;
+  // sums over the lanes before this one and over all
+  int upto = own;
+#pragma unroll
+  for (int s = 1; s < 64; s <<= 1) {
+    const int o = __shfl_up(upto, s);
+    upto += lane >= s ? o : 0;
+    below += __shfl_xor(below, s);
+  }
+  if (lane == 63) own_of[w] = upto;
+  if (lane == 0) below_of[w] = below;
+  __syncthreads();
+  int base = 0, total = 0, before = upto - own;
+#pragma unroll
+  for (int i = 0; i < kWaves; ++i) {
+    base += below_of[i];
+    total += own_of[i];
+    before += i < w ? own_of[i] : 0;
+  }
+  if (threadIdx.x == 0) start[g] = base;
+  if (g == G - 1 && threadIdx.x == 0) start[G] = base + total;
+  if (own == 0) return;
+  int at = base + before;
+  if (per <= kGroupHeld) {
+#pragma unroll
+    for (int i = 0; i < kGroupHeld; ++i)
+      if (held[i] == g) order[at++] = (int)first + i;
+  } else {
+    for (int i = 0; i < mine; ++i)
+      if (ids[first + i] == g) order[at++] = (int)first + i;
+  }
 }
 
 // ---------------------------------------------------------------------------
 // T[m][j] = alpha[g] sum_k X[m][k] F_g[j][k] (F_g: r x K, rows contiguous), zeros
 // from rank r on to rank_pad.  A workgroup takes 16 kRows rows (of `order` if
-// given, else as they lie) and all ranks; its 8 waves take every eighth 64
-// elements of K, and their sums are added in their order.  Both operands are
-// loaded as the matrix cores take them, 16 bytes of a row per lane: X from
-// memory once, F from the caches.  Rows of several adapters are multiplied by
-// each of them, a row keeping its own adapter's result.
+// given, else as they lie) and all ranks; its 16 waves take every sixteenth 64
+// elements of K, and their sums are added in their order.  A load instruction
+// fetches 8 whole lines of 128 bytes (X from memory once, F from the caches); a
+// wave turns them into the matrix cores' operands through its own part of LDS,
+// 16-byte chunks XOR-swizzled by the row, without barriers.  Rows of several
+// adapters are multiplied by each of them, a row keeping its own adapter's
+// result.
 // ---------------------------------------------------------------------------
 struct Narrow {
   const unsigned char *X, *F;
@@ -86,18 +104,20 @@ struct Narrow {
   int K;
 };
 template <int ELEM, int kRows, int kBlocks>
-__global__ __launch_bounds__(512) void narrow_kernel(Narrow n0, Narrow n1,
-                                                     const float *__restrict__ alpha,
-                                                     const int *__restrict__ ids,
-                                                     const int *__restrict__ order,
-                                                     const int *__restrict__ start, int M, int r,
-                                                     int rp, int G) {
+__global__ __launch_bounds__(1024) void narrow_kernel(Narrow n0, Narrow n1,
+                                                      const float *__restrict__ alpha,
+                                                      const int *__restrict__ ids,
+                                                      const int *__restrict__ order,
+                                                      const int *__restrict__ start, int M, int r,
+                                                      int rp, int G) {
   constexpr int DT = ELEM == TCU_ELEM_F16 ? TCU_F16_F32 : TCU_BF16_F32;
-  constexpr int kWaves = 8, kStep = 64;
-  __shared__ f32x4 sums[kWaves][kRows * kBlocks][64];
+  constexpr int kWaves = 16, kStep = 64, kPart = (kRows + kBlocks) * 2048;
+  static_assert(kRows * kBlocks * 1024 <= kPart, "a wave's sums");
+  __shared__ __attribute__((aligned(128))) unsigned char lds[kWaves * kPart];
   const Narrow n = blockIdx.y == 0 ? n0 : n1;
   const int lane = threadIdx.x & 63, w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int c = lane & 15, q = lane >> 4;
+  const int lr = lane >> 3, lc = lane & 7;      // a load's row and chunk
   const int count = order ? start[G] : M;
   const int first = blockIdx.x * (16 * kRows);
   if (first >= count) return;
@@ -111,9 +131,17 @@ __global__ __launch_bounds__(512) void narrow_kernel(Narrow n0, Narrow n1,
     if (id[i] >= G || id[i] < 0) id[i] = -1;
     left |= (unsigned)(__ballot(id[i] >= 0) & 0xffffu) << (16 * i);
   }
-  const unsigned char *x[kRows];
+  const unsigned char *x[kRows][2];
 #pragma unroll
-  for (int i = 0; i < kRows; ++i) x[i] = n.X + 2 * ((int64_t)row[i] * n.ldx + 8 * q);
+  for (int i = 0; i < kRows; ++i)
+#pragma unroll
+    for (int h = 0; h < 2; ++h)
+      x[i][h] = n.X + 2 * ((int64_t)__shfl(row[i], 8 * h + lr) * n.ldx + 8 * lc);
+  unsigned char *const mine_lds = lds + w * kPart;
+  unsigned char *const put = mine_lds + lr * 128 + 16 * (lc ^ lr);
+  const unsigned char *get[2];
+#pragma unroll
+  for (int h = 0; h < 2; ++h) get[h] = mine_lds + c * 128 + 16 * ((4 * h + q) ^ (c & 7));
   while (left != 0u) {
     // the adapter of the first row left, and its rows
     const int lead = __builtin_ctz(left);
@@ -126,59 +154,93 @@ __global__ __launch_bounds__(512) void narrow_kernel(Narrow n0, Narrow n1,
     for (int i = 0; i < kRows; ++i)
       mine |= (unsigned)(__ballot(id[i] == g) & 0xffffu) << (16 * i);
     left &= ~mine;
-    const unsigned char *fg = n.F + 2 * ((int64_t)g * r * n.K + 8 * q);
+    const unsigned char *fg = n.F + 2 * ((int64_t)g * r * n.K + 8 * lc);
     const float al = alpha[g];
     for (int j0 = 0; j0 < rp; j0 += 16 * kBlocks) {
-      const unsigned char *f[kBlocks];
+      const unsigned char *f[kBlocks][2];
       f32x4 acc[kRows][kBlocks];
 #pragma unroll
       for (int b = 0; b < kBlocks; ++b) {
-        const int j = j0 + 16 * b + c;
-        f[b] = fg + 2 * (int64_t)(j < r ? j : r - 1) * n.K;
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+          const int j = j0 + 16 * b + 8 * h + lr;
+          f[b][h] = fg + 2 * (int64_t)(j < r ? j : r - 1) * n.K;
+        }
 #pragma unroll
         for (int i = 0; i < kRows; ++i) acc[i][b] = f32x4{0.f, 0.f, 0.f, 0.f};
       }
-      // kU chunks of 64 elements, their loads in flight together
-      auto step = [&](int k, auto chunks, auto whole) __attribute__((always_inline)) {
-        constexpr int kU = decltype(chunks)::value;
-        u32x4 xv[kU][2][kRows], fv[kU][2][kBlocks];
-#pragma unroll
-        for (int u = 0; u < kU; ++u)
+      struct Chunk {
+        u32x4 x[kRows][2], f[kBlocks][2];
+      };
+      auto load = [&](int k, Chunk &v) __attribute__((always_inline)) {
+        if (k + kStep <= n.K) {
 #pragma unroll
           for (int h = 0; h < 2; ++h) {
-            const int at = k + u * kWaves * kStep + 32 * h;
-            const int valid = decltype(whole)::value ? 8 : n.K - at - 8 * q;
 #pragma unroll
-            for (int i = 0; i < kRows; ++i) xv[u][h][i] = load8<ELEM>(x[i] + 2 * at, valid).v[0];
+            for (int i = 0; i < kRows; ++i) v.x[i][h] = load16_any(x[i][h] + 2 * k);
 #pragma unroll
-            for (int b = 0; b < kBlocks; ++b) fv[u][h][b] = load8<ELEM>(f[b] + 2 * at, valid).v[0];
+            for (int b = 0; b < kBlocks; ++b) v.f[b][h] = load16_any(f[b][h] + 2 * k);
           }
+        } else {
+          // zeros past K
+          const int valid = n.K - k - 8 * lc;
 #pragma unroll
-        for (int u = 0; u < kU; ++u)
+          for (int h = 0; h < 2; ++h) {
 #pragma unroll
-          for (int h = 0; h < 2; ++h)
+            for (int i = 0; i < kRows; ++i) v.x[i][h] = load8<ELEM>(x[i][h] + 2 * k, valid).v[0];
 #pragma unroll
-            for (int i = 0; i < kRows; ++i)
-#pragma unroll
-              for (int b = 0; b < kBlocks; ++b)
-                acc[i][b] = mfma_k32(DT, fv[u][h][b], xv[u][h][i], acc[i][b]);
+            for (int b = 0; b < kBlocks; ++b) v.f[b][h] = load8<ELEM>(f[b][h] + 2 * k, valid).v[0];
+          }
+        }
       };
+      auto multiply = [&](const Chunk &v) __attribute__((always_inline)) {
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+#pragma unroll
+          for (int i = 0; i < kRows; ++i) *(u32x4 *)(put + 2048 * i + 1024 * h) = v.x[i][h];
+#pragma unroll
+          for (int b = 0; b < kBlocks; ++b)
+            *(u32x4 *)(put + 2048 * (kRows + b) + 1024 * h) = v.f[b][h];
+        }
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+          u32x4 xf[kRows], ff[kBlocks];
+#pragma unroll
+          for (int i = 0; i < kRows; ++i) xf[i] = *(const u32x4 *)(get[h] + 2048 * i);
+#pragma unroll
+          for (int b = 0; b < kBlocks; ++b) ff[b] = *(const u32x4 *)(get[h] + 2048 * (kRows + b));
+#pragma unroll
+          for (int i = 0; i < kRows; ++i)
+#pragma unroll
+            for (int b = 0; b < kBlocks; ++b) acc[i][b] = mfma_k32(DT, ff[b], xf[i], acc[i][b]);
+        }
+      };
+      // kAhead chunks in flight
+      constexpr int kAhead = kRows * kBlocks == 1 ? 4 : 2, kNext = kWaves * kStep;
+      Chunk v[kAhead];
       int k = w * kStep;
-      constexpr int kU = kRows == 1 ? 4 : 2, kFar = (kU - 1) * kWaves * kStep;
-      for (; k + kFar + kStep <= n.K; k += kU * kWaves * kStep)
-        step(k, std::integral_constant<int, kU>{}, std::true_type{});
-      for (; k + kStep <= n.K; k += kWaves * kStep)
-        step(k, std::integral_constant<int, 1>{}, std::true_type{});
-      if (k < n.K) step(k, std::integral_constant<int, 1>{}, std::false_type{});
+#pragma unroll
+      for (int u = 0; u < kAhead; ++u)
+        if (k + u * kNext < n.K) load(k + u * kNext, v[u]);
+      while (k < n.K) {
+#pragma unroll
+        for (int u = 0; u < kAhead; ++u) {
+          if (k >= n.K) break;
+          multiply(v[u]);
+          if (k + kAhead * kNext < n.K) load(k + kAhead * kNext, v[u]);
+          k += kNext;
+        }
+      }
 #pragma unroll
       for (int i = 0; i < kRows; ++i)
 #pragma unroll
-        for (int b = 0; b < kBlocks; ++b) sums[w][i * kBlocks + b][lane] = acc[i][b];
+        for (int b = 0; b < kBlocks; ++b)
+          *(f32x4 *)(mine_lds + (i * kBlocks + b) * 1024 + 16 * lane) = acc[i][b];
       __syncthreads();
       for (int s = w; s < kRows * kBlocks; s += kWaves) {
-        f32x4 v = sums[0][s][lane];
+        f32x4 v = *(const f32x4 *)(lds + s * 1024 + 16 * lane);
 #pragma unroll
-        for (int u = 1; u < kWaves; ++u) v += sums[u][s][lane];
+        for (int u = 1; u < kWaves; ++u) v += *(const f32x4 *)(lds + u * kPart + s * 1024 + 16 * lane);
         // ranks j .. j + 3 of row c of the block
         const int i = s / kBlocks, j = j0 + 16 * (s % kBlocks) + 4 * q;
         int m = row[0];
@@ -215,16 +277,16 @@ struct AdapterTail {
   static constexpr int kWords = ELEM == TCU_ELEM_BF16 && OUT != TCU_BF16_BF16 ? 3 : 2;
 
   const float *T, *xscale, *wscale;
-  const unsigned char *B;      // N x rp of every adapter, at this part's first column
+  const unsigned char *B;      // N x rb of every adapter, at this part's first column
   const int *ids;
   int64_t bstride;             // bytes from one adapter's B to the next
-  int rp, G;
+  int rp, rb, G;               // rb: a multiple of 8, at most rp
 
   AdapterTail at(int64_t row, int64_t col) const {
     AdapterTail t = *this;
     if (G > 0) {
       t.T += row * rp;
-      t.B += col * rp * 2;
+      t.B += col * rb * 2;
       t.ids += row;
     }
     if (kQ8) {
@@ -354,8 +416,10 @@ struct AdapterTail {
 #pragma unroll
             for (int fn = 0; fn < FN; ++fn) {
               const int n = col0 + 16 * fn + c;
-              wf[fn] = *(const u32x4 *)(B + (int64_t)g * bstride +
-                                        2 * ((int64_t)(n < N ? n : N - 1) * rp + rank));
+              // past the ranks: zeros, as T has them
+              wf[fn] = rank < rb ? *(const u32x4 *)(B + (int64_t)g * bstride +
+                                                    2 * ((int64_t)(n < N ? n : N - 1) * rb + rank))
+                                 : u32x4{0u, 0u, 0u, 0u};
             }
           }
           auto product = [&](int fn, f32x4 d) __attribute__((always_inline)) {
@@ -381,7 +445,8 @@ struct AdapterTail {
   }
 };
 
-// B of every adapter with rows of rp ranks, zeros from rank r on.
+// B of every adapter with rows of rp ranks, zeros from rank r on (ranks that are
+// no multiple of 8).
 __global__ __launch_bounds__(256) void pad_ranks_kernel(const unsigned short *__restrict__ B,
                                                         unsigned short *__restrict__ out,
                                                         int64_t rows, int r, int rp) {
@@ -548,8 +613,15 @@ __global__ __launch_bounds__(256) void finish_kernel(Factor f0, Factor f1,
          i += (int64_t)gridDim.x * 256) {
       float v = 0.f;
       if (s1 > s0) {
-        v = f.parts[(2 * (int64_t)first + 1) * rc + i];
-        for (int k = first + 1; k <= last; ++k) v += f.parts[2 * (int64_t)k * rc + i];
+        const float *p = f.parts + 2 * (int64_t)first * rc + i;
+        v = p[rc];
+        p += 2 * rc;
+        int k = first + 1;
+        for (; k + 4 <= last + 1; k += 4, p += 8 * rc) {
+          const float u0 = p[0], u1 = p[2 * rc], u2 = p[4 * rc], u3 = p[6 * rc];
+          v = v + u0 + u1 + u2 + u3;
+        }
+        for (; k <= last; ++k, p += 2 * rc) v += p[0];
       }
       const int64_t j = i / f.C, c = i - j * f.C;
       f.D[g * rc + j * f.dj + c * f.dc] = v;
@@ -620,7 +692,7 @@ hipError_t narrow(const Narrow &n0, const Narrow &n1, const float *alpha, const 
     constexpr int kRows = decltype(rows)::value, kBlocks = decltype(blocks)::value;
     hipLaunchKernelGGL((narrow_kernel<ELEM, kRows, kBlocks>),
                        dim3((unsigned)((M + 16 * kRows - 1) / (16 * kRows)), n1.X ? 2 : 1),
-                       dim3(512), 0, stream, n0, n1, alpha, ids, order, start, (int)M, (int)r, rp,
+                       dim3(1024), 0, stream, n0, n1, alpha, ids, order, start, (int)M, (int)r, rp,
                        (int)G);
   };
   auto by_blocks = [&](auto rows) {
@@ -652,15 +724,15 @@ constexpr int64_t kOrderRows = 1024;
 
 template <int ELEM, int DT, int OUT, bool kQ8>
 hipError_t project(const AdapterArgs &a, const Scratch &s, hipStream_t stream, int num_cus) {
-  const int64_t rp = rank_pad(a.r);
+  const int64_t rp = rank_pad(a.r), rb = (a.r + 7) / 8 * 8;
   const void *B = a.B;
   hipError_t e = hipSuccess;
   if (a.G > 0) {
-    if (rp != a.r) {
+    if (rb != a.r) {
       const int64_t rows = a.G * a.N;
-      hipLaunchKernelGGL(pad_ranks_kernel, dim3(grid_for((rows * rp + 255) / 256)), dim3(256), 0,
+      hipLaunchKernelGGL(pad_ranks_kernel, dim3(grid_for((rows * rb + 255) / 256)), dim3(256), 0,
                          stream, (const unsigned short *)a.B, (unsigned short *)s.padded, rows,
-                         (int)a.r, (int)rp);
+                         (int)a.r, (int)rb);
       e = hipGetLastError();
       if (e != hipSuccess) return e;
       B = s.padded;
@@ -674,7 +746,7 @@ hipError_t project(const AdapterArgs &a, const Scratch &s, hipStream_t stream, i
     if (e != hipSuccess) return e;
   }
   const AdapterTail<ELEM, OUT, kQ8> tail{s.t, a.xscale, a.wscale, (const unsigned char *)B,
-                                         a.ids, a.N * rp * 2, (int)rp, (int)a.G};
+                                         a.ids, a.N * rb * 2, (int)rp, (int)rb, (int)a.G};
   const RectArgs p{kQ8 ? a.Xq : a.X, kQ8 ? a.ldxq : a.ldx, a.W, a.ldw, a.Y, a.ldy,
                    a.M, a.K, a.N, false};
   return launch_dt<DT>(p, stream, num_cus, tail);
@@ -729,7 +801,7 @@ hipError_t grad_go(const AdapterGradArgs &a, hipStream_t stream) {
     if (e != hipSuccess) return e;
   }
   const int64_t most = a.r * (a.K > a.N ? a.K : a.N);
-  hipLaunchKernelGGL(finish_kernel, dim3(most < 64 * 256 ? (unsigned)((most + 255) / 256) : 64, 2,
+  hipLaunchKernelGGL(finish_kernel, dim3(most < 512 * 256 ? (unsigned)((most + 255) / 256) : 512, 2,
                                          (unsigned)(a.G < 1024 ? a.G : 1024)),
                      dim3(256), 0, stream, fa, fb, s.start, (int)a.r, (int)a.G, chunk);
   return hipGetLastError();

@@ -31,13 +31,18 @@ struct Table {
 };
 static_assert(sizeof(Table) + 64 <= 4096, "kernel arguments");
 
-// Calls f(tensor, first element, elements) for every gridDim.x'th chunk.
-template <typename F>
+// Calls f(tensor, first element, elements) for every gridDim.x'th chunk, from
+// the first on or (kBack) from the last.
+template <bool kBack, typename F>
 __device__ __forceinline__ void walk(const Table &t, F f) {
   const unsigned total = t.first[t.tensors];
-  int i = 0;
-  for (unsigned c = blockIdx.x; c < total; c += gridDim.x) {
-    while (c >= t.first[i + 1]) ++i;
+  int i = kBack ? t.tensors - 1 : 0;
+  for (unsigned b = blockIdx.x; b < total; b += gridDim.x) {
+    const unsigned c = kBack ? total - 1 - b : b;
+    if constexpr (kBack)
+      while (c < t.first[i]) --i;
+    else
+      while (c >= t.first[i + 1]) ++i;
     const int64_t at = (int64_t)(c - t.first[i]) * kChunk;
     const int64_t left = t.count[i] - at;
     f(i, at, (int)(left < kChunk ? left : kChunk));
@@ -74,7 +79,7 @@ __global__ __launch_bounds__(256) void clip_norm_kernel(Table t, double *__restr
                                                         int more) {
   __shared__ double lds[4];
   double s = 0.0;
-  walk(t, [&](int i, int64_t at, int n) {
+  walk<false>(t, [&](int i, int64_t at, int n) {
     switch (t.elem[i]) {
       case TCU_ELEM_F32: s += chunk_squares<TCU_ELEM_F32>(t.g[i] + at * 4, n); break;
       case TCU_ELEM_F16: s += chunk_squares<TCU_ELEM_F16>(t.g[i] + at * 2, n); break;
@@ -111,7 +116,8 @@ __device__ __forceinline__ void chunk_scale(const unsigned char *g, unsigned cha
   }
 }
 
-// Every workgroup adds the parts in the same order, then scales its chunks.
+// Every workgroup adds the parts in the same order, then scales its chunks, the
+// ones read last first: they are still in the caches.
 __global__ __launch_bounds__(256) void clip_scale_kernel(Table t, const double *__restrict__ parts,
                                                          float max_norm,
                                                          float *__restrict__ result, int write) {
@@ -129,7 +135,7 @@ __global__ __launch_bounds__(256) void clip_scale_kernel(Table t, const double *
     result[0] = (float)norm;
     result[1] = coef;
   }
-  walk(t, [&](int i, int64_t at, int n) {
+  walk<true>(t, [&](int i, int64_t at, int n) {
     if (coef == 1.f && t.out[i] == t.g[i]) return;   // in place and unchanged
     switch (t.elem[i]) {
       case TCU_ELEM_F32:

@@ -121,6 +121,8 @@ __device__ __forceinline__ void narrow_row(const FewArgs &a, int m) {
 template <int DT, int ELEM, int kMB>
 __global__ __launch_bounds__(64 * few_waves(in_bytes(DT), kMB)) void few_kernel(FewArgs a) {
   constexpr int ES = in_bytes(DT), kWaves = few_waves(ES, kMB);
+  // 8-bit W and more than 32 rows: a second step's registers are not there
+  constexpr bool kAhead = ES == 2 || kMB <= 2;
   constexpr bool kI8 = ES == 1;
   typedef Step<ES> S;
   typedef typename std::conditional<kI8, i32x4, f32x4>::type Acc;
@@ -185,16 +187,25 @@ __global__ __launch_bounds__(64 * few_waves(in_bytes(DT), kMB)) void few_kernel(
           acc[b][j] = mfma_k32(DT, run[j], xr[b], acc[b][j]);
       }
   };
-  u32x2 w0[S::kRun], w1[S::kRun];
-  u32x4 x0[kMB], x1[kMB];
   int s = s_begin + w;
-  if (s < s_end) load(s, w0, x0);
-  for (; s < s_end; s += 2 * kWaves) {
-    if (s + kWaves < s_end) load(s + kWaves, w1, x1);
-    multiply(w0, x0);
-    if (s + kWaves >= s_end) break;
-    if (s + 2 * kWaves < s_end) load(s + 2 * kWaves, w0, x0);
-    multiply(w1, x1);
+  if constexpr (kAhead) {
+    u32x2 w0[S::kRun], w1[S::kRun];
+    u32x4 x0[kMB], x1[kMB];
+    if (s < s_end) load(s, w0, x0);
+    for (; s < s_end; s += 2 * kWaves) {
+      if (s + kWaves < s_end) load(s + kWaves, w1, x1);
+      multiply(w0, x0);
+      if (s + kWaves >= s_end) break;
+      if (s + 2 * kWaves < s_end) load(s + 2 * kWaves, w0, x0);
+      multiply(w1, x1);
+    }
+  } else {
+    for (; s < s_end; s += kWaves) {
+      u32x2 w0[S::kRun];
+      u32x4 x0[kMB];
+      load(s, w0, x0);
+      multiply(w0, x0);
+    }
   }
   // The waves' sums, 16 rows at a time: a lane holds column kCols (4 q + e) + j
   // of the strip and row c of the block.
@@ -262,7 +273,7 @@ __global__ __launch_bounds__(256) void join_kernel(FewArgs f, const unsigned cha
   f32_to_elem<OUT>(Y + ((int64_t)m * ldy + n) * elem_bytes<OUT>, v);
 }
 
-int row_blocks(int64_t M) { return M <= 16 ? 1 : M <= 32 ? 2 : 4; }
+int row_blocks(int64_t M) { return M <= 16 ? 1 : (int)((M + 15) / 16); }
 
 int strip_cols(bool q8) { return q8 ? Step<1>::kStrip : Step<2>::kStrip; }
 
@@ -312,6 +323,7 @@ hipError_t few(const AdapterArgs &a, hipStream_t stream) {
   switch (row_blocks(a.M)) {
     case 1: go(std::integral_constant<int, 1>{}); break;
     case 2: go(std::integral_constant<int, 2>{}); break;
+    case 3: go(std::integral_constant<int, 3>{}); break;
     default: go(std::integral_constant<int, 4>{});
   }
   const hipError_t e = hipGetLastError();

@@ -676,23 +676,25 @@ def tcu_clip_grads(grads, outs, max_norm: float, result, work,
     _dtypes(where, _F32, result)
     L = _lib or lib()
     dev, (pres, pwork) = _addresses(where, (), ((result, 2),), work, L.tcu_clip_grads_work())
-    elems, counts = [], []
-    for g, o in zip(grads, outs):
-        code = _ELEMS.get(g.dtype)
-        if code is None:
-            raise TcuError(TCU_ERR_UNSUPPORTED, f"{where}: element type {g.dtype}")
-        if o.dtype != g.dtype or o.numel() != g.numel():
+    import torch
+    T = torch.Tensor
+    # one pass of each check over all tensors: a call may have hundreds
+    types, counts = [g.dtype for g in grads], list(map(T.numel, grads))
+    try:
+        elems = [_ELEMS[t] for t in types]
+    except KeyError as e:
+        raise TcuError(TCU_ERR_UNSUPPORTED, f"{where}: element type {e.args[0]}") from None
+    if outs is not grads:
+        if [o.dtype for o in outs] != types or list(map(T.numel, outs)) != counts:
             raise ValueError(f"{where}: an output differs from its gradient in type or size")
-        if g.get_device() != dev or o.get_device() != dev:
+    for ts in (grads,) if outs is grads else (grads, outs):
+        if any(d != dev for d in map(T.get_device, ts)):
             raise ValueError(f"{where}: all tensors must be on the same HIP device")
-        if not (g.is_contiguous() and o.is_contiguous()):
+        if not all(map(T.is_contiguous, ts)):
             raise ValueError(f"{where}: tensors must be contiguous")
-        elems.append(code)
-        counts.append(g.numel())
-    _check(L.tcu_clip_grads((_vp * n)(*[g.data_ptr() for g in grads]),
-                            (_vp * n)(*[o.data_ptr() for o in outs]), (_i64 * n)(*counts),
-                            (ctypes.c_int32 * n)(*elems), n, max_norm, pres, pwork,
-                            _stream_of(dev, stream_ptr)), where)
+    _check(L.tcu_clip_grads((_vp * n)(*map(T.data_ptr, grads)), (_vp * n)(*map(T.data_ptr, outs)),
+                            (_i64 * n)(*counts), (ctypes.c_int32 * n)(*elems), n, max_norm, pres,
+                            pwork, _stream_of(dev, stream_ptr)), where)
 
 
 # --------------------------------------------------------- cost accounting
