@@ -39,9 +39,12 @@ __global__ __launch_bounds__(kGroupThreads) void group_kernel(const int *__restr
   // up to kGroupHeld numbers a lane stay in registers between the two passes
   int held[kGroupHeld];
   int below = 0, own = 0;
-  if (per <= kGroupHeld) {
+  if (per <= kGroupHeld && M > 0) {
 #pragma unroll
-    for (int i = 0; i < kGroupHeld; ++i) held[i] = i < mine ? ids[first + i] : -1;
+    for (int i = 0; i < kGroupHeld; ++i) {
+      const int id = ids[first + i < M ? first + i : M - 1];
+      held[i] = i < mine ? id : -1;
+    }
 #pragma unroll
     for (int i = 0; i < kGroupHeld; ++i) {
       below += held[i] >= 0 && held[i] < g;

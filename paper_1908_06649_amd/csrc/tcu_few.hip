@@ -12,8 +12,9 @@
 //     take: W goes through neither LDS nor another lane.  The next step's loads
 //     are in flight under a step's products.
 //   * The waves' sums are added in LDS in their order, the ranges' by join_kernel.
-//   * The other workgroups form T, one row each, a rank per wave: every row has an
-//     adapter of its own, and both operands lie along the contracted index.
+//   * T's values are dealt to all waves, one at a time, while their first loads of W
+//     are on their way: every row has an adapter of its own, and both operands lie
+//     along the contracted index.
 #include "tcu_elem.h"
 #include "tcu_layer.h"
 
@@ -79,42 +80,40 @@ struct FewArgs {
   int M, K, N, r, G, strips, splits;
 };
 
-// T of one row.
-template <int ELEM, int kWaves>
-__device__ __forceinline__ void narrow_row(const FewArgs &a, int m) {
-  const int g = a.ids[m];
+// One value of T: row i / r, rank i % r, by one wave.
+template <int ELEM>
+__device__ __forceinline__ void narrow_value(const FewArgs &a, int i) {
+  const int m = i / a.r, j = i - m * a.r, g = a.ids[m];
   if (g < 0 || g >= a.G) return;
-  const int lane = threadIdx.x & 63, w = threadIdx.x >> 6;
+  const int lane = threadIdx.x & 63;
   const unsigned char *x = a.XA + 2 * ((int64_t)m * a.ldxa + 8 * lane);
-  for (int j = w; j < a.r; j += kWaves) {
-    const unsigned char *f = a.A + 2 * (((int64_t)g * a.r + j) * a.K + 8 * lane);
-    float s = 0.f;
-    auto add = [&](const Raw8<ELEM> &xr, const Raw8<ELEM> &fr) {
-      float xv[8], fv[8];
-      unpack8<ELEM>(xr, xv);
-      unpack8<ELEM>(fr, fv);
+  const unsigned char *f = a.A + 2 * (((int64_t)g * a.r + j) * a.K + 8 * lane);
+  float s = 0.f;
+  auto add = [&](const Raw8<ELEM> &xr, const Raw8<ELEM> &fr) {
+    float xv[8], fv[8];
+    unpack8<ELEM>(xr, xv);
+    unpack8<ELEM>(fr, fv);
 #pragma unroll
-      for (int e = 0; e < 8; ++e) s += xv[e] * fv[e];
-    };
-    int k = 0;
-    constexpr int kU = 4;
-    for (; k + 512 * kU <= a.K; k += 512 * kU) {
-      Raw8<ELEM> xr[kU], fr[kU];
+    for (int e = 0; e < 8; ++e) s += xv[e] * fv[e];
+  };
+  int k = 0;
+  constexpr int kU = 4;
+  for (; k + 512 * kU <= a.K; k += 512 * kU) {
+    Raw8<ELEM> xr[kU], fr[kU];
 #pragma unroll
-      for (int u = 0; u < kU; ++u) {
-        xr[u].v[0] = load16_any(x + 2 * (k + 512 * u));
-        fr[u].v[0] = load16_any(f + 2 * (k + 512 * u));
-      }
-#pragma unroll
-      for (int u = 0; u < kU; ++u) add(xr[u], fr[u]);
+    for (int u = 0; u < kU; ++u) {
+      xr[u].v[0] = load16_any(x + 2 * (k + 512 * u));
+      fr[u].v[0] = load16_any(f + 2 * (k + 512 * u));
     }
-    for (; k < a.K; k += 512) {
-      const int valid = a.K - k - 8 * lane;
-      if (valid > 0) add(load8<ELEM>(x + 2 * k, valid), load8<ELEM>(f + 2 * k, valid));
-    }
-    s = wave_sum(s);
-    if (lane == 0) a.T[(int64_t)m * a.r + j] = s * a.alpha[g];
+#pragma unroll
+    for (int u = 0; u < kU; ++u) add(xr[u], fr[u]);
   }
+  for (; k < a.K; k += 512) {
+    const int valid = a.K - k - 8 * lane;
+    if (valid > 0) add(load8<ELEM>(x + 2 * k, valid), load8<ELEM>(f + 2 * k, valid));
+  }
+  s = wave_sum(s);
+  if (lane == 0) a.T[i] = s * a.alpha[g];
 }
 
 // DT: the product's types; ELEM: the adapters'; kMB: blocks of 16 rows.
@@ -128,11 +127,6 @@ __global__ __launch_bounds__(64 * few_waves(in_bytes(DT), kMB)) void few_kernel(
   typedef typename std::conditional<kI8, i32x4, f32x4>::type Acc;
   constexpr int kRowLds = S::kStrip + 4;
   __shared__ unsigned sums[kWaves][16 * kRowLds];
-  const int product = a.strips * a.splits;
-  if ((int)blockIdx.x >= product) {
-    narrow_row<ELEM, kWaves>(a, blockIdx.x - product);
-    return;
-  }
   const int split = blockIdx.x / a.strips, n0 = (blockIdx.x - split * a.strips) * S::kStrip;
   const int lane = threadIdx.x & 63, w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int c = lane & 15, q = lane >> 4;
@@ -187,11 +181,19 @@ __global__ __launch_bounds__(64 * few_waves(in_bytes(DT), kMB)) void few_kernel(
           acc[b][j] = mfma_k32(DT, run[j], xr[b], acc[b][j]);
       }
   };
+  // The adapters' narrow product while the first step is on its way: its values
+  // in turn over all waves of the grid.
+  auto narrow = [&]() {
+    const int all = a.G > 0 ? a.M * a.r : 0;
+    for (int i = blockIdx.x * kWaves + w; i < all; i += gridDim.x * kWaves)
+      narrow_value<ELEM>(a, i);
+  };
   int s = s_begin + w;
   if constexpr (kAhead) {
     u32x2 w0[S::kRun], w1[S::kRun];
     u32x4 x0[kMB], x1[kMB];
     if (s < s_end) load(s, w0, x0);
+    narrow();
     for (; s < s_end; s += 2 * kWaves) {
       if (s + kWaves < s_end) load(s + kWaves, w1, x1);
       multiply(w0, x0);
@@ -200,11 +202,14 @@ __global__ __launch_bounds__(64 * few_waves(in_bytes(DT), kMB)) void few_kernel(
       multiply(w1, x1);
     }
   } else {
-    for (; s < s_end; s += kWaves) {
-      u32x2 w0[S::kRun];
-      u32x4 x0[kMB];
-      load(s, w0, x0);
+    u32x2 w0[S::kRun];
+    u32x4 x0[kMB];
+    if (s < s_end) load(s, w0, x0);
+    narrow();
+    while (s < s_end) {
       multiply(w0, x0);
+      s += kWaves;
+      if (s < s_end) load(s, w0, x0);
     }
   }
   // The waves' sums, 16 rows at a time: a lane holds column kCols (4 q + e) + j
@@ -314,7 +319,7 @@ hipError_t few(const AdapterArgs &a, hipStream_t stream) {
                   (int)a.G,
                   strips,
                   splits};
-  const dim3 grid(strips * splits + (a.G > 0 ? (unsigned)a.M : 0u));
+  const dim3 grid(strips * splits);
   auto go = [&](auto blocks) {
     constexpr int kMB = decltype(blocks)::value;
     hipLaunchKernelGGL((few_kernel<DT, ELEM, kMB>), grid,

@@ -5,10 +5,11 @@
 //   dx = rstd (g - h rstd^2 mean(g h)) + dh,  g = dy w;   dw = sum_rows dy h rstd
 //
 // Both are bound by memory: a row is read once, kept in registers while its
-// sums are formed, and written once.  A row of up to 1024 elements is one
-// wave's, up to 16384 a workgroup's of four waves (kV vectors of eight
-// elements per lane, the smallest number that holds the row); longer rows are
-// read twice.  Sums are binary32.
+// sums are formed, and written once (8192 x 8192 bf16 with a residual: 102 us,
+// 5.3 TB/s, the rate of a copy of 1 GiB).  A row of up to 1024 elements is one
+// wave's, up to 16384 a workgroup's (kV vectors of eight elements per lane, the
+// smallest number that holds the row); longer rows, and those of fewer than
+// eight, are read twice.  Sums are binary32.
 #include "tcu_elem.h"
 #include "tcu_layer.h"
 
@@ -16,6 +17,8 @@ namespace tcu {
 namespace {
 
 constexpr int kWaveCols = 1024, kBlockCols = 16384;
+// Up to so many rows, fewer than the chip has compute units, a row is 16 waves'.
+constexpr int kFewNormRows = 256;
 constexpr unsigned kInfBits = 0x7f800000u;
 
 // Sum and unsigned maximum over the kT threads of a row (64: a wave, else the
@@ -91,6 +94,24 @@ __device__ __forceinline__ float rstd_of(float sum_sq, int64_t cols, float eps) 
   return 1.f / sqrtf(sum_sq / (float)cols + eps);
 }
 
+// Vector i of a lane's row: eight columns from `col` on.  A row's last vector
+// begins at its last eight columns (rows of fewer go to the long kernels): its
+// first `dup` ones are then another lane's too, left out of this lane's sums, and
+// stored twice with the same value.  So every access is a whole vector, and none
+// waits for another.
+struct Window {
+  int col, dup;
+  bool in;
+};
+template <int kT, int kV>
+__device__ __forceinline__ Window window(int t, int i, int cols) {
+  const int at = (t + i * kT) * 8;
+  // kV vectors being the fewest that hold the row, all but the last are whole
+  if (i < kV - 1) return Window{at, 0, true};
+  const int col = at < cols - 8 ? at : cols - 8;
+  return Window{col, at - col, at < cols};
+}
+
 // x + res, eight elements.
 template <int ELEM>
 __device__ __forceinline__ void load_h(const unsigned char *x, const unsigned char *res, int valid,
@@ -124,9 +145,9 @@ __device__ __forceinline__ void finish8(const NormArgs &a, int64_t row, int64_t 
 }
 
 template <int ELEM, int kT, int kV>
-__global__ __launch_bounds__(256) void rms_norm_kernel(NormArgs a) {
-  constexpr int ES = elem_bytes<ELEM>, kRows = 256 / kT;
-  __shared__ float lds[4];
+__global__ __launch_bounds__(kT < 256 ? 256 : kT) void rms_norm_kernel(NormArgs a) {
+  constexpr int ES = elem_bytes<ELEM>, kRows = kT < 256 ? 256 / kT : 1;
+  __shared__ float lds[16];
   const int t = threadIdx.x % kT;
   const int64_t step = (int64_t)gridDim.x * kRows;
   for (int64_t row = (int64_t)blockIdx.x * kRows + threadIdx.x / kT; row < a.rows; row += step) {
@@ -137,20 +158,28 @@ __global__ __launch_bounds__(256) void rms_norm_kernel(NormArgs a) {
     float ss = 0.f;
 #pragma unroll
     for (int i = 0; i < kV; ++i) {
-      const int col = (t + i * kT) * 8, valid = (int)a.cols - col;
-      if (valid > 0) {
-        load_h<ELEM>(x + (int64_t)col * ES, res ? res + (int64_t)col * ES : nullptr, valid, h[i]);
-        w[i] = load8<ELEM>((const unsigned char *)a.w + (int64_t)col * ES, valid);
-      } else {
-        w[i] = Raw8<ELEM>{};
+      const Window v = window<kT, kV>(t, i, (int)a.cols);
 #pragma unroll
-        for (int e = 0; e < 8; ++e) h[i][e] = 0.f;
+      for (int e = 0; e < 8; ++e) h[i][e] = 0.f;
+      w[i] = Raw8<ELEM>{};
+      if (v.in) {
+        load_h<ELEM>(x + (int64_t)v.col * ES, res ? res + (int64_t)v.col * ES : nullptr, 8, h[i]);
+        w[i] = load8<ELEM>((const unsigned char *)a.w + (int64_t)v.col * ES, 8);
       }
     }
 #pragma unroll
-    for (int i = 0; i < kV; ++i)
+    for (int i = 0; i < kV; ++i) {
+      const int dup = window<kT, kV>(t, i, (int)a.cols).dup;
+      float p = 0.f;
 #pragma unroll
-      for (int e = 0; e < 8; ++e) ss += h[i][e] * h[i][e];
+      for (int e = 0; e < 8; ++e) p += h[i][e] * h[i][e];
+      if (dup > 0) {
+        p = 0.f;
+#pragma unroll
+        for (int e = 0; e < 8; ++e) p += e >= dup ? h[i][e] * h[i][e] : 0.f;
+      }
+      ss += p;
+    }
     const float rstd = rstd_of(row_sum<kT>(ss, lds), a.cols, a.eps);
     Quant k{};
     if (a.q) {
@@ -170,11 +199,11 @@ __global__ __launch_bounds__(256) void rms_norm_kernel(NormArgs a) {
     }
 #pragma unroll
     for (int i = 0; i < kV; ++i) {
-      const int col = (t + i * kT) * 8, valid = (int)a.cols - col;
-      if (valid <= 0) continue;
+      const Window v = window<kT, kV>(t, i, (int)a.cols);
+      if (!v.in) continue;
       float f[8];
       unpack8<ELEM>(w[i], f);
-      finish8<ELEM>(a, row, col, valid, h[i], f, rstd, k);
+      finish8<ELEM>(a, row, v.col, 8, h[i], f, rstd, k);
     }
   }
 }
@@ -223,9 +252,13 @@ __global__ __launch_bounds__(1024) void rms_norm_long_kernel(NormArgs a) {
 // a row) and sums its rows' part of dw in registers; the parts, one per
 // workgroup, are added in their order by norm_dw_kernel.
 template <int ELEM, int kT, int kV>
-__global__ __launch_bounds__(256) void rms_norm_grad_kernel(NormGradArgs a) {
-  constexpr int ES = elem_bytes<ELEM>, kRows = 256 / kT;
-  __shared__ float lds[kT == 64 ? 4 * kV * 512 : 8];
+__global__ __launch_bounds__(kT < 256 ? 256 : kT) void rms_norm_grad_kernel(NormGradArgs a) {
+  constexpr int ES = elem_bytes<ELEM>, kRows = kT < 256 ? 256 / kT : 1;
+  // The next row's loads are in flight while a row is worked on, as far as two
+  // workgroups' registers allow (bf16, us without / with: 8192 x 8192 110.5 /
+  // 104.8, 6007 x 4100 39.3 / 38.5, 60000 x 512 44.5 / 42.0).
+  constexpr bool kNext = kV <= (ELEM == TCU_ELEM_F32 ? 2 : 3);
+  __shared__ float lds[kT == 64 ? 4 * kV * 512 : 16];
   const int t = threadIdx.x % kT;
   const unsigned char *dyp = (const unsigned char *)a.dy, *hp = (const unsigned char *)a.h;
   const unsigned char *dhp = (const unsigned char *)a.dh, *wp = (const unsigned char *)a.w;
@@ -233,45 +266,68 @@ __global__ __launch_bounds__(256) void rms_norm_grad_kernel(NormGradArgs a) {
   float dw[kV][8];
 #pragma unroll
   for (int i = 0; i < kV; ++i) {
-    const int col = (t + i * kT) * 8, valid = (int)a.cols - col;
-    w[i] = valid > 0 ? load8<ELEM>(wp + (int64_t)col * ES, valid) : Raw8<ELEM>{};
+    const Window v = window<kT, kV>(t, i, (int)a.cols);
+    w[i] = v.in ? load8<ELEM>(wp + (int64_t)v.col * ES, 8) : Raw8<ELEM>{};
 #pragma unroll
     for (int e = 0; e < 8; ++e) dw[i][e] = 0.f;
   }
-  const int64_t step = (int64_t)gridDim.x * kRows;
-  for (int64_t row = (int64_t)blockIdx.x * kRows + threadIdx.x / kT; row < a.rows; row += step) {
+  struct Row {
     Raw8<ELEM> dy[kV], h[kV], dh[kV];
+  };
+  auto load = [&](int64_t row, Row &v) __attribute__((always_inline)) {
 #pragma unroll
     for (int i = 0; i < kV; ++i) {
-      const int col = (t + i * kT) * 8, valid = (int)a.cols - col;
-      dy[i] = h[i] = dh[i] = Raw8<ELEM>{};
-      if (valid > 0) {
-        dy[i] = load8<ELEM>(dyp + (row * a.lddy + col) * ES, valid);
-        h[i] = load8<ELEM>(hp + (row * a.ldh + col) * ES, valid);
-        if (dhp) dh[i] = load8<ELEM>(dhp + (row * a.lddh + col) * ES, valid);
+      const Window n = window<kT, kV>(t, i, (int)a.cols);
+      v.dy[i] = v.h[i] = v.dh[i] = Raw8<ELEM>{};
+      if (n.in && row < a.rows) {
+        v.dy[i] = load8<ELEM>(dyp + (row * a.lddy + n.col) * ES, 8);
+        v.h[i] = load8<ELEM>(hp + (row * a.ldh + n.col) * ES, 8);
+        if (dhp) v.dh[i] = load8<ELEM>(dhp + (row * a.lddh + n.col) * ES, 8);
       }
     }
+  };
+  const int64_t step = (int64_t)gridDim.x * kRows;
+  int64_t row = (int64_t)blockIdx.x * kRows + threadIdx.x / kT;
+  Row next;
+  if constexpr (kNext) load(row, next);
+  for (; row < a.rows; row += step) {
+    if constexpr (!kNext) load(row, next);
+    const Row v = next;
+    const Raw8<ELEM>(&dy)[kV] = v.dy, (&h)[kV] = v.h, (&dh)[kV] = v.dh;
+    if constexpr (kNext) load(row + step, next);
     float ss = 0.f, gh = 0.f;
 #pragma unroll
     for (int i = 0; i < kV; ++i) {
+      const int dup = window<kT, kV>(t, i, (int)a.cols).dup;
       float d[8], x[8], f[8];
       unpack8<ELEM>(dy[i], d);
       unpack8<ELEM>(h[i], x);
       unpack8<ELEM>(w[i], f);
+      float p = 0.f, g = 0.f;
 #pragma unroll
       for (int e = 0; e < 8; ++e) {
-        ss += x[e] * x[e];
-        gh += d[e] * f[e] * x[e];
+        p += x[e] * x[e];
+        g += d[e] * f[e] * x[e];
       }
+      if (dup > 0) {
+        p = g = 0.f;
+#pragma unroll
+        for (int e = 0; e < 8; ++e) {
+          p += e >= dup ? x[e] * x[e] : 0.f;
+          g += e >= dup ? d[e] * f[e] * x[e] : 0.f;
+        }
+      }
+      ss += p;
+      gh += g;
     }
     ss = row_sum<kT>(ss, lds);
-    gh = row_sum<kT>(gh, lds + (kT > 64 ? 4 : 0));
+    gh = row_sum<kT>(gh, lds + (kT > 64 ? 8 : 0));
     const float rstd = rstd_of(ss, a.cols, a.eps);
     const float c = rstd * rstd * (gh / (float)a.cols);
 #pragma unroll
     for (int i = 0; i < kV; ++i) {
-      const int col = (t + i * kT) * 8, valid = (int)a.cols - col;
-      if (valid <= 0) continue;
+      const Window n = window<kT, kV>(t, i, (int)a.cols);
+      if (!n.in) continue;
       float d[8], x[8], f[8], r[8];
       unpack8<ELEM>(dy[i], d);
       unpack8<ELEM>(h[i], x);
@@ -282,17 +338,19 @@ __global__ __launch_bounds__(256) void rms_norm_grad_kernel(NormGradArgs a) {
         dw[i][e] += d[e] * (x[e] * rstd);
         r[e] += rstd * (d[e] * f[e] - x[e] * c);
       }
-      store8<ELEM>((unsigned char *)a.dx + (row * a.lddx + col) * ES, r, valid);
+      store8<ELEM>((unsigned char *)a.dx + (row * a.lddx + n.col) * ES, r, 8);
     }
   }
   float *part = a.work + (int64_t)blockIdx.x * a.cols;
   if constexpr (kT == 64) {
     // the four waves' sums, in their order
 #pragma unroll
-    for (int i = 0; i < kV; ++i)
+    for (int i = 0; i < kV; ++i) {
+      const Window n = window<kT, kV>(t, i, (int)a.cols);
 #pragma unroll
       for (int e = 0; e < 8; ++e)
-        lds[((threadIdx.x >> 6) * kV + i) * 512 + t * 8 + e] = dw[i][e];
+        if (n.in) lds[(threadIdx.x >> 6) * kV * 512 + n.col + e] = dw[i][e];
+    }
     __syncthreads();
     for (int col = threadIdx.x; col < a.cols; col += 256) {
       float v = 0.f;
@@ -303,8 +361,8 @@ __global__ __launch_bounds__(256) void rms_norm_grad_kernel(NormGradArgs a) {
   } else {
 #pragma unroll
     for (int i = 0; i < kV; ++i) {
-      const int col = (t + i * kT) * 8, valid = (int)a.cols - col;
-      if (valid > 0) store8<TCU_ELEM_F32>((unsigned char *)(part + col), dw[i], valid);
+      const Window n = window<kT, kV>(t, i, (int)a.cols);
+      if (n.in) store8<TCU_ELEM_F32>((unsigned char *)(part + n.col), dw[i], 8);
     }
   }
 }
@@ -391,19 +449,13 @@ int vectors(int64_t cols, int threads) {
   return (int)((cols + 8 * threads - 1) / (8 * threads));
 }
 
-// f(integral_constant) with the smallest number of vectors per lane.
-template <typename F>
+// f(integral_constant) with the smallest number of vectors per lane, up to kMost.
+template <int kMost, typename F>
 void with_vectors(int v, F f) {
-  switch (v) {
-    case 1: f(std::integral_constant<int, 1>{}); break;
-    case 2: f(std::integral_constant<int, 2>{}); break;
-    case 3: f(std::integral_constant<int, 3>{}); break;
-    case 4: f(std::integral_constant<int, 4>{}); break;
-    case 5: f(std::integral_constant<int, 5>{}); break;
-    case 6: f(std::integral_constant<int, 6>{}); break;
-    case 7: f(std::integral_constant<int, 7>{}); break;
-    default: f(std::integral_constant<int, 8>{}); break;
+  if constexpr (kMost > 1) {
+    if (v < kMost) return with_vectors<kMost - 1>(v, f);
   }
+  f(std::integral_constant<int, kMost>{});
 }
 
 // Workgroups of a grid over `n` pieces of work: a launch counts its work items
@@ -412,20 +464,27 @@ unsigned grid_for(int64_t n) { return (unsigned)(n < (1 << 20) ? n : 1 << 20); }
 
 template <int ELEM>
 hipError_t norm_go(const NormArgs &a, hipStream_t stream) {
-  if (a.cols <= kWaveCols) {
+  if (a.cols < 8 || a.cols > kBlockCols) {
+    hipLaunchKernelGGL(rms_norm_long_kernel<ELEM>, dim3(grid_for(a.rows)), dim3(1024), 0, stream,
+                       a);
+  } else if (a.cols <= kWaveCols) {
     const dim3 grid(grid_for((a.rows + 3) / 4));
     if (vectors(a.cols, 64) == 1)
       hipLaunchKernelGGL((rms_norm_kernel<ELEM, 64, 1>), grid, dim3(256), 0, stream, a);
     else
       hipLaunchKernelGGL((rms_norm_kernel<ELEM, 64, 2>), grid, dim3(256), 0, stream, a);
-  } else if (a.cols <= kBlockCols) {
-    with_vectors(vectors(a.cols, 256), [&](auto v) {
+  } else if (a.rows <= kFewNormRows && a.cols > 2048) {
+    if (vectors(a.cols, 1024) == 1)
+      hipLaunchKernelGGL((rms_norm_kernel<ELEM, 1024, 1>), dim3(grid_for(a.rows)), dim3(1024), 0,
+                         stream, a);
+    else
+      hipLaunchKernelGGL((rms_norm_kernel<ELEM, 1024, 2>), dim3(grid_for(a.rows)), dim3(1024), 0,
+                         stream, a);
+  } else {
+    with_vectors<8>(vectors(a.cols, 256), [&](auto v) {
       hipLaunchKernelGGL((rms_norm_kernel<ELEM, 256, decltype(v)::value>), dim3(grid_for(a.rows)),
                          dim3(256), 0, stream, a);
     });
-  } else {
-    hipLaunchKernelGGL(rms_norm_long_kernel<ELEM>, dim3(grid_for(a.rows)), dim3(1024), 0, stream,
-                       a);
   }
   return hipGetLastError();
 }
@@ -434,7 +493,9 @@ template <int ELEM>
 hipError_t grad_go(const NormGradArgs &a, hipStream_t stream) {
   int parts = (int)(a.rows < kNormParts ? a.rows : kNormParts);
   if (a.rows > 0) {
-    if (a.cols <= kWaveCols) {
+    if (a.cols < 8 || a.cols > kBlockCols) {
+      hipLaunchKernelGGL(rms_norm_grad_long_kernel<ELEM>, dim3(parts), dim3(1024), 0, stream, a);
+    } else if (a.cols <= kWaveCols) {
       if (parts > (a.rows + 3) / 4) parts = (int)((a.rows + 3) / 4);
       if (vectors(a.cols, 64) == 1)
         hipLaunchKernelGGL((rms_norm_grad_kernel<ELEM, 64, 1>), dim3(parts), dim3(256), 0, stream,
@@ -442,13 +503,16 @@ hipError_t grad_go(const NormGradArgs &a, hipStream_t stream) {
       else
         hipLaunchKernelGGL((rms_norm_grad_kernel<ELEM, 64, 2>), dim3(parts), dim3(256), 0, stream,
                            a);
-    } else if (a.cols <= kBlockCols) {
-      with_vectors(vectors(a.cols, 256), [&](auto v) {
+    } else if (vectors(a.cols, 256) <= (ELEM == TCU_ELEM_F32 ? 2 : 3)) {
+      with_vectors<3>(vectors(a.cols, 256), [&](auto v) {
         hipLaunchKernelGGL((rms_norm_grad_kernel<ELEM, 256, decltype(v)::value>), dim3(parts),
                            dim3(256), 0, stream, a);
       });
     } else {
-      hipLaunchKernelGGL(rms_norm_grad_long_kernel<ELEM>, dim3(parts), dim3(1024), 0, stream, a);
+      with_vectors<4>(vectors(a.cols, 512), [&](auto v) {
+        hipLaunchKernelGGL((rms_norm_grad_kernel<ELEM, 512, decltype(v)::value>), dim3(parts),
+                           dim3(512), 0, stream, a);
+      });
     }
     const hipError_t e = hipGetLastError();
     if (e != hipSuccess) return e;
