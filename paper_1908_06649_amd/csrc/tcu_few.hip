@@ -3,9 +3,9 @@
 //
 // few_kernel forms the product's partial sums and T = alpha X A^T in one launch,
 // join_kernel adds the partial sums and T B^T and rounds.
-//   * A workgroup's 16 or 8 waves share a strip of W's columns (64 of 16 bits, 128 of
-//     8) over one of `splits` ranges of the contracted index, about one workgroup
-//     per CU in all; the waves take the steps of 64 bytes of it in turn, for all
+//   * A workgroup's 8 waves share a strip of W's columns (64 of 16 bits, 128 of
+//     8) over one of `splits` ranges of the contracted index, one or two
+//     workgroups per CU in all; the waves take the steps of 64 bytes of it in turn, for all
 //     rows.  A lane loads 8 bytes of each of a step's 8 (16) rows of W that it
 //     holds, 16 lanes a whole row of the strip, and exchanges bytes in its own
 //     registers to the runs along the contracted index that the matrix cores
@@ -21,11 +21,7 @@
 namespace tcu {
 namespace {
 
-// A workgroup's waves: 16 where a wave's sums and two steps of W fit 128
-// registers (16-bit W, up to 32 rows), else 8.
-__host__ __device__ constexpr int few_waves(int es, int row_blocks) {
-  return es == 2 && row_blocks <= 2 ? 16 : 8;
-}
+constexpr int kWaves = 8;   // of a workgroup
 
 // How a step of W lies: ES bytes per element, kRun elements of the contracted
 // index per lane, kCols columns per lane (8 bytes).
@@ -118,8 +114,8 @@ __device__ __forceinline__ void narrow_value(const FewArgs &a, int i) {
 
 // DT: the product's types; ELEM: the adapters'; kMB: blocks of 16 rows.
 template <int DT, int ELEM, int kMB>
-__global__ __launch_bounds__(64 * few_waves(in_bytes(DT), kMB)) void few_kernel(FewArgs a) {
-  constexpr int ES = in_bytes(DT), kWaves = few_waves(ES, kMB);
+__global__ __launch_bounds__(64 * kWaves) void few_kernel(FewArgs a) {
+  constexpr int ES = in_bytes(DT);
   // 8-bit W and more than 32 rows: a second step's registers are not there
   constexpr bool kAhead = ES == 2 || kMB <= 2;
   constexpr bool kI8 = ES == 1;
@@ -185,7 +181,7 @@ __global__ __launch_bounds__(64 * few_waves(in_bytes(DT), kMB)) void few_kernel(
   // in turn over all waves of the grid.
   auto narrow = [&]() {
     const int all = a.G > 0 ? a.M * a.r : 0;
-    for (int i = blockIdx.x * kWaves + w; i < all; i += gridDim.x * kWaves)
+    for (int i = blockIdx.x + w * gridDim.x; i < all; i += gridDim.x * kWaves)
       narrow_value<ELEM>(a, i);
   };
   int s = s_begin + w;
@@ -193,13 +189,14 @@ __global__ __launch_bounds__(64 * few_waves(in_bytes(DT), kMB)) void few_kernel(
     u32x2 w0[S::kRun], w1[S::kRun];
     u32x4 x0[kMB], x1[kMB];
     if (s < s_end) load(s, w0, x0);
+    if (s + kWaves < s_end) load(s + kWaves, w1, x1);
     narrow();
-    for (; s < s_end; s += 2 * kWaves) {
-      if (s + kWaves < s_end) load(s + kWaves, w1, x1);
+    while (s < s_end) {
       multiply(w0, x0);
-      if (s + kWaves >= s_end) break;
       if (s + 2 * kWaves < s_end) load(s + 2 * kWaves, w0, x0);
-      multiply(w1, x1);
+      if (s + kWaves < s_end) multiply(w1, x1);
+      if (s + 3 * kWaves < s_end) load(s + 3 * kWaves, w1, x1);
+      s += 2 * kWaves;
     }
   } else {
     u32x2 w0[S::kRun];
@@ -282,12 +279,16 @@ int row_blocks(int64_t M) { return M <= 16 ? 1 : (int)((M + 15) / 16); }
 
 int strip_cols(bool q8) { return q8 ? Step<1>::kStrip : Step<2>::kStrip; }
 
-// Ranges of the contracted index: about one workgroup per compute unit, and a
-// step at least for every wave.
+// Ranges of the contracted index: about two workgroups per compute unit where
+// two fit its registers (16-bit W, up to 32 rows), else one, and a step at least
+// for every wave.  Us of a call, bf16, 256 / 512 workgroups: 8 x 4096 x 4096 17.0
+// / 15.5, 8 x 8192 x 8192 31.9 / 29.2, 48 x 4096 x 4096 18.6 / 22.5 (the ranges'
+// sums); int8 32 x 8192 x 8192 25.7 / 29.4.
 int few_splits(int64_t M, int64_t K, int64_t N, bool q8) {
   const int64_t strips = N > 0 ? (N + strip_cols(q8) - 1) / strip_cols(q8) : 1;
-  const int64_t wave_elems = (int64_t)(q8 ? 64 : 32) * few_waves(q8 ? 1 : 2, row_blocks(M));
-  int64_t n = (256 + strips / 2) / strips;
+  const int64_t wave_elems = (int64_t)(q8 ? 64 : 32) * kWaves;
+  const int64_t want = !q8 && M <= 32 ? 512 : 256;
+  int64_t n = (want + strips / 2) / strips;
   const int64_t most = (K + wave_elems - 1) / wave_elems;
   if (n > most) n = most;
   return (int)(n < 1 ? 1 : n > 16 ? 16 : n);
@@ -323,7 +324,7 @@ hipError_t few(const AdapterArgs &a, hipStream_t stream) {
   auto go = [&](auto blocks) {
     constexpr int kMB = decltype(blocks)::value;
     hipLaunchKernelGGL((few_kernel<DT, ELEM, kMB>), grid,
-                       dim3(64 * few_waves(kQ8 ? 1 : 2, kMB)), 0, stream, f);
+                       dim3(64 * kWaves), 0, stream, f);
   };
   switch (row_blocks(a.M)) {
     case 1: go(std::integral_constant<int, 1>{}); break;
