@@ -20,242 +20,319 @@ constexpr int64_t round256(int64_t n) { return (n + 255) / 256 * 256; }
 __host__ __device__ constexpr int64_t rank_pad(int64_t r) { return r <= 16 ? 16 : (r + 31) / 32 * 32; }
 
 // ---------------------------------------------------------------------------
-// The rows in the order of their adapters, the rows of one in their own order:
-// order[start[g] .. start[g + 1]) are g's, start[G] the rows that have one.
-// Workgroup g counts the rows of smaller numbers, then places its own; every
-// lane a run of consecutive rows, so the order is fixed.
-// ---------------------------------------------------------------------------
-constexpr int kGroupThreads = 1024, kGroupHeld = 8;
-__global__ __launch_bounds__(kGroupThreads) void group_kernel(const int *__restrict__ ids,
-                                                              int *__restrict__ start,
-                                                              int *__restrict__ order, int M,
-                                                              int G) {
-  constexpr int kWaves = kGroupThreads / 64;
-  __shared__ int below_of[kWaves], own_of[kWaves];
-  const int lane = threadIdx.x & 63, w = threadIdx.x >> 6, g = blockIdx.x;
-  const int per = (M + kGroupThreads - 1) / kGroupThreads;
-  const int64_t first = (int64_t)threadIdx.x * per;
-  const int mine = first < M ? (M - first < per ? (int)(M - first) : per) : 0;
-  // up to kGroupHeld numbers a lane stay in registers between the two passes
-  int held[kGroupHeld];
-  int below = 0, own = 0;
-  if (per <= kGroupHeld && M > 0) {
-#pragma unroll
-    for (int i = 0; i < kGroupHeld; ++i) {
-      const int id = ids[first + i < M ? first + i : M - 1];
-      held[i] = i < mine ? id : -1;
-    }
-#pragma unroll
-    for (int i = 0; i < kGroupHeld; ++i) {
-      below += held[i] >= 0 && held[i] < g;
-      own += held[i] == g;
-    }
-  } else {
-    for (int i = 0; i < mine; ++i) {
-      const int id = ids[first + i];
-      below += id >= 0 && id < g;
-      own += id == g;
-    }
-  }
-  // sums over the lanes before this one and over all
-  int upto = own;
-#pragma unroll
-  for (int s = 1; s < 64; s <<= 1) {
-    const int o = __shfl_up(upto, s);
-    upto += lane >= s ? o : 0;
-    below += __shfl_xor(below, s);
-  }
-  if (lane == 63) own_of[w] = upto;
-  if (lane == 0) below_of[w] = below;
-  __syncthreads();
-  int base = 0, total = 0, before = upto - own;
-#pragma unroll
-  for (int i = 0; i < kWaves; ++i) {
-    base += below_of[i];
-    total += own_of[i];
-    before += i < w ? own_of[i] : 0;
-  }
-  if (threadIdx.x == 0) start[g] = base;
-  if (g == G - 1 && threadIdx.x == 0) start[G] = base + total;
-  if (own == 0) return;
-  int at = base + before;
-  if (per <= kGroupHeld) {
-#pragma unroll
-    for (int i = 0; i < kGroupHeld; ++i)
-      if (held[i] == g) order[at++] = (int)first + i;
-  } else {
-    for (int i = 0; i < mine; ++i)
-      if (ids[first + i] == g) order[at++] = (int)first + i;
-  }
-}
-
-// ---------------------------------------------------------------------------
 // T[m][j] = alpha[g] sum_k X[m][k] F_g[j][k] (F_g: r x K, rows contiguous), zeros
-// from rank r on to rank_pad.  A workgroup takes 16 kRows rows (of `order` if
-// given, else as they lie) and all ranks; its 16 waves take every sixteenth 64
+// from rank r on to rank_pad.  A workgroup takes up to 16 rows of one
+// adapter, wherever they lie, and all ranks; its 8 waves take every eighth 64
 // elements of K, and their sums are added in their order.  A load instruction
 // fetches 8 whole lines of 128 bytes (X from memory once, F from the caches); a
 // wave turns them into the matrix cores' operands through its own part of LDS,
-// 16-byte chunks XOR-swizzled by the row, without barriers.  Rows of several
-// adapters are multiplied by each of them, a row keeping its own adapter's
-// result.
+// 16-byte chunks XOR-swizzled by the row, without barriers.
+//
+// Which rows a workgroup takes it finds out by itself (kFromIds: up to kScanRows
+// rows and kScanAdapters adapters): it counts every adapter's rows, and with
+// them the pieces of 16 rows before its own, then places its adapter's
+// rows.  Larger calls, and those that need the order elsewhere, read it off
+// group_kernel's.  (A launch of group_kernel takes 5 to 9 us of a call; taking
+// rows as they lie, a product for each adapter of a block, 60 us for 128 rows of
+// 16 adapters in turn.)
 // ---------------------------------------------------------------------------
+constexpr int kNarrowThreads = 512, kScanHeld = 16, kPiece = 16;
+constexpr int64_t kScanRows = kNarrowThreads * kScanHeld, kScanAdapters = kNarrowThreads;
+
 struct Narrow {
   const unsigned char *X, *F;
   float *T;
   int64_t ldx;
   int K;
 };
-template <int ELEM, int kRows, int kBlocks>
-__global__ __launch_bounds__(1024) void narrow_kernel(Narrow n0, Narrow n1,
+
+// Inclusive sum over a workgroup's lanes in their order; part: a word of LDS per wave.
+template <int kThreads>
+__device__ __forceinline__ int block_scan(int v, int *part) {
+  const int lane = threadIdx.x & 63, w = threadIdx.x >> 6;
+#pragma unroll
+  for (int s = 1; s < 64; s <<= 1) {
+    const int o = __shfl_up(v, s);
+    v += lane >= s ? o : 0;
+  }
+  __syncthreads();   // earlier reads of part
+  if (lane == 63) part[w] = v;
+  __syncthreads();
+#pragma unroll
+  for (int i = 0; i < kThreads / 64; ++i) v += i < w ? part[i] : 0;
+  return v;
+}
+
+// Rows t, t + kThreads, .. of a tile of kThreads kHeld rows that begins at row m0:
+// their adapters' numbers, -1 without one.
+template <int kThreads, int kHeld>
+__device__ __forceinline__ void load_ids(const int *__restrict__ ids, int m0, int M, int G,
+                                         int (&held)[kHeld]) {
+#pragma unroll
+  for (int i = 0; i < kHeld; ++i) {
+    const int m = m0 + kThreads * i + (int)threadIdx.x;
+    const int id = ids[m < M ? m : M - 1];
+    held[i] = m < M && id >= 0 && id < G ? id : -1;
+  }
+}
+
+// f(place, row) for every row of the tile that names g, its place among them in
+// the order of the rows; returns how many there are.  tab: LDS, a word for each
+// wave and held row, and one more.
+template <int kThreads, int kHeld, typename F>
+__device__ __forceinline__ int place_rows(const int (&held)[kHeld], int g, int m0, int *tab, F f) {
+  constexpr int kWaves = kThreads / 64, kWords = kWaves * kHeld;
+  static_assert(kWords == 128, "two words a lane");
+  const int lane = threadIdx.x & 63, w = threadIdx.x >> 6;
+  __syncthreads();   // earlier reads of tab
+#pragma unroll
+  for (int i = 0; i < kHeld; ++i) {
+    const int n = __popcll(__ballot(held[i] == g));
+    if (lane == 0) tab[i * kWaves + w] = n;
+  }
+  __syncthreads();
+  if (w == 0) {
+    const int a = tab[2 * lane], b = tab[2 * lane + 1];
+    int v = a + b;
+#pragma unroll
+    for (int s = 1; s < 64; s <<= 1) {
+      const int o = __shfl_up(v, s);
+      v += lane >= s ? o : 0;
+    }
+    tab[2 * lane] = v - a - b;
+    tab[2 * lane + 1] = v - b;
+    if (lane == 63) tab[kWords] = v;
+  }
+  __syncthreads();
+#pragma unroll
+  for (int i = 0; i < kHeld; ++i) {
+    const unsigned long long votes = __ballot(held[i] == g);
+    if (held[i] == g)
+      f(tab[i * kWaves + w] + __popcll(votes & ((1ull << lane) - 1)),
+        m0 + kThreads * i + (int)threadIdx.x);
+  }
+  return tab[kWords];
+}
+
+// The adapter of piece `piece` and the rows of it (up to kPiece of them, to
+// rows[]); returns how many there are, 0 if there is no such piece.
+struct Piece {
+  int bins[kScanAdapters], part[8], tab[129], rows[kPiece], g, chunk, n;
+};
+template <bool kFromIds>
+__device__ __forceinline__ int find_piece(Piece &s, const int *__restrict__ ids,
+                                          const int *__restrict__ order,
+                                          const int *__restrict__ start, int M, int G, int piece) {
+  const int t = threadIdx.x;
+  int held[kScanHeld];
+  if (t == 0) s.n = 0;
+  if constexpr (kFromIds) {
+    load_ids<kNarrowThreads>(ids, 0, M, G, held);
+    s.bins[t] = 0;
+    __syncthreads();
+    // (sums of counts: any order gives the same).  A wave whose rows all name one
+    // adapter adds them at once: one by one its lanes would queue at one address.
+#pragma unroll
+    for (int i = 0; i < kScanHeld; ++i) {
+      if (kNarrowThreads * i >= M) break;
+      const int lead = __builtin_amdgcn_readfirstlane(held[i]);
+      if (__all(held[i] == lead)) {
+        if ((t & 63) == 0 && lead >= 0) atomicAdd(&s.bins[lead], 64);
+      } else if (held[i] >= 0) {
+        atomicAdd(&s.bins[held[i]], 1);
+      }
+    }
+    __syncthreads();
+    const int n = s.bins[t], pieces = (n + kPiece - 1) / kPiece;
+    const int before = block_scan<kNarrowThreads>(pieces, s.part) - pieces;
+    if (piece >= before && piece < before + pieces) {
+      s.g = t;
+      s.chunk = piece - before;
+      s.n = min(n - s.chunk * kPiece, kPiece);
+    }
+  } else {
+    int base = 0;
+    for (int g0 = 0; g0 < G && base <= piece; g0 += kNarrowThreads) {
+      const int g = g0 + t, n = g < G ? start[g + 1] - start[g] : 0;
+      const int pieces = (n + kPiece - 1) / kPiece;
+      const int upto = block_scan<kNarrowThreads>(pieces, s.part), before = base + upto - pieces;
+      if (piece >= before && piece < before + pieces) {
+        s.g = g;
+        s.chunk = piece - before;
+        s.n = min(n - s.chunk * kPiece, kPiece);
+      }
+      __syncthreads();   // s.part has been read
+      if (t == kNarrowThreads - 1) s.part[0] = upto;
+      __syncthreads();
+      base += s.part[0];
+    }
+  }
+  __syncthreads();
+  const int n = s.n;
+  if (n == 0) return 0;
+  const int from = s.chunk * kPiece;
+  if constexpr (kFromIds) {
+    place_rows<kNarrowThreads>(held, s.g, 0, s.tab, [&](int at, int m) {
+      if (at >= from && at < from + n) s.rows[at - from] = m;
+    });
+  } else {
+    if (t < n) s.rows[t] = order[start[s.g] + from + t];
+  }
+  __syncthreads();
+  return n;
+}
+
+// Two workgroups a compute unit: the few pieces past a whole round that short last
+// pieces make would cost a second one.
+template <int ELEM, int kBlocks, bool kFromIds>
+__global__ __launch_bounds__(kNarrowThreads, 4) void narrow_kernel(Narrow n0, Narrow n1,
                                                       const float *__restrict__ alpha,
                                                       const int *__restrict__ ids,
                                                       const int *__restrict__ order,
                                                       const int *__restrict__ start, int M, int r,
                                                       int rp, int G) {
   constexpr int DT = ELEM == TCU_ELEM_F16 ? TCU_F16_F32 : TCU_BF16_F32;
-  constexpr int kWaves = 16, kStep = 64, kPart = (kRows + kBlocks) * 2048;
-  static_assert(kRows * kBlocks * 1024 <= kPart, "a wave's sums");
+  constexpr int kWaves = kNarrowThreads / 64, kStep = 64, kPart = (1 + kBlocks) * 2048;
+  static_assert(kBlocks * 1024 <= kPart, "a wave's sums");
+  static_assert(sizeof(Piece) <= kWaves * kPart, "the search");
   __shared__ __attribute__((aligned(128))) unsigned char lds[kWaves * kPart];
   const Narrow n = blockIdx.y == 0 ? n0 : n1;
   const int lane = threadIdx.x & 63, w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int c = lane & 15, q = lane >> 4;
   const int lr = lane >> 3, lc = lane & 7;      // a load's row and chunk
-  const int count = order ? start[G] : M;
-  const int first = blockIdx.x * (16 * kRows);
-  if (first >= count) return;
-  int row[kRows], id[kRows];
-  unsigned left = 0u;
+  Piece &found = *(Piece *)lds;
+  const int count = find_piece<kFromIds>(found, ids, order, start, M, G, blockIdx.x);
+  if (count == 0) return;
+  const int g = __builtin_amdgcn_readfirstlane(found.g);
+  const int row = found.rows[c < count ? c : count - 1];
+  __syncthreads();   // the search's LDS is free
+  const unsigned char *x[2];
 #pragma unroll
-  for (int i = 0; i < kRows; ++i) {
-    const int at = first + 16 * i + c;
-    row[i] = order ? order[at < count ? at : count - 1] : (at < count ? at : count - 1);
-    id[i] = at < count ? ids[row[i]] : -1;
-    if (id[i] >= G || id[i] < 0) id[i] = -1;
-    left |= (unsigned)(__ballot(id[i] >= 0) & 0xffffu) << (16 * i);
-  }
-  const unsigned char *x[kRows][2];
-#pragma unroll
-  for (int i = 0; i < kRows; ++i)
-#pragma unroll
-    for (int h = 0; h < 2; ++h)
-      x[i][h] = n.X + 2 * ((int64_t)__shfl(row[i], 8 * h + lr) * n.ldx + 8 * lc);
+  for (int h = 0; h < 2; ++h)
+    x[h] = n.X + 2 * ((int64_t)__shfl(row, 8 * h + lr) * n.ldx + 8 * lc);
   unsigned char *const mine_lds = lds + w * kPart;
   unsigned char *const put = mine_lds + lr * 128 + 16 * (lc ^ lr);
   const unsigned char *get[2];
 #pragma unroll
   for (int h = 0; h < 2; ++h) get[h] = mine_lds + c * 128 + 16 * ((4 * h + q) ^ (c & 7));
-  while (left != 0u) {
-    // the adapter of the first row left, and its rows
-    const int lead = __builtin_ctz(left);
-    int g = 0;
-    unsigned mine = 0u;
+  const unsigned char *fg = n.F + 2 * ((int64_t)g * r * n.K + 8 * lc);
+  const float al = alpha[g];
+  for (int j0 = 0; j0 < rp; j0 += 16 * kBlocks) {
+    const unsigned char *f[kBlocks][2];
+    f32x4 acc[kBlocks];
 #pragma unroll
-    for (int i = 0; i < kRows; ++i)
-      if (lead >> 4 == i) g = __builtin_amdgcn_readlane(id[i], lead & 15);
+    for (int b = 0; b < kBlocks; ++b) {
 #pragma unroll
-    for (int i = 0; i < kRows; ++i)
-      mine |= (unsigned)(__ballot(id[i] == g) & 0xffffu) << (16 * i);
-    left &= ~mine;
-    const unsigned char *fg = n.F + 2 * ((int64_t)g * r * n.K + 8 * lc);
-    const float al = alpha[g];
-    for (int j0 = 0; j0 < rp; j0 += 16 * kBlocks) {
-      const unsigned char *f[kBlocks][2];
-      f32x4 acc[kRows][kBlocks];
-#pragma unroll
-      for (int b = 0; b < kBlocks; ++b) {
-#pragma unroll
-        for (int h = 0; h < 2; ++h) {
-          const int j = j0 + 16 * b + 8 * h + lr;
-          f[b][h] = fg + 2 * (int64_t)(j < r ? j : r - 1) * n.K;
-        }
-#pragma unroll
-        for (int i = 0; i < kRows; ++i) acc[i][b] = f32x4{0.f, 0.f, 0.f, 0.f};
+      for (int h = 0; h < 2; ++h) {
+        const int j = j0 + 16 * b + 8 * h + lr;
+        f[b][h] = fg + 2 * (int64_t)(j < r ? j : r - 1) * n.K;
       }
-      struct Chunk {
-        u32x4 x[kRows][2], f[kBlocks][2];
-      };
-      auto load = [&](int k, Chunk &v) __attribute__((always_inline)) {
-        if (k + kStep <= n.K) {
-#pragma unroll
-          for (int h = 0; h < 2; ++h) {
-#pragma unroll
-            for (int i = 0; i < kRows; ++i) v.x[i][h] = load16_any(x[i][h] + 2 * k);
-#pragma unroll
-            for (int b = 0; b < kBlocks; ++b) v.f[b][h] = load16_any(f[b][h] + 2 * k);
-          }
-        } else {
-          // zeros past K
-          const int valid = n.K - k - 8 * lc;
-#pragma unroll
-          for (int h = 0; h < 2; ++h) {
-#pragma unroll
-            for (int i = 0; i < kRows; ++i) v.x[i][h] = load8<ELEM>(x[i][h] + 2 * k, valid).v[0];
-#pragma unroll
-            for (int b = 0; b < kBlocks; ++b) v.f[b][h] = load8<ELEM>(f[b][h] + 2 * k, valid).v[0];
-          }
-        }
-      };
-      auto multiply = [&](const Chunk &v) __attribute__((always_inline)) {
+      acc[b] = f32x4{0.f, 0.f, 0.f, 0.f};
+    }
+    struct Chunk {
+      u32x4 x[2], f[kBlocks][2];
+    };
+    auto load = [&](int k, Chunk &v) __attribute__((always_inline)) {
+      if (k + kStep <= n.K) {
 #pragma unroll
         for (int h = 0; h < 2; ++h) {
+          v.x[h] = load16_any(x[h] + 2 * k);
 #pragma unroll
-          for (int i = 0; i < kRows; ++i) *(u32x4 *)(put + 2048 * i + 1024 * h) = v.x[i][h];
-#pragma unroll
-          for (int b = 0; b < kBlocks; ++b)
-            *(u32x4 *)(put + 2048 * (kRows + b) + 1024 * h) = v.f[b][h];
+          for (int b = 0; b < kBlocks; ++b) v.f[b][h] = load16_any(f[b][h] + 2 * k);
         }
+      } else {
+        // zeros past K
+        const int valid = n.K - k - 8 * lc;
 #pragma unroll
         for (int h = 0; h < 2; ++h) {
-          u32x4 xf[kRows], ff[kBlocks];
+          v.x[h] = load8<ELEM>(x[h] + 2 * k, valid).v[0];
 #pragma unroll
-          for (int i = 0; i < kRows; ++i) xf[i] = *(const u32x4 *)(get[h] + 2048 * i);
-#pragma unroll
-          for (int b = 0; b < kBlocks; ++b) ff[b] = *(const u32x4 *)(get[h] + 2048 * (kRows + b));
-#pragma unroll
-          for (int i = 0; i < kRows; ++i)
-#pragma unroll
-            for (int b = 0; b < kBlocks; ++b) acc[i][b] = mfma_k32(DT, ff[b], xf[i], acc[i][b]);
-        }
-      };
-      // kAhead chunks in flight
-      constexpr int kAhead = kRows * kBlocks == 1 ? 4 : 2, kNext = kWaves * kStep;
-      Chunk v[kAhead];
-      int k = w * kStep;
-#pragma unroll
-      for (int u = 0; u < kAhead; ++u)
-        if (k + u * kNext < n.K) load(k + u * kNext, v[u]);
-      while (k < n.K) {
-#pragma unroll
-        for (int u = 0; u < kAhead; ++u) {
-          if (k >= n.K) break;
-          multiply(v[u]);
-          if (k + kAhead * kNext < n.K) load(k + kAhead * kNext, v[u]);
-          k += kNext;
+          for (int b = 0; b < kBlocks; ++b) v.f[b][h] = load8<ELEM>(f[b][h] + 2 * k, valid).v[0];
         }
       }
+    };
+    auto multiply = [&](const Chunk &v) __attribute__((always_inline)) {
 #pragma unroll
-      for (int i = 0; i < kRows; ++i)
+      for (int h = 0; h < 2; ++h) {
+        *(u32x4 *)(put + 1024 * h) = v.x[h];
 #pragma unroll
         for (int b = 0; b < kBlocks; ++b)
-          *(f32x4 *)(mine_lds + (i * kBlocks + b) * 1024 + 16 * lane) = acc[i][b];
-      __syncthreads();
-      for (int s = w; s < kRows * kBlocks; s += kWaves) {
-        f32x4 v = *(const f32x4 *)(lds + s * 1024 + 16 * lane);
-#pragma unroll
-        for (int u = 1; u < kWaves; ++u) v += *(const f32x4 *)(lds + u * kPart + s * 1024 + 16 * lane);
-        // ranks j .. j + 3 of row c of the block
-        const int i = s / kBlocks, j = j0 + 16 * (s % kBlocks) + 4 * q;
-        int m = row[0];
-#pragma unroll
-        for (int u = 1; u < kRows; ++u) m = i == u ? row[u] : m;
-#pragma unroll
-        for (int e = 0; e < 4; ++e) v[e] = j + e < r ? v[e] * al : 0.f;
-        if (mine >> (16 * i + c) & 1u) *(f32x4 *)(n.T + (int64_t)m * rp + j) = v;
+          *(u32x4 *)(put + 2048 * (1 + b) + 1024 * h) = v.f[b][h];
       }
-      __syncthreads();   // read before the next sums overwrite
+#pragma unroll
+      for (int h = 0; h < 2; ++h) {
+        const u32x4 xf = *(const u32x4 *)get[h];
+#pragma unroll
+        for (int b = 0; b < kBlocks; ++b)
+          acc[b] = mfma_k32(DT, *(const u32x4 *)(get[h] + 2048 * (1 + b)), xf, acc[b]);
+      }
+    };
+    // kAhead chunks in flight
+    constexpr int kAhead = kBlocks == 1 ? 4 : 2, kNext = kWaves * kStep;
+    Chunk v[kAhead];
+    int k = w * kStep;
+#pragma unroll
+    for (int u = 0; u < kAhead; ++u)
+      if (k + u * kNext < n.K) load(k + u * kNext, v[u]);
+    while (k < n.K) {
+#pragma unroll
+      for (int u = 0; u < kAhead; ++u) {
+        if (k >= n.K) break;
+        multiply(v[u]);
+        if (k + kAhead * kNext < n.K) load(k + kAhead * kNext, v[u]);
+        k += kNext;
+      }
     }
+#pragma unroll
+    for (int b = 0; b < kBlocks; ++b) *(f32x4 *)(mine_lds + b * 1024 + 16 * lane) = acc[b];
+    __syncthreads();
+    if (w < kBlocks) {
+      f32x4 v = *(const f32x4 *)(lds + w * 1024 + 16 * lane);
+#pragma unroll
+      for (int u = 1; u < kWaves; ++u) v += *(const f32x4 *)(lds + u * kPart + w * 1024 + 16 * lane);
+      // ranks j .. j + 3 of row c
+      const int j = j0 + 16 * w + 4 * q;
+#pragma unroll
+      for (int e = 0; e < 4; ++e) v[e] = j + e < r ? v[e] * al : 0.f;
+      if (c < count) *(f32x4 *)(n.T + (int64_t)row * rp + j) = v;
+    }
+    __syncthreads();   // read before the next sums overwrite
   }
+}
+
+// ---------------------------------------------------------------------------
+// The rows in the order of their adapters, the rows of one in their own order:
+// order[start[g] .. start[g + 1]) are g's, start[G] the rows that have one.
+// Workgroup g counts the rows of smaller numbers, then places its own.
+// ---------------------------------------------------------------------------
+constexpr int kGroupThreads = 1024, kGroupHeld = 8, kGroupTile = kGroupThreads * kGroupHeld;
+__global__ __launch_bounds__(kGroupThreads) void group_kernel(const int *__restrict__ ids,
+                                                              int *__restrict__ start,
+                                                              int *__restrict__ order, int M,
+                                                              int G) {
+  __shared__ int part[kGroupThreads / 64], tab[129];
+  const int lane = threadIdx.x & 63, w = threadIdx.x >> 6, g = blockIdx.x;
+  int held[kGroupHeld];
+  int below = 0;
+  for (int64_t m0 = 0; m0 < M; m0 += kGroupTile) {
+    load_ids<kGroupThreads>(ids, (int)m0, M, G, held);
+#pragma unroll
+    for (int i = 0; i < kGroupHeld; ++i) below += held[i] >= 0 && held[i] < g;
+  }
+#pragma unroll
+  for (int s = 1; s < 64; s <<= 1) below += __shfl_xor(below, s);
+  if (lane == 0) part[w] = below;
+  __syncthreads();
+  int at = 0;
+#pragma unroll
+  for (int i = 0; i < kGroupThreads / 64; ++i) at += part[i];
+  if (threadIdx.x == 0) start[g] = at;
+  for (int64_t m0 = 0; m0 < M; m0 += kGroupTile) {
+    if (M > kGroupTile) load_ids<kGroupThreads>(ids, (int)m0, M, G, held);   // else still there
+    at += place_rows<kGroupThreads>(held, g, (int)m0, tab,
+                                    [&](int place, int m) { order[at + place] = m; });
+  }
+  if (g == G - 1 && threadIdx.x == 0) start[G] = at;
 }
 
 // ---------------------------------------------------------------------------
@@ -269,8 +346,9 @@ __global__ __launch_bounds__(1024) void narrow_kernel(Narrow n0, Narrow n1,
 // product of 32.  Every adapter's product is formed apart and added by its own
 // rows alone, so that no row sees another adapter's values (a block costs one
 // product per distinct adapter of its 16 rows; summing in place where there is
-// one made the 256 x 256 tiles spill 175 registers).  B's fragments are loaded
-// from the caches, again only where the adapter changes from block to block.
+// one made the 256 x 256 tiles spill 175 registers).  A wave goes through the
+// adapters of 32 rows at a time, the next 32 rows' T and the next adapter's
+// fragments of B on their way from the caches under the products of one.
 // ---------------------------------------------------------------------------
 template <int ELEM, int OUT, bool kQ8>
 struct AdapterTail {
@@ -357,6 +435,7 @@ struct AdapterTail {
       }
     }
     if (any == 0) return;
+    static_assert(FM % 2 == 0, "blocks in pairs");
     // binary16: 2^e brings the row's largest |T| to [2^14, 2^15)
     int ex[FM];
     if constexpr (ELEM == TCU_ELEM_F16) {
@@ -385,64 +464,95 @@ struct AdapterTail {
     }
     const bool narrow = rp == 16;
     const int steps = narrow ? 1 : rp / 32;
+    constexpr int kGroup = 2;
     for (int s = 0; s < steps; ++s) {
       const int rank = 32 * s + 8 * (narrow ? q & 1 : q);
+      auto load_b = [&](int g, u32x4 (&wf)[FN]) __attribute__((always_inline)) {
+#pragma unroll
+        for (int fn = 0; fn < FN; ++fn) {
+          const int n = col0 + 16 * fn + c;
+          // past the ranks: zeros, as T has them
+          wf[fn] = rank < rb ? *(const u32x4 *)(B + (int64_t)g * bstride +
+                                                2 * ((int64_t)(n < N ? n : N - 1) * rb + rank))
+                             : u32x4{0u, 0u, 0u, 0u};
+        }
+      };
+      auto load_t = [&](int f0, Raw8<TCU_ELEM_F32> (&t)[kGroup]) __attribute__((always_inline)) {
+#pragma unroll
+        for (int i = 0; i < kGroup; ++i) {
+          const int m = row0 + 16 * (f0 + i) + c;
+          t[i] = load8<TCU_ELEM_F32>(
+              (const unsigned char *)(T + (int64_t)(m < M ? m : M - 1) * rp + rank), 8);
+        }
+      };
       int held = -1;
       u32x4 wf[FN];
 #pragma unroll
       for (int fn = 0; fn < FN; ++fn) wf[fn] = u32x4{0u, 0u, 0u, 0u};
+      Raw8<TCU_ELEM_F32> t[kGroup];
+      load_t(0, t);
 #pragma unroll
-      for (int fm = 0; fm < FM; ++fm) {
-        unsigned left = (unsigned)(__ballot(id[fm] >= 0) & 0xffffu);
-        if (left == 0u) continue;
-        const int m = row0 + 16 * fm + c;
-        float t[8];
-        unpack8<TCU_ELEM_F32>(
-            load8<TCU_ELEM_F32>((const unsigned char *)(T + (int64_t)(m < M ? m : M - 1) * rp + rank),
-                                8),
-            t);
-        u32x4 w[kWords];
-        words(t, ELEM == TCU_ELEM_F16 ? ex[fm] : 0, w);
-        if (narrow) {
-          // lanes of the upper ranks' places take the second word, and of a
-          // third word's product nothing
-          const u32x4 none = {0u, 0u, 0u, 0u};
-          w[0] = q < 2 ? w[0] : w[1];
-          if constexpr (kWords == 3) w[1] = q < 2 ? w[2] : none;
+      for (int f0 = 0; f0 < FM; f0 += kGroup) {
+        u32x4 w[kGroup][kWords];
+#pragma unroll
+        for (int i = 0; i < kGroup; ++i) {
+          float v[8];
+          unpack8<TCU_ELEM_F32>(t[i], v);
+          words(v, ELEM == TCU_ELEM_F16 ? ex[f0 + i] : 0, w[i]);
+          if (narrow) {
+            // lanes of the upper ranks' places take the second word, and of a
+            // third word's product nothing
+            const u32x4 none = {0u, 0u, 0u, 0u};
+            w[i][0] = q < 2 ? w[i][0] : w[i][1];
+            if constexpr (kWords == 3) w[i][1] = q < 2 ? w[i][2] : none;
+          }
         }
-        while (left != 0u) {
-          const int g = __builtin_amdgcn_readlane(id[fm], __builtin_ctz(left));
-          const unsigned mine = (unsigned)(__ballot(id[fm] == g) & 0xffffu);
+        if (f0 + kGroup < FM) load_t(f0 + kGroup, t);
+        // rows whose adapter is still to come, 16 bits a block
+        unsigned left = 0u;
+#pragma unroll
+        for (int i = 0; i < kGroup; ++i)
+          left |= (unsigned)(__ballot(id[f0 + i] >= 0) & 0xffffu) << (16 * i);
+        auto lead = [&]() __attribute__((always_inline)) {
+          const int at = __builtin_ctz(left);
+          return __builtin_amdgcn_readlane(at < 16 ? id[f0] : id[f0 + 1], at & 15);
+        };
+        if (left == 0u) continue;
+        int g = lead();
+        if (g != held) load_b(g, wf);
+        while (true) {
+          unsigned mine = 0u;
+#pragma unroll
+          for (int i = 0; i < kGroup; ++i)
+            mine |= (unsigned)(__ballot(id[f0 + i] == g) & 0xffffu) << (16 * i);
           left &= ~mine;
-          if (g != held) {
-            held = g;
+          // the next adapter's B is on its way under this one's products
+          const int next = left != 0u ? lead() : g;
+          u32x4 wn[FN];
+          if (left != 0u) load_b(next, wn);
+#pragma unroll
+          for (int i = 0; i < kGroup; ++i) {
+            if ((mine >> (16 * i) & 0xffffu) == 0u) continue;
+            const bool own = id[f0 + i] == g;
 #pragma unroll
             for (int fn = 0; fn < FN; ++fn) {
-              const int n = col0 + 16 * fn + c;
-              // past the ranks: zeros, as T has them
-              wf[fn] = rank < rb ? *(const u32x4 *)(B + (int64_t)g * bstride +
-                                                    2 * ((int64_t)(n < N ? n : N - 1) * rb + rank))
-                                 : u32x4{0u, 0u, 0u, 0u};
+              f32x4 d = mfma_k32(DT, wf[fn], w[i][0], f32x4{0.f, 0.f, 0.f, 0.f});
+              if (kWords == 3 || !narrow) d = mfma_k32(DT, wf[fn], w[i][1], d);
+              if constexpr (kWords == 3)
+                if (!narrow) d = mfma_k32(DT, wf[fn], w[i][2], d);
+              f32x4 v = bitcast<f32x4>(acc[fn][f0 + i]);
+#pragma unroll
+              for (int e = 0; e < 4; ++e)
+                v[e] = own ? v[e] + (ELEM == TCU_ELEM_F16 ? ldexpf(d[e], ex[f0 + i]) : d[e]) : v[e];
+              acc[fn][f0 + i] = bitcast<Acc>(v);
             }
           }
-          auto product = [&](int fn, f32x4 d) __attribute__((always_inline)) {
-            d = mfma_k32(DT, wf[fn], w[0], d);
-            if (kWords == 3 || !narrow) d = mfma_k32(DT, wf[fn], w[1], d);
-            if constexpr (kWords == 3)
-              if (!narrow) d = mfma_k32(DT, wf[fn], w[2], d);
-            return d;
-          };
-          const bool own = id[fm] == g;
+          if (left == 0u) break;
+          g = next;
 #pragma unroll
-          for (int fn = 0; fn < FN; ++fn) {
-            const f32x4 d = product(fn, f32x4{0.f, 0.f, 0.f, 0.f});
-            f32x4 v = bitcast<f32x4>(acc[fn][fm]);
-#pragma unroll
-            for (int e = 0; e < 4; ++e)
-              v[e] = own ? v[e] + (ELEM == TCU_ELEM_F16 ? ldexpf(d[e], ex[fm]) : d[e]) : v[e];
-            acc[fn][fm] = bitcast<Acc>(v);
-          }
+          for (int fn = 0; fn < FN; ++fn) wf[fn] = wn[fn];
         }
+        held = g;
       }
     }
   }
@@ -685,30 +795,29 @@ hipError_t group(const int32_t *ids, const Scratch &s, int64_t M, int64_t G, hip
   return hipGetLastError();
 }
 
-// T of one product, or of two (n1.X not null).
+// T of one product, or of two (n1.X not null); order null: found by the kernel.
 template <int ELEM>
 hipError_t narrow(const Narrow &n0, const Narrow &n1, const float *alpha, const int32_t *ids,
                   const int *order, const int *start, int64_t M, int64_t r, int64_t G,
                   hipStream_t stream) {
   const int rp = (int)rank_pad(r);
-  auto go = [&](auto rows, auto blocks) {
-    constexpr int kRows = decltype(rows)::value, kBlocks = decltype(blocks)::value;
-    hipLaunchKernelGGL((narrow_kernel<ELEM, kRows, kBlocks>),
-                       dim3((unsigned)((M + 16 * kRows - 1) / (16 * kRows)), n1.X ? 2 : 1),
-                       dim3(1024), 0, stream, n0, n1, alpha, ids, order, start, (int)M, (int)r, rp,
-                       (int)G);
+  // pieces: every adapter's last one may be short
+  const int64_t most = (M + kPiece - 1) / kPiece + G - 1;
+  auto go = [&](auto blocks, auto from_ids) {
+    hipLaunchKernelGGL((narrow_kernel<ELEM, decltype(blocks)::value, decltype(from_ids)::value>),
+                       dim3((unsigned)(most < M ? most : M), n1.X ? 2 : 1), dim3(kNarrowThreads), 0,
+                       stream, n0, n1, alpha, ids, order, start, (int)M, (int)r, rp, (int)G);
   };
-  auto by_blocks = [&](auto rows) {
-    if (rp == 16)
-      go(rows, std::integral_constant<int, 1>{});
+  auto by_order = [&](auto blocks) {
+    if (order)
+      go(blocks, std::false_type{});
     else
-      go(rows, std::integral_constant<int, 2>{});
+      go(blocks, std::true_type{});
   };
-  // 32 rows read the factors half as often as 16, as long as they fill the chip
-  if (M >= 8192)
-    by_blocks(std::integral_constant<int, 2>{});
+  if (rp == 16)
+    by_order(std::integral_constant<int, 1>{});
   else
-    by_blocks(std::integral_constant<int, 1>{});
+    by_order(std::integral_constant<int, 2>{});
   return hipGetLastError();
 }
 
@@ -720,10 +829,6 @@ hipError_t transpose(const void *in, void *out, int64_t G, int64_t rows, int64_t
                      (const unsigned short *)in, (unsigned short *)out, rows, cols, tiles);
   return hipGetLastError();
 }
-
-// From how many rows on they are taken in their adapters' order: an order of
-// mixed rows costs a block of 16 rows one product for each of its adapters.
-constexpr int64_t kOrderRows = 1024;
 
 template <int ELEM, int DT, int OUT, bool kQ8>
 hipError_t project(const AdapterArgs &a, const Scratch &s, hipStream_t stream, int num_cus) {
@@ -740,7 +845,7 @@ hipError_t project(const AdapterArgs &a, const Scratch &s, hipStream_t stream, i
       if (e != hipSuccess) return e;
       B = s.padded;
     }
-    const bool ordered = a.M > kOrderRows && a.G > 1;
+    const bool ordered = a.M > kScanRows || a.G > kScanAdapters;
     if (ordered) e = group(a.ids, s, a.M, a.G, stream);
     if (e != hipSuccess) return e;
     const Narrow n{(const unsigned char *)a.X, (const unsigned char *)a.A, s.t, a.ldx, (int)a.K};

@@ -1054,7 +1054,7 @@ gemm_ring_kernel(const unsigned char *__restrict__ A, const unsigned char *__res
 }
 template <int DT, int kTile, int kStages, bool kDma, bool kCut, class Tail>
 __global__ __attribute__((amdgpu_flat_work_group_size(256, 256),
-                          amdgpu_waves_per_eu(1, kTile == 64 ? (kDma ? 3 : 4) : 2))) void
+                          amdgpu_waves_per_eu(kTile == 64 ? 1 : 2, kTile == 64 ? (kDma ? 3 : 4) : 2))) void
 tail_ring_kernel(const unsigned char *__restrict__ A, const unsigned char *__restrict__ B,
                  unsigned char *__restrict__ C, int M, int N, int K, int64_t lda, int64_t ldb,
                  int64_t ldc, int tiles_m, int tiles_n, int nsplit, int whole, int first,
