@@ -306,12 +306,10 @@ __global__ __launch_bounds__(kNarrowThreads, 4) void narrow_kernel(Narrow n0, Na
 // Workgroup g counts the rows of smaller numbers, then places its own.
 // ---------------------------------------------------------------------------
 constexpr int kGroupThreads = 1024, kGroupHeld = 8, kGroupTile = kGroupThreads * kGroupHeld;
-__global__ __launch_bounds__(kGroupThreads) void group_kernel(const int *__restrict__ ids,
-                                                              int *__restrict__ start,
-                                                              int *__restrict__ order, int M,
-                                                              int G) {
+__device__ __forceinline__ void group_rows(const int *__restrict__ ids, int *__restrict__ start,
+                                           int *__restrict__ order, int M, int G, int g) {
   __shared__ int part[kGroupThreads / 64], tab[129];
-  const int lane = threadIdx.x & 63, w = threadIdx.x >> 6, g = blockIdx.x;
+  const int lane = threadIdx.x & 63, w = threadIdx.x >> 6;
   int held[kGroupHeld];
   int below = 0;
   for (int64_t m0 = 0; m0 < M; m0 += kGroupTile) {
@@ -333,6 +331,12 @@ __global__ __launch_bounds__(kGroupThreads) void group_kernel(const int *__restr
                                     [&](int place, int m) { order[at + place] = m; });
   }
   if (g == G - 1 && threadIdx.x == 0) start[G] = at;
+}
+__global__ __launch_bounds__(kGroupThreads) void group_kernel(const int *__restrict__ ids,
+                                                              int *__restrict__ start,
+                                                              int *__restrict__ order, int M,
+                                                              int G) {
+  group_rows(ids, start, order, M, G, blockIdx.x);
 }
 
 // ---------------------------------------------------------------------------
@@ -572,27 +576,43 @@ __global__ __launch_bounds__(256) void pad_ranks_kernel(const unsigned short *__
   }
 }
 
-// out (cols x rows) of every adapter = in (rows x cols), 16-bit values, in
+// out (cols x rows) of every adapter = in (rows x cols), 16-bit values, in `tiles`
 // tiles of 32 x 32.
-__global__ __launch_bounds__(256) void transpose_kernel(const unsigned short *__restrict__ in,
-                                                        unsigned short *__restrict__ out,
-                                                        int64_t rows, int64_t cols,
-                                                        int64_t tiles) {
-  __shared__ unsigned short tile[32][33];
-  const int64_t tc = (cols + 31) / 32, per = tc * ((rows + 31) / 32);
+struct Transpose {
+  const unsigned short *in;
+  unsigned short *out;
+  int64_t rows, cols, tiles;
+};
+__device__ __forceinline__ void transpose_tiles(const Transpose &a, int64_t t, int64_t step,
+                                                unsigned short (&tile)[32][33]) {
+  const int64_t tc = (a.cols + 31) / 32, per = tc * ((a.rows + 31) / 32);
   const int x = threadIdx.x & 31, y = threadIdx.x >> 5;
-  for (int64_t t = blockIdx.x; t < tiles; t += gridDim.x) {
+  for (; t < a.tiles; t += step) {
     const int64_t g = t / per, r0 = (t - g * per) / tc * 32, c0 = (t - g * per) % tc * 32;
-    const int64_t base = g * rows * cols;
-#pragma unroll
-    for (int i = y; i < 32; i += 8)
-      if (r0 + i < rows && c0 + x < cols) tile[i][x] = in[base + (r0 + i) * cols + c0 + x];
+    const int64_t base = g * a.rows * a.cols;
+    if (r0 + y < a.rows && c0 + x < a.cols) tile[y][x] = a.in[base + (r0 + y) * a.cols + c0 + x];
     __syncthreads();
-#pragma unroll
-    for (int i = y; i < 32; i += 8)
-      if (c0 + i < cols && r0 + x < rows) out[base + (c0 + i) * rows + r0 + x] = tile[x][i];
+    if (c0 + y < a.cols && r0 + x < a.rows) a.out[base + (c0 + y) * a.rows + r0 + x] = tile[x][y];
     __syncthreads();
   }
+}
+
+// What the gradients need first, in one launch: one or two transposes and (order
+// not null) the rows' order.
+__global__ __launch_bounds__(kGroupThreads) void prepare_kernel(Transpose t0, Transpose t1,
+                                                                const int *__restrict__ ids,
+                                                                int *__restrict__ start,
+                                                                int *__restrict__ order, int M,
+                                                                int G) {
+  __shared__ unsigned short tile[32][33];
+  const int groups = order ? G : 0;
+  if ((int)blockIdx.x < groups) {
+    group_rows(ids, start, order, M, G, blockIdx.x);
+    return;
+  }
+  const int64_t t = (int)blockIdx.x - groups, step = (int)gridDim.x - groups;
+  transpose_tiles(t0, t, step, tile);
+  transpose_tiles(t1, t, step, tile);
 }
 
 // ---------------------------------------------------------------------------
@@ -821,12 +841,19 @@ hipError_t narrow(const Narrow &n0, const Narrow &n1, const float *alpha, const 
   return hipGetLastError();
 }
 
-hipError_t transpose(const void *in, void *out, int64_t G, int64_t rows, int64_t cols,
-                     hipStream_t stream) {
-  const int64_t tiles = G * ((rows + 31) / 32) * ((cols + 31) / 32);
-  if (tiles == 0) return hipSuccess;
-  hipLaunchKernelGGL(transpose_kernel, dim3(grid_for(tiles)), dim3(256), 0, stream,
-                     (const unsigned short *)in, (unsigned short *)out, rows, cols, tiles);
+Transpose transpose_of(const void *in, void *out, int64_t G, int64_t rows, int64_t cols) {
+  return Transpose{(const unsigned short *)in, (unsigned short *)out, rows, cols,
+                   G * ((rows + 31) / 32) * ((cols + 31) / 32)};
+}
+
+// ids null: the transposes alone.
+hipError_t prepare(const Transpose &t0, const Transpose &t1, const int32_t *ids, const Scratch &s,
+                   int64_t M, int64_t G, hipStream_t stream) {
+  const int64_t tiles = t0.tiles > t1.tiles ? t0.tiles : t1.tiles;
+  const int64_t blocks = (ids ? G : 0) + (tiles < 2048 ? tiles : 2048);
+  if (blocks == 0) return hipSuccess;
+  hipLaunchKernelGGL(prepare_kernel, dim3((unsigned)blocks), dim3(kGroupThreads), 0, stream, t0, t1,
+                     ids, s.start, ids ? s.order : nullptr, (int)M, (int)G);
   return hipGetLastError();
 }
 
@@ -884,8 +911,9 @@ template <int ELEM>
 hipError_t grad_go(const AdapterGradArgs &a, hipStream_t stream) {
   const Scratch s = scratch(a.work, a.M, a.K, a.N, a.r, a.G);
   const int rp = (int)rank_pad(a.r);
-  hipError_t e = group(a.ids, s, a.M, a.G, stream);
-  if (e == hipSuccess) e = transpose(a.B, s.bt, a.G, a.N, a.r, stream);
+  // (no rows: their order is then found empty, whatever ids is)
+  hipError_t e = prepare(transpose_of(a.B, s.bt, a.G, a.N, a.r), Transpose{},
+                         a.M > 0 ? a.ids : (const int32_t *)s.order, s, a.M, a.G, stream);
   if (e != hipSuccess) return e;
   const unsigned char *X = (const unsigned char *)a.X, *dY = (const unsigned char *)a.dY;
   const int chunk = chunk_rows(a.M, a.K, a.N);
@@ -930,8 +958,8 @@ hipError_t launch_adapter_input_grad(int dtype, const AdapterArgs &a, hipStream_
   // The adapters' factors change places: A' = B^T (r x K here), B' = A^T (N x r).
   const Scratch s = scratch(a.work, a.M, a.K, a.N, a.r, a.G);
   AdapterArgs b = a;
-  hipError_t e = transpose(a.B, s.at, a.G, a.K, a.r, stream);
-  if (e == hipSuccess) e = transpose(a.A, s.bt, a.G, a.r, a.N, stream);
+  const hipError_t e = prepare(transpose_of(a.B, s.at, a.G, a.K, a.r),
+                               transpose_of(a.A, s.bt, a.G, a.r, a.N), nullptr, s, a.M, a.G, stream);
   if (e != hipSuccess) return e;
   b.A = s.at;
   b.B = s.bt;
