@@ -406,8 +406,8 @@ int64_t tcu_rms_norm_grad_work(int64_t rows, int64_t cols);
  * that are not finite.  X A^T is summed in binary32 and enters the second
  * product with at least 16 significant bits where Y is bfloat16 and 22
  * otherwise; the sum of both parts is formed in binary32 and rounded once.
- *   0 <= M, K, N <= TCU_MAX_RECT_DIM (M = 0 or N = 0: a no-op);
- *   0 <= G <= TCU_MAX_ADAPTERS;  1 <= r <= TCU_MAX_RANK;
+ *   0 <= M <= TCU_MAX_RECT_DIM, 0 <= K, N <= TCU_MAX_ADAPTED_DIM (M = 0 or
+ *   N = 0: a no-op);  0 <= G <= TCU_MAX_ADAPTERS;  1 <= r <= TCU_MAX_RANK;
  *   A, B, alpha and ids may be NULL if G = 0.
  *   dtype: TCU_F16_F32, TCU_BF16_F32 or TCU_BF16_BF16 (X, W, A, B and Y).
  * As for tcu_gemm, binary32 results with K >= 2048 may differ in their low
@@ -419,6 +419,7 @@ int64_t tcu_rms_norm_grad_work(int64_t rows, int64_t cols);
  * M rows: every row goes through one adapter. */
 #define TCU_MAX_ADAPTERS ((int64_t)1 << 16)
 #define TCU_MAX_RANK 128
+#define TCU_MAX_ADAPTED_DIM ((int64_t)1 << 24)
 int tcu_adapter_gemm(const void *X, int64_t ldx, const void *W, int64_t ldw, const void *A,
                      const void *B, const float *alpha, const int32_t *ids, void *Y, int64_t ldy,
                      void *work, int64_t M, int64_t K, int64_t N, int64_t r, int64_t G, int dtype,

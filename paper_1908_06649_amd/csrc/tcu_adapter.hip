@@ -22,7 +22,7 @@ __host__ __device__ constexpr int64_t rank_pad(int64_t r) { return r <= 16 ? 16 
 // ---------------------------------------------------------------------------
 // T[m][j] = alpha[g] sum_k X[m][k] F_g[j][k] (F_g: r x K, rows contiguous), zeros
 // from rank r on to rank_pad.  A workgroup takes up to 16 rows of one
-// adapter, wherever they lie, and all ranks; its 8 waves take every eighth 64
+// adapter, wherever they lie, and 16 or 32 ranks; its 8 waves take every eighth 64
 // elements of K, and their sums are added in their order.  A load instruction
 // fetches 8 whole lines of 128 bytes (X from memory once, F from the caches); a
 // wave turns them into the matrix cores' operands through its own part of LDS,
@@ -190,7 +190,7 @@ __global__ __launch_bounds__(kNarrowThreads, 4) void narrow_kernel(Narrow n0, Na
                                                       const int *__restrict__ ids,
                                                       const int *__restrict__ order,
                                                       const int *__restrict__ start, int M, int r,
-                                                      int rp, int G) {
+                                                      int rp, int G, int first) {
   constexpr int DT = ELEM == TCU_ELEM_F16 ? TCU_F16_F32 : TCU_BF16_F32;
   constexpr int kWaves = kNarrowThreads / 64, kStep = 64, kPart = (1 + kBlocks) * 2048;
   static_assert(kBlocks * 1024 <= kPart, "a wave's sums");
@@ -201,7 +201,7 @@ __global__ __launch_bounds__(kNarrowThreads, 4) void narrow_kernel(Narrow n0, Na
   const int c = lane & 15, q = lane >> 4;
   const int lr = lane >> 3, lc = lane & 7;      // a load's row and chunk
   Piece &found = *(Piece *)lds;
-  const int count = find_piece<kFromIds>(found, ids, order, start, M, G, blockIdx.x);
+  const int count = find_piece<kFromIds>(found, ids, order, start, M, G, first + blockIdx.x);
   if (count == 0) return;
   const int g = __builtin_amdgcn_readfirstlane(found.g);
   const int row = found.rows[c < count ? c : count - 1];
@@ -217,86 +217,84 @@ __global__ __launch_bounds__(kNarrowThreads, 4) void narrow_kernel(Narrow n0, Na
   for (int h = 0; h < 2; ++h) get[h] = mine_lds + c * 128 + 16 * ((4 * h + q) ^ (c & 7));
   const unsigned char *fg = n.F + 2 * ((int64_t)g * r * n.K + 8 * lc);
   const float al = alpha[g];
-  for (int j0 = 0; j0 < rp; j0 += 16 * kBlocks) {
-    const unsigned char *f[kBlocks][2];
-    f32x4 acc[kBlocks];
+  const int j0 = blockIdx.z * (16 * kBlocks);
+  const unsigned char *f[kBlocks][2];
+  f32x4 acc[kBlocks];
 #pragma unroll
-    for (int b = 0; b < kBlocks; ++b) {
+  for (int b = 0; b < kBlocks; ++b) {
+#pragma unroll
+    for (int h = 0; h < 2; ++h) {
+      const int j = j0 + 16 * b + 8 * h + lr;
+      f[b][h] = fg + 2 * (int64_t)(j < r ? j : r - 1) * n.K;
+    }
+    acc[b] = f32x4{0.f, 0.f, 0.f, 0.f};
+  }
+  struct Chunk {
+    u32x4 x[2], f[kBlocks][2];
+  };
+  auto load = [&](int k, Chunk &v) __attribute__((always_inline)) {
+    if (k + kStep <= n.K) {
 #pragma unroll
       for (int h = 0; h < 2; ++h) {
-        const int j = j0 + 16 * b + 8 * h + lr;
-        f[b][h] = fg + 2 * (int64_t)(j < r ? j : r - 1) * n.K;
+        v.x[h] = load16_any(x[h] + 2 * k);
+#pragma unroll
+        for (int b = 0; b < kBlocks; ++b) v.f[b][h] = load16_any(f[b][h] + 2 * k);
       }
-      acc[b] = f32x4{0.f, 0.f, 0.f, 0.f};
-    }
-    struct Chunk {
-      u32x4 x[2], f[kBlocks][2];
-    };
-    auto load = [&](int k, Chunk &v) __attribute__((always_inline)) {
-      if (k + kStep <= n.K) {
-#pragma unroll
-        for (int h = 0; h < 2; ++h) {
-          v.x[h] = load16_any(x[h] + 2 * k);
-#pragma unroll
-          for (int b = 0; b < kBlocks; ++b) v.f[b][h] = load16_any(f[b][h] + 2 * k);
-        }
-      } else {
-        // zeros past K
-        const int valid = n.K - k - 8 * lc;
-#pragma unroll
-        for (int h = 0; h < 2; ++h) {
-          v.x[h] = load8<ELEM>(x[h] + 2 * k, valid).v[0];
-#pragma unroll
-          for (int b = 0; b < kBlocks; ++b) v.f[b][h] = load8<ELEM>(f[b][h] + 2 * k, valid).v[0];
-        }
-      }
-    };
-    auto multiply = [&](const Chunk &v) __attribute__((always_inline)) {
+    } else {
+      // zeros past K
+      const int valid = n.K - k - 8 * lc;
 #pragma unroll
       for (int h = 0; h < 2; ++h) {
-        *(u32x4 *)(put + 1024 * h) = v.x[h];
+        v.x[h] = load8<ELEM>(x[h] + 2 * k, valid).v[0];
 #pragma unroll
-        for (int b = 0; b < kBlocks; ++b)
-          *(u32x4 *)(put + 2048 * (1 + b) + 1024 * h) = v.f[b][h];
-      }
-#pragma unroll
-      for (int h = 0; h < 2; ++h) {
-        const u32x4 xf = *(const u32x4 *)get[h];
-#pragma unroll
-        for (int b = 0; b < kBlocks; ++b)
-          acc[b] = mfma_k32(DT, *(const u32x4 *)(get[h] + 2048 * (1 + b)), xf, acc[b]);
-      }
-    };
-    // kAhead chunks in flight
-    constexpr int kAhead = kBlocks == 1 ? 4 : 2, kNext = kWaves * kStep;
-    Chunk v[kAhead];
-    int k = w * kStep;
-#pragma unroll
-    for (int u = 0; u < kAhead; ++u)
-      if (k + u * kNext < n.K) load(k + u * kNext, v[u]);
-    while (k < n.K) {
-#pragma unroll
-      for (int u = 0; u < kAhead; ++u) {
-        if (k >= n.K) break;
-        multiply(v[u]);
-        if (k + kAhead * kNext < n.K) load(k + kAhead * kNext, v[u]);
-        k += kNext;
+        for (int b = 0; b < kBlocks; ++b) v.f[b][h] = load8<ELEM>(f[b][h] + 2 * k, valid).v[0];
       }
     }
+  };
+  auto multiply = [&](const Chunk &v) __attribute__((always_inline)) {
 #pragma unroll
-    for (int b = 0; b < kBlocks; ++b) *(f32x4 *)(mine_lds + b * 1024 + 16 * lane) = acc[b];
-    __syncthreads();
-    if (w < kBlocks) {
-      f32x4 v = *(const f32x4 *)(lds + w * 1024 + 16 * lane);
+    for (int h = 0; h < 2; ++h) {
+      *(u32x4 *)(put + 1024 * h) = v.x[h];
 #pragma unroll
-      for (int u = 1; u < kWaves; ++u) v += *(const f32x4 *)(lds + u * kPart + w * 1024 + 16 * lane);
-      // ranks j .. j + 3 of row c
-      const int j = j0 + 16 * w + 4 * q;
-#pragma unroll
-      for (int e = 0; e < 4; ++e) v[e] = j + e < r ? v[e] * al : 0.f;
-      if (c < count) *(f32x4 *)(n.T + (int64_t)row * rp + j) = v;
+      for (int b = 0; b < kBlocks; ++b)
+        *(u32x4 *)(put + 2048 * (1 + b) + 1024 * h) = v.f[b][h];
     }
-    __syncthreads();   // read before the next sums overwrite
+#pragma unroll
+    for (int h = 0; h < 2; ++h) {
+      const u32x4 xf = *(const u32x4 *)get[h];
+#pragma unroll
+      for (int b = 0; b < kBlocks; ++b)
+        acc[b] = mfma_k32(DT, *(const u32x4 *)(get[h] + 2048 * (1 + b)), xf, acc[b]);
+    }
+  };
+  // kAhead chunks in flight
+  constexpr int kAhead = kBlocks == 1 ? 4 : 2, kNext = kWaves * kStep;
+  Chunk v[kAhead];
+  int k = w * kStep;
+#pragma unroll
+  for (int u = 0; u < kAhead; ++u)
+    if (k + u * kNext < n.K) load(k + u * kNext, v[u]);
+  while (k < n.K) {
+#pragma unroll
+    for (int u = 0; u < kAhead; ++u) {
+      if (k >= n.K) break;
+      multiply(v[u]);
+      if (k + kAhead * kNext < n.K) load(k + kAhead * kNext, v[u]);
+      k += kNext;
+    }
+  }
+#pragma unroll
+  for (int b = 0; b < kBlocks; ++b) *(f32x4 *)(mine_lds + b * 1024 + 16 * lane) = acc[b];
+  __syncthreads();
+  if (w < kBlocks) {
+    f32x4 v = *(const f32x4 *)(lds + w * 1024 + 16 * lane);
+#pragma unroll
+    for (int u = 1; u < kWaves; ++u) v += *(const f32x4 *)(lds + u * kPart + w * 1024 + 16 * lane);
+    // ranks j .. j + 3 of row c
+    const int j = j0 + 16 * w + 4 * q;
+#pragma unroll
+    for (int e = 0; e < 4; ++e) v[e] = j + e < r ? v[e] * al : 0.f;
+    if (c < count) *(f32x4 *)(n.T + (int64_t)row * rp + j) = v;
   }
 }
 
@@ -577,22 +575,38 @@ __global__ __launch_bounds__(256) void pad_ranks_kernel(const unsigned short *__
 }
 
 // out (cols x rows) of every adapter = in (rows x cols), 16-bit values, in `tiles`
-// tiles of 32 x 32.
+// tiles of 4096: 32 along the shorter side, the rank's, 128 along the other.
 struct Transpose {
   const unsigned short *in;
   unsigned short *out;
   int64_t rows, cols, tiles;
 };
+__host__ __device__ constexpr int64_t tiles_of(int64_t rows, int64_t cols) {
+  return rows < cols ? (rows + 31) / 32 * ((cols + 127) / 128)
+                     : (rows + 127) / 128 * ((cols + 31) / 32);
+}
+template <int kR, int kC>
 __device__ __forceinline__ void transpose_tiles(const Transpose &a, int64_t t, int64_t step,
-                                                unsigned short (&tile)[32][33]) {
-  const int64_t tc = (a.cols + 31) / 32, per = tc * ((a.rows + 31) / 32);
-  const int x = threadIdx.x & 31, y = threadIdx.x >> 5;
+                                                unsigned short *tile) {
+  const unsigned tc = (unsigned)((a.cols + kC - 1) / kC), per = (unsigned)tiles_of(a.rows, a.cols);
+  const int rows = (int)a.rows, cols = (int)a.cols;
   for (; t < a.tiles; t += step) {
-    const int64_t g = t / per, r0 = (t - g * per) / tc * 32, c0 = (t - g * per) % tc * 32;
-    const int64_t base = g * a.rows * a.cols;
-    if (r0 + y < a.rows && c0 + x < a.cols) tile[y][x] = a.in[base + (r0 + y) * a.cols + c0 + x];
+    const int64_t g = t / per, base = g * a.rows * a.cols;
+    const unsigned in_g = (unsigned)(t - g * per);
+    const int r0 = in_g / tc * kR, c0 = in_g % tc * kC;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      const int e = threadIdx.x + 1024 * i, y = e / kC, x = e % kC;
+      if (r0 + y < rows && c0 + x < cols)
+        tile[y * (kC + 2) + x] = a.in[base + (int64_t)(r0 + y) * cols + c0 + x];
+    }
     __syncthreads();
-    if (c0 + y < a.cols && r0 + x < a.rows) a.out[base + (c0 + y) * a.rows + r0 + x] = tile[x][y];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      const int e = threadIdx.x + 1024 * i, y = e / kR, x = e % kR;
+      if (c0 + y < cols && r0 + x < rows)
+        a.out[base + (int64_t)(c0 + y) * rows + r0 + x] = tile[x * (kC + 2) + y];
+    }
     __syncthreads();
   }
 }
@@ -604,20 +618,27 @@ __global__ __launch_bounds__(kGroupThreads) void prepare_kernel(Transpose t0, Tr
                                                                 int *__restrict__ start,
                                                                 int *__restrict__ order, int M,
                                                                 int G) {
-  __shared__ unsigned short tile[32][33];
+  __shared__ unsigned short tile[128 * 34];
   const int groups = order ? G : 0;
   if ((int)blockIdx.x < groups) {
     group_rows(ids, start, order, M, G, blockIdx.x);
     return;
   }
   const int64_t t = (int)blockIdx.x - groups, step = (int)gridDim.x - groups;
-  transpose_tiles(t0, t, step, tile);
-  transpose_tiles(t1, t, step, tile);
+  auto transpose = [&](const Transpose &a) {
+    if (a.rows < a.cols)
+      transpose_tiles<32, 128>(a, t, step, tile);
+    else
+      transpose_tiles<128, 32>(a, t, step, tile);
+  };
+  transpose(t0);
+  transpose(t1);
 }
 
 // ---------------------------------------------------------------------------
 // D_g(j, c) = sum over g's rows of T[m][j] X[m][c], the rows in the order of
-// group_kernel cut into chunks.  A workgroup takes one chunk and 128 columns,
+// group_kernel cut into chunks.  A workgroup takes one chunk, 128 columns and
+// every gridDim.z'th adapter,
 // its 4 waves every fourth group of 4 rows: binary32 matrix products over 4 rows,
 // a lane holding 8 columns of one of them (16 bytes), value e of the 16 lanes
 // being columns e, 8 + e, .. of product e.  An adapter whose rows lie in one
@@ -636,7 +657,6 @@ constexpr int kFactorCols = 128;
 
 template <int ELEM, int kBlocks>
 __global__ __launch_bounds__(256) void factor_kernel(Factor f0, Factor f1,
-                                                     const int *__restrict__ ids,
                                                      const int *__restrict__ order,
                                                      const int *__restrict__ start, int r, int rp,
                                                      int G, int chunk, int cols0) {
@@ -650,84 +670,92 @@ __global__ __launch_bounds__(256) void factor_kernel(Factor f0, Factor f1,
   const int end = begin + chunk < count ? begin + chunk : count;
   const int col = c0 + 8 * c, valid = f.C - col;
   const int64_t rc = (int64_t)r * f.C;
-  for (int at = begin; at < end;) {
-    const int g = ids[order[at]];
-    const int s0 = start[g], s1 = start[g + 1], to = s1 < end ? s1 : end;
-    float *out;
-    int64_t dj = f.dj, dc = f.dc;
-    if (s0 >= begin && s1 <= end) {
-      out = f.D + g * rc;
-    } else {
-      out = f.parts + (2 * (int64_t)blockIdx.y + (s0 >= begin)) * rc;
-      dj = f.C;
-      dc = 1;
-    }
-    for (int j0 = 0; j0 < rp; j0 += 16 * kBlocks) {
-      f32x4 acc[kBlocks][8];
+  // this workgroup's adapters with rows in the chunk: every gridDim.z'th
+  for (int g0 = blockIdx.z; g0 < G; g0 += 64 * gridDim.z) {
+    const int gl = g0 + lane * (int)gridDim.z;
+    const int b0 = gl < G ? start[gl] : 0, b1 = gl < G ? start[gl + 1] : 0;
+    unsigned long long here = __ballot(b0 < b1 && b0 < end && b1 > begin);
+    while (here != 0) {
+      const int from = __builtin_ctzll(here);
+      here &= here - 1;
+      const int g = g0 + from * (int)gridDim.z;
+      const int s0 = __builtin_amdgcn_readlane(b0, from), s1 = __builtin_amdgcn_readlane(b1, from);
+      const int at = s0 > begin ? s0 : begin, to = s1 < end ? s1 : end;
+      float *out;
+      int64_t dj = f.dj, dc = f.dc;
+      if (s0 >= begin && s1 <= end) {
+        out = f.D + g * rc;
+      } else {
+        out = f.parts + (2 * (int64_t)blockIdx.y + (s0 >= begin)) * rc;
+        dj = f.C;
+        dc = 1;
+      }
+      for (int j0 = 0; j0 < rp; j0 += 16 * kBlocks) {
+        f32x4 acc[kBlocks][8];
 #pragma unroll
-      for (int b = 0; b < kBlocks; ++b)
+        for (int b = 0; b < kBlocks; ++b)
 #pragma unroll
-        for (int e = 0; e < 8; ++e) acc[b][e] = f32x4{0.f, 0.f, 0.f, 0.f};
-      // kU groups of 4 rows, their loads in flight together; past the run's end
-      // (not `whole`) zeros
-      constexpr int kU = 4;
-      auto rows = [&](int m0, auto whole) __attribute__((always_inline)) {
-        constexpr bool kWhole = decltype(whole)::value;
-        Raw8<ELEM> xr[kU];
-        float t[kU][kBlocks];
-        int m[kU];
+          for (int e = 0; e < 8; ++e) acc[b][e] = f32x4{0.f, 0.f, 0.f, 0.f};
+        // kU groups of 4 rows, their loads in flight together; past the run's end
+        // (not `whole`) zeros
+        constexpr int kU = 4;
+        auto rows = [&](int m0, auto whole) __attribute__((always_inline)) {
+          constexpr bool kWhole = decltype(whole)::value;
+          Raw8<ELEM> xr[kU];
+          float t[kU][kBlocks];
+          int m[kU];
 #pragma unroll
-        for (int u = 0; u < kU; ++u) {
-          const int i = m0 + 16 * u + q;
-          m[u] = order[kWhole || i < to ? i : to - 1];
-        }
+          for (int u = 0; u < kU; ++u) {
+            const int i = m0 + 16 * u + q;
+            m[u] = order[kWhole || i < to ? i : to - 1];
+          }
 #pragma unroll
-        for (int u = 0; u < kU; ++u) {
-          const bool in = kWhole || m0 + 16 * u + q < to;
-          xr[u] = load8<ELEM>(f.X + 2 * ((int64_t)m[u] * f.ldx + col),
-                              kWhole ? 8 : in ? valid : 0);
+          for (int u = 0; u < kU; ++u) {
+            const bool in = kWhole || m0 + 16 * u + q < to;
+            xr[u] = load8<ELEM>(f.X + 2 * ((int64_t)m[u] * f.ldx + col),
+                                kWhole ? 8 : in ? valid : 0);
 #pragma unroll
-          for (int b = 0; b < kBlocks; ++b)
-            t[u][b] = in ? f.T[(int64_t)m[u] * rp + j0 + 16 * b + c] : 0.f;
-        }
+            for (int b = 0; b < kBlocks; ++b)
+              t[u][b] = in ? f.T[(int64_t)m[u] * rp + j0 + 16 * b + c] : 0.f;
+          }
 #pragma unroll
-        for (int u = 0; u < kU; ++u) {
-          float x[8];
-          unpack8<ELEM>(xr[u], x);
+          for (int u = 0; u < kU; ++u) {
+            float x[8];
+            unpack8<ELEM>(xr[u], x);
 #pragma unroll
-          for (int b = 0; b < kBlocks; ++b)
+            for (int b = 0; b < kBlocks; ++b)
 #pragma unroll
-            for (int e = 0; e < 8; ++e)
-              acc[b][e] = __builtin_amdgcn_mfma_f32_16x16x4f32(t[u][b], x[e], acc[b][e], 0, 0, 0);
-        }
-      };
-      int m0 = at + 4 * w;
-      if (c0 + kFactorCols <= f.C)
-        for (; m0 + 16 * (kU - 1) + 4 <= to; m0 += 16 * kU) rows(m0, std::true_type{});
-      for (; m0 < to; m0 += 16 * kU) rows(m0, std::false_type{});
-      // the waves' sums, 16 ranks at a time: lane holds ranks 4 q .. of column 8 c + e
+              for (int e = 0; e < 8; ++e)
+                acc[b][e] = __builtin_amdgcn_mfma_f32_16x16x4f32(t[u][b], x[e], acc[b][e], 0, 0, 0);
+          }
+        };
+        int m0 = at + 4 * w;
+        if (c0 + kFactorCols <= f.C)
+          for (; m0 + 16 * (kU - 1) + 4 <= to; m0 += 16 * kU) rows(m0, std::true_type{});
+        for (; m0 < to; m0 += 16 * kU) rows(m0, std::false_type{});
+        // the waves' sums, 16 ranks at a time: lane holds ranks 4 q .. of column 8 c + e
 #pragma unroll
-      for (int b = 0; b < kBlocks; ++b) {
-        __syncthreads();
+        for (int b = 0; b < kBlocks; ++b) {
+          __syncthreads();
 #pragma unroll
-        for (int e = 0; e < 8; ++e) sums[w][e][lane] = acc[b][e];
-        __syncthreads();
+          for (int e = 0; e < 8; ++e) sums[w][e][lane] = acc[b][e];
+          __syncthreads();
 #pragma unroll
-        for (int h = 0; h < 2; ++h) {
-          const int e = 2 * w + h;
-          f32x4 v = sums[0][e][lane];
+          for (int h = 0; h < 2; ++h) {
+            const int e = 2 * w + h;
+            f32x4 v = sums[0][e][lane];
 #pragma unroll
-          for (int u = 1; u < 4; ++u) v += sums[u][e][lane];
-          const int cc = col + e, j = j0 + 16 * b + 4 * q;
-          if (cc < f.C) {
+            for (int u = 1; u < 4; ++u) v += sums[u][e][lane];
+            const int cc = col + e, j = j0 + 16 * b + 4 * q;
+            if (cc < f.C) {
 #pragma unroll
-            for (int k = 0; k < 4; ++k)
-              if (j + k < r) out[(j + k) * dj + cc * dc] = v[k];
+              for (int k = 0; k < 4; ++k)
+                if (j + k < r) out[(j + k) * dj + cc * dc] = v[k];
+            }
           }
         }
       }
     }
-    at = to;
   }
 }
 
@@ -768,7 +796,7 @@ int chunk_rows(int64_t M, int64_t K, int64_t N) {
   const int64_t strips = (K + kFactorCols - 1) / kFactorCols + (N + kFactorCols - 1) / kFactorCols;
   int64_t rows = M * strips / 1024;
   rows = (rows + 63) / 64 * 64;
-  return (int)(rows < 64 ? 64 : rows > 8192 ? 8192 : rows);
+  return (int)(rows < 64 ? 64 : rows);
 }
 
 // Scratch: T of X and of dY, the rows in their adapters' order, the adapters
@@ -824,9 +852,17 @@ hipError_t narrow(const Narrow &n0, const Narrow &n1, const float *alpha, const 
   // pieces: every adapter's last one may be short
   const int64_t most = (M + kPiece - 1) / kPiece + G - 1;
   auto go = [&](auto blocks, auto from_ids) {
-    hipLaunchKernelGGL((narrow_kernel<ELEM, decltype(blocks)::value, decltype(from_ids)::value>),
-                       dim3((unsigned)(most < M ? most : M), n1.X ? 2 : 1), dim3(kNarrowThreads), 0,
-                       stream, n0, n1, alpha, ids, order, start, (int)M, (int)r, rp, (int)G);
+    constexpr int kBlocks = decltype(blocks)::value;
+    // a launch counts its work items in 32 bits
+    constexpr int64_t kMost = 1 << 22;
+    const int64_t pieces = most < M ? most : M;
+    for (int64_t first = 0;
+         first < pieces && (first == 0 || hipPeekAtLastError() == hipSuccess); first += kMost)
+      hipLaunchKernelGGL((narrow_kernel<ELEM, kBlocks, decltype(from_ids)::value>),
+                         dim3((unsigned)(pieces - first < kMost ? pieces - first : kMost),
+                              n1.X ? 2 : 1, rp / (16 * kBlocks)),
+                         dim3(kNarrowThreads), 0, stream, n0, n1, alpha, ids, order, start, (int)M,
+                         (int)r, rp, (int)G, (int)first);
   };
   auto by_order = [&](auto blocks) {
     if (order)
@@ -843,7 +879,7 @@ hipError_t narrow(const Narrow &n0, const Narrow &n1, const float *alpha, const 
 
 Transpose transpose_of(const void *in, void *out, int64_t G, int64_t rows, int64_t cols) {
   return Transpose{(const unsigned short *)in, (unsigned short *)out, rows, cols,
-                   G * ((rows + 31) / 32) * ((cols + 31) / 32)};
+                   G * tiles_of(rows, cols)};
 }
 
 // ids null: the transposes alone.
@@ -857,11 +893,42 @@ hipError_t prepare(const Transpose &t0, const Transpose &t1, const int32_t *ids,
   return hipGetLastError();
 }
 
+// The narrow product's launch beside a product of few tiles.
+constexpr double kNarrowUs = 9;
+
 template <int ELEM, int DT, int OUT, bool kQ8>
 hipError_t project(const AdapterArgs &a, const Scratch &s, hipStream_t stream, int num_cus) {
+  typedef AdapterTail<ELEM, OUT, kQ8> Tail;
+  const RectArgs p{kQ8 ? a.Xq : a.X, kQ8 ? a.ldxq : a.ldx, a.W, a.ldw, a.Y, a.ldy,
+                   a.M, a.K, a.N, false};
   const int64_t rp = rank_pad(a.r), rb = (a.r + 7) / 8 * 8;
-  const void *B = a.B;
+  auto narrow_of = [&]() {
+    const bool ordered = a.M > kScanRows || a.G > kScanAdapters;
+    const hipError_t e = ordered ? group(a.ids, s, a.M, a.G, stream) : hipSuccess;
+    if (e != hipSuccess) return e;
+    const Narrow n{(const unsigned char *)a.X, (const unsigned char *)a.A, s.t, a.ldx, (int)a.K};
+    return narrow<ELEM>(n, Narrow{}, a.alpha, a.ids, ordered ? s.order : nullptr, s.start, a.M, a.r,
+                        a.G, stream);
+  };
   hipError_t e = hipSuccess;
+  if (few_ok(DT, a)) {
+    // Past one block of rows by the models of both sides' times.
+    const int64_t cus = knob(TCU_KNOB_PP_GRID) > 0 ? knob(TCU_KNOB_PP_GRID) : num_cus;
+    const bool dma = ring_dma_ok<DT>(p);
+    double t_us = few_narrow_us(a, kQ8);
+    const bool apart = t_us > kNarrowUs;
+    if (apart) t_us = kNarrowUs;
+    if (a.M <= kFewBlock ||
+        (gemm_path() == GemmPath::kAuto &&
+         few_us(a, kQ8) + t_us <
+             choose_ring<DT, Tail>(p, dma, GemmPath::kAuto, cus).us + kNarrowUs)) {
+      AdapterArgs b = a;
+      b.work = s.few;
+      if (apart) e = narrow_of();
+      return e != hipSuccess ? e : launch_few(DT, b, apart ? s.t : nullptr, (int)rp, stream);
+    }
+  }
+  const void *B = a.B;
   if (a.G > 0) {
     if (rb != a.r) {
       const int64_t rows = a.G * a.N;
@@ -872,28 +939,16 @@ hipError_t project(const AdapterArgs &a, const Scratch &s, hipStream_t stream, i
       if (e != hipSuccess) return e;
       B = s.padded;
     }
-    const bool ordered = a.M > kScanRows || a.G > kScanAdapters;
-    if (ordered) e = group(a.ids, s, a.M, a.G, stream);
-    if (e != hipSuccess) return e;
-    const Narrow n{(const unsigned char *)a.X, (const unsigned char *)a.A, s.t, a.ldx, (int)a.K};
-    e = narrow<ELEM>(n, Narrow{}, a.alpha, a.ids, ordered ? s.order : nullptr, s.start, a.M, a.r,
-                     a.G, stream);
+    e = narrow_of();
     if (e != hipSuccess) return e;
   }
-  const AdapterTail<ELEM, OUT, kQ8> tail{s.t, a.xscale, a.wscale, (const unsigned char *)B,
-                                         a.ids, a.N * rb * 2, (int)rp, (int)rb, (int)a.G};
-  const RectArgs p{kQ8 ? a.Xq : a.X, kQ8 ? a.ldxq : a.ldx, a.W, a.ldw, a.Y, a.ldy,
-                   a.M, a.K, a.N, false};
+  const Tail tail{s.t,   a.xscale,       a.wscale, (const unsigned char *)B,
+                  a.ids, a.N * rb * 2, (int)rp,  (int)rb, (int)a.G};
   return launch_dt<DT>(p, stream, num_cus, tail);
 }
 
 hipError_t project_dt(int dtype, const AdapterArgs &a, const Scratch &s, hipStream_t stream,
                       int num_cus) {
-  if (few_ok(dtype, a)) {
-    AdapterArgs b = a;
-    b.work = s.few;
-    return launch_few(dtype, b, stream);
-  }
   switch (dtype) {
     case TCU_F16_F32:
       return project<TCU_ELEM_F16, TCU_F16_F32, TCU_F16_F32, false>(a, s, stream, num_cus);
@@ -926,12 +981,14 @@ hipError_t grad_go(const AdapterGradArgs &a, hipStream_t stream) {
     if (e != hipSuccess) return e;
     const int ca = (int)((a.K + kFactorCols - 1) / kFactorCols);
     const int cb = (int)((a.N + kFactorCols - 1) / kFactorCols);
-    const dim3 grid(ca + cb, (unsigned)((a.M + chunk - 1) / chunk));
+    // a chunk's adapters side by side, about as many workgroups as it has adapters
+    const int64_t chunks = (a.M + chunk - 1) / chunk, beside = a.G / chunks + 1;
+    const dim3 grid(ca + cb, (unsigned)chunks, (unsigned)(beside < 16 ? beside : 16));
     if (rp == 16)
-      hipLaunchKernelGGL((factor_kernel<ELEM, 1>), grid, dim3(256), 0, stream, fa, fb, a.ids,
+      hipLaunchKernelGGL((factor_kernel<ELEM, 1>), grid, dim3(256), 0, stream, fa, fb,
                          s.order, s.start, (int)a.r, rp, (int)a.G, chunk, ca);
     else
-      hipLaunchKernelGGL((factor_kernel<ELEM, 2>), grid, dim3(256), 0, stream, fa, fb, a.ids,
+      hipLaunchKernelGGL((factor_kernel<ELEM, 2>), grid, dim3(256), 0, stream, fa, fb,
                          s.order, s.start, (int)a.r, rp, (int)a.G, chunk, ca);
     e = hipGetLastError();
     if (e != hipSuccess) return e;

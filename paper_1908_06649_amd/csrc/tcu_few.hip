@@ -3,6 +3,8 @@
 //
 // few_kernel forms the product's partial sums and T = alpha X A^T in one launch,
 // join_kernel adds the partial sums and T B^T and rounds.
+//   * Rows go in blocks of 64, each reading W for itself (the later ones from the
+//     caches).
 //   * A workgroup's 8 waves share a strip of W's columns (64 of 16 bits, 128 of
 //     8) over one of `splits` ranges of the contracted index, one or two
 //     workgroups per CU in all; the waves take the steps of 64 bytes of it in turn, for all
@@ -71,9 +73,10 @@ struct FewArgs {
   const float *alpha;
   const int *ids;
   unsigned *parts;                 // splits x M x N sums (binary32 or int32)
-  float *T;                        // M x r
+  float *T;                        // M rows of tld
   int64_t ldx, ldw, ldxa;
-  int M, K, N, r, G, strips, splits;
+  int M, K, N, r, G, strips, splits, tld;
+  bool narrow;                     // T is formed here
 };
 
 // One value of T: row i / r, rank i % r, by one wave.
@@ -109,7 +112,7 @@ __device__ __forceinline__ void narrow_value(const FewArgs &a, int i) {
     if (valid > 0) add(load8<ELEM>(x + 2 * k, valid), load8<ELEM>(f + 2 * k, valid));
   }
   s = wave_sum(s);
-  if (lane == 0) a.T[i] = s * a.alpha[g];
+  if (lane == 0) a.T[(int64_t)m * a.tld + j] = s * a.alpha[g];
 }
 
 // DT: the product's types; ELEM: the adapters'; kMB: blocks of 16 rows.
@@ -123,6 +126,7 @@ __global__ __launch_bounds__(64 * kWaves) void few_kernel(FewArgs a) {
   typedef typename std::conditional<kI8, i32x4, f32x4>::type Acc;
   constexpr int kRowLds = S::kStrip + 4;
   __shared__ unsigned sums[kWaves][16 * kRowLds];
+  const int row0 = blockIdx.y * (int)kFewBlock, rows = min(a.M - row0, (int)kFewBlock);
   const int split = blockIdx.x / a.strips, n0 = (blockIdx.x - split * a.strips) * S::kStrip;
   const int lane = threadIdx.x & 63, w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int c = lane & 15, q = lane >> 4;
@@ -135,7 +139,7 @@ __global__ __launch_bounds__(64 * kWaves) void few_kernel(FewArgs a) {
   const unsigned char *xp[kMB];
 #pragma unroll
   for (int b = 0; b < kMB; ++b)
-    xp[b] = a.X + ((int64_t)min(16 * b + c, a.M - 1) * a.ldx + S::kRun * q) * ES;
+    xp[b] = a.X + ((int64_t)(row0 + min(16 * b + c, rows - 1)) * a.ldx + S::kRun * q) * ES;
   Acc acc[kMB][S::kCols];
 #pragma unroll
   for (int b = 0; b < kMB; ++b)
@@ -180,8 +184,9 @@ __global__ __launch_bounds__(64 * kWaves) void few_kernel(FewArgs a) {
   // The adapters' narrow product while the first step is on its way: its values
   // in turn over all waves of the grid.
   auto narrow = [&]() {
-    const int all = a.G > 0 ? a.M * a.r : 0;
-    for (int i = blockIdx.x + w * gridDim.x; i < all; i += gridDim.x * kWaves)
+    const int all = a.narrow ? a.M * a.r : 0;
+    const int groups = gridDim.x * gridDim.y;
+    for (int i = blockIdx.y * gridDim.x + blockIdx.x + w * groups; i < all; i += groups * kWaves)
       narrow_value<ELEM>(a, i);
   };
   int s = s_begin + w;
@@ -213,7 +218,7 @@ __global__ __launch_bounds__(64 * kWaves) void few_kernel(FewArgs a) {
   // of the strip and row c of the block.
 #pragma unroll
   for (int b = 0; b < kMB; ++b) {
-    if (16 * b >= a.M) break;
+    if (16 * b >= rows) break;
     if (b > 0) __syncthreads();   // read before the next sums overwrite
 #pragma unroll
     for (int j = 0; j < S::kCols; ++j)
@@ -232,8 +237,8 @@ __global__ __launch_bounds__(64 * kWaves) void few_kernel(FewArgs a) {
       }
       const int first = n0 + at / S::kCols * S::kCols;
       const int n = min(first, a.N - S::kCols) + at % S::kCols;
-      if (16 * b + m < a.M && n >= first)
-        a.parts[((int64_t)split * a.M + 16 * b + m) * a.N + n] = v;
+      if (16 * b + m < rows && n >= first)
+        a.parts[((int64_t)split * a.M + row0 + 16 * b + m) * a.N + n] = v;
     }
   }
 }
@@ -260,7 +265,7 @@ __global__ __launch_bounds__(256) void join_kernel(FewArgs f, const unsigned cha
   const int g = f.G > 0 ? f.ids[m] : -1;
   if (g >= 0 && g < f.G) {
     const unsigned char *b = B + 2 * (((int64_t)g * f.N + n) * f.r);
-    const float *t = f.T + (int64_t)m * f.r;
+    const float *t = f.T + (int64_t)m * f.tld;
     float low = 0.f;
     for (int j = 0; j < f.r; j += 8) {
       float x[8];
@@ -275,7 +280,7 @@ __global__ __launch_bounds__(256) void join_kernel(FewArgs f, const unsigned cha
   f32_to_elem<OUT>(Y + ((int64_t)m * ldy + n) * elem_bytes<OUT>, v);
 }
 
-int row_blocks(int64_t M) { return M <= 16 ? 1 : (int)((M + 15) / 16); }
+int row_blocks(int64_t M) { return M <= 16 ? 1 : M < kFewBlock ? (int)((M + 15) / 16) : 4; }
 
 int strip_cols(bool q8) { return q8 ? Step<1>::kStrip : Step<2>::kStrip; }
 
@@ -288,7 +293,8 @@ int few_splits(int64_t M, int64_t K, int64_t N, bool q8) {
   const int64_t strips = N > 0 ? (N + strip_cols(q8) - 1) / strip_cols(q8) : 1;
   const int64_t wave_elems = (int64_t)(q8 ? 64 : 32) * kWaves;
   const int64_t want = !q8 && M <= 32 ? 512 : 256;
-  int64_t n = (want + strips / 2) / strips;
+  const int64_t groups = strips * ((M + kFewBlock - 1) / kFewBlock);
+  int64_t n = groups > 0 ? (want + groups / 2) / groups : 1;
   const int64_t most = (K + wave_elems - 1) / wave_elems;
   if (n > most) n = most;
   return (int)(n < 1 ? 1 : n > 16 ? 16 : n);
@@ -299,7 +305,7 @@ int64_t parts_bytes(int64_t M, int64_t K, int64_t N, bool q8) {
 }
 
 template <int DT, int ELEM, int OUT, bool kQ8>
-hipError_t few(const AdapterArgs &a, hipStream_t stream) {
+hipError_t few(const AdapterArgs &a, float *T, int tld, hipStream_t stream) {
   const int strips = (int)((a.N + strip_cols(kQ8) - 1) / strip_cols(kQ8));
   const int splits = few_splits(a.M, a.K, a.N, kQ8);
   const FewArgs f{(const unsigned char *)(kQ8 ? a.Xq : a.X),
@@ -309,7 +315,7 @@ hipError_t few(const AdapterArgs &a, hipStream_t stream) {
                   a.alpha,
                   a.ids,
                   (unsigned *)a.work,
-                  (float *)((unsigned char *)a.work + parts_bytes(a.M, a.K, a.N, kQ8)),
+                  T ? T : (float *)((unsigned char *)a.work + parts_bytes(a.M, a.K, a.N, kQ8)),
                   kQ8 ? a.ldxq : a.ldx,
                   a.ldw,
                   a.ldx,
@@ -319,8 +325,10 @@ hipError_t few(const AdapterArgs &a, hipStream_t stream) {
                   (int)a.r,
                   (int)a.G,
                   strips,
-                  splits};
-  const dim3 grid(strips * splits);
+                  splits,
+                  T ? tld : (int)a.r,
+                  a.G > 0 && !T};
+  const dim3 grid(strips * splits, (unsigned)((a.M + kFewBlock - 1) / kFewBlock));
   auto go = [&](auto blocks) {
     constexpr int kMB = decltype(blocks)::value;
     hipLaunchKernelGGL((few_kernel<DT, ELEM, kMB>), grid,
@@ -347,18 +355,42 @@ bool few_ok(int dtype, const AdapterArgs &a) {
   return a.M <= kFewRows && a.K > 0 && a.N >= (dtype == TCU_I8_I32 ? 8 : 4);
 }
 
+// What forming T here adds: one value a wave goes under the loads of W, each more
+// takes a memory latency, about a microsecond, for every 2048 elements of K and
+// every 512 of the rest (188 x 6976 x 512 rank 64: 56 us with T here, 37 with it
+// apart; 148 x 2845 x 369 rank 64 int8 102 / 37; 256 x 8192 x 256 rank 16 22 / 27).
+double few_narrow_us(const AdapterArgs &a, bool q8) {
+  const int64_t strips = (a.N + strip_cols(q8) - 1) / strip_cols(q8);
+  const int64_t waves = strips * few_splits(a.M, a.K, a.N, q8) *
+                        ((a.M + kFewBlock - 1) / kFewBlock) * kWaves;
+  const int64_t values = a.G > 0 ? (a.M * a.r + waves - 1) / waves : 0;
+  const int64_t latencies = a.K / 2048 + (a.K % 2048 + 511) / 512;
+  return values > 1 ? (double)((values - 1) * latencies) * 1.05 : 0.0;
+}
+
+// Us, here / tiles with the narrow product's launch, W not in the caches: bf16
+// 128 x 4096 x 4096 27 / 45, 192 x 4096 x 4096 42 / 44, 256 x 4096 x 1024 20 / 33,
+// 101 x 6848 x 832 25 / 43, 128 x 8192 x 8192 72 / 74; int8 128 x 4096 x 4096
+// 21 / 38, 256 x 2048 x 2048 19 / 18.
+double few_us(const AdapterArgs &a, bool q8) {
+  const double blocks = (double)((a.M + kFewBlock - 1) / kFewBlock);
+  return 6 + blocks * (double)a.K * (double)a.N * (q8 ? 1 : 2) / 3.2e6;
+}
+
 int64_t few_work_bytes(int64_t M, int64_t K, int64_t N, int64_t r) {
   if (M > kFewRows) return 0;
   const int64_t a = parts_bytes(M, K, N, false), b = parts_bytes(M, K, N, true);
   return (a > b ? a : b) + M * r * 4;
 }
 
-hipError_t launch_few(int dtype, const AdapterArgs &a, hipStream_t stream) {
+hipError_t launch_few(int dtype, const AdapterArgs &a, float *T, int tld, hipStream_t stream) {
   switch (dtype) {
-    case TCU_F16_F32: return few<TCU_F16_F32, TCU_ELEM_F16, TCU_ELEM_F32, false>(a, stream);
-    case TCU_BF16_F32: return few<TCU_BF16_F32, TCU_ELEM_BF16, TCU_ELEM_F32, false>(a, stream);
-    case TCU_BF16_BF16: return few<TCU_BF16_BF16, TCU_ELEM_BF16, TCU_ELEM_BF16, false>(a, stream);
-    case TCU_I8_I32: return few<TCU_I8_I32, TCU_ELEM_BF16, TCU_ELEM_BF16, true>(a, stream);
+    case TCU_F16_F32: return few<TCU_F16_F32, TCU_ELEM_F16, TCU_ELEM_F32, false>(a, T, tld, stream);
+    case TCU_BF16_F32:
+      return few<TCU_BF16_F32, TCU_ELEM_BF16, TCU_ELEM_F32, false>(a, T, tld, stream);
+    case TCU_BF16_BF16:
+      return few<TCU_BF16_BF16, TCU_ELEM_BF16, TCU_ELEM_BF16, false>(a, T, tld, stream);
+    case TCU_I8_I32: return few<TCU_I8_I32, TCU_ELEM_BF16, TCU_ELEM_BF16, true>(a, T, tld, stream);
   }
   return hipErrorInvalidValue;
 }

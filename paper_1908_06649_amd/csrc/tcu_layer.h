@@ -59,10 +59,13 @@ hipError_t launch_adapter_grad(int elem, const AdapterGradArgs &a, hipStream_t s
 hipError_t launch_adapter_input_grad(int dtype, const AdapterArgs &a, hipStream_t stream,
                                      int num_cus);
 // The same for few rows (see tcu_few.hip), with work of few_work_bytes; the
-// sizes it takes, by few_ok.
-constexpr int64_t kFewRows = 64;
+// sizes it takes, by few_ok, and its time in microseconds.
+constexpr int64_t kFewBlock = 64, kFewRows = 256;
 bool few_ok(int dtype, const AdapterArgs &a);
-hipError_t launch_few(int dtype, const AdapterArgs &a, hipStream_t stream);
+double few_us(const AdapterArgs &a, bool q8);
+double few_narrow_us(const AdapterArgs &a, bool q8);
+// T: the narrow product, rows of tld values, or null: it is formed there too.
+hipError_t launch_few(int dtype, const AdapterArgs &a, float *T, int tld, hipStream_t stream);
 int64_t few_work_bytes(int64_t M, int64_t K, int64_t N, int64_t r);
 int64_t adapter_work_bytes(int64_t M, int64_t K, int64_t N, int64_t r, int64_t G);
 

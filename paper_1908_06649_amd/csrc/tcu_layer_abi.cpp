@@ -88,7 +88,7 @@ int64_t blocks(int64_t n, int64_t s) { return (n + s - 1) / s; }
 
 // Whether sizes are in range, G * r * max(K, N) 16-bit values among them.
 int check_sizes(int64_t M, int64_t K, int64_t N, int64_t r, int64_t G) {
-  if (!dim_ok(M) || !dim_ok(K) || !dim_ok(N) || G < 0 || G > TCU_MAX_ADAPTERS || r < 1 ||
+  if (!dim_ok(M) || K < 0 || N < 0 || K > TCU_MAX_ADAPTED_DIM || N > TCU_MAX_ADAPTED_DIM || G < 0 || G > TCU_MAX_ADAPTERS || r < 1 ||
       r > TCU_MAX_RANK)
     return TCU_ERR_SHAPE;
   if (G * r * std::max(K, N) >= kMaxExtent / 4) return TCU_ERR_SHAPE;

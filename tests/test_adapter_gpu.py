@@ -13,7 +13,8 @@ SIZES = [(1, 64, 64, 16, 1), (1, 1000, 257, 8, 4), (3, 512, 1024, 16, 3), (8, 40
          (16, 100, 96, 4, 2), (17, 33, 31, 1, 3), (40, 2048, 640, 32, 40), (64, 1024, 1000, 16, 5),
          (65, 257, 129, 20, 2), (100, 8, 8, 64, 3), (130, 640, 300, 128, 2), (256, 512, 512, 16, 1),
          (300, 1003, 517, 8, 7), (513, 320, 768, 32, 4), (1000, 256, 264, 16, 30),
-         (2, 3, 5, 3, 2), (33, 1, 1, 2, 2), (700, 4096, 256, 16, 2)]
+         (2, 3, 5, 3, 2), (33, 1, 1, 2, 2), (700, 4096, 256, 16, 2), (128, 4096, 256, 16, 5),
+         (256, 2048, 200, 8, 3), (64, 8192, 72, 128, 4), (200, 3001, 100, 64, 9)]
 
 
 def work_of(d):
@@ -238,6 +239,26 @@ def test_adapter_wide_offsets(M):
                          work_of(d), M, 200, 136, 16, 3)
     y, e = d.forward64()
     within(Y, y, e + y.abs() * ROUND[BF16])
+
+
+def test_adapter_more_pieces_than_a_launch():
+    """2^26 rows of one adapter: 2^22 pieces of 16 rows and some."""
+    M = (1 << 26) + 33
+    d = Layer(64, 8, 8, 4, 2, BF16, 3, torch.ones(64))
+    reps = M // 64 + 1
+    X = d.X.to(DEV).repeat(reps, 1)[:M]
+    ids = torch.ones(M, dtype=torch.int32, device=DEV)
+    ids[:100] = 0
+    Y = torch.empty(M, 8, dtype=BF16, device=DEV)
+    work = torch.empty(tcu.tcu_adapter_work(M, 8, 8, 4, 2), dtype=torch.uint8, device=DEV)
+    tcu.tcu_adapter_gemm(X, 8, d.W.to(DEV), 8, *dev(d.A, d.B, d.alpha), ids, Y, 8, work, M, 8, 8, 4,
+                         2)
+    y, e = d.forward64()
+    within(Y[128:192], y, e + y.abs() * ROUND[BF16])
+    tail = Y[128:][:(M - 128) // 64 * 64].view(-1, 64, 8)
+    assert bool((tail == tail[0]).all())
+    rest = (M - 128) % 64
+    assert torch.equal(Y[M - rest:], tail[0][:rest])
 
 
 def test_adapter_other_stream_and_graph():

@@ -57,7 +57,8 @@ for f, left, right, out in ((FWD, "X", "W", "Y"), (Q8, "X", "Wq", "Y"), (IG, "dY
                             (AG, "X", "dY", "dA")):
     REFUSED += [(f, {k: 0}, NULL) for k in (left, right, "A", "B", "alpha", "ids", out, "work")]
     REFUSED += [(f, {k: v}, SHAPE) for k, v in (("M", -1), ("K", -1), ("N", -5), ("M", BIG + 1),
-                                                ("r", 0), ("r", 129), ("G", -1), ("G", 65537))]
+                                                ("r", 0), ("r", 129), ("G", -1), ("G", 65537),
+                                                ("K", (1 << 24) + 1), ("N", (1 << 24) + 1))]
     REFUSED += [(f, {k: CALLS[f][k] + 2}, ALIGN) for k in (left, "A", "B", out, "work", "ids")]
     REFUSED += [(f, {out: CALLS[f][left]}, OVER), (f, {out: CALLS[f]["A"]}, OVER),
                 (f, dict(work=CALLS[f][right]), OVER), (f, {"work": CALLS[f][out]}, OVER)]
