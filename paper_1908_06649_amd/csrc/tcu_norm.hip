@@ -90,8 +90,10 @@ __device__ __forceinline__ void store_q8(unsigned char *p, const float (&y)[8], 
   }
 }
 
+// (without an eps a row of zeros has none to divide by: 0, not NaN)
 __device__ __forceinline__ float rstd_of(float sum_sq, int64_t cols, float eps) {
-  return 1.f / sqrtf(sum_sq / (float)cols + eps);
+  const float v = sum_sq / (float)cols + eps;
+  return v == 0.f ? 0.f : 1.f / sqrtf(v);
 }
 
 // Vector i of a lane's row: eight columns from `col` on.  A row's last vector

@@ -173,3 +173,27 @@ def test_norm_wide_offsets():
     _, y64 = norm64(x, None, w, EPS)
     within(y, y64, y64.abs() * (2.0 ** -8 + sum_bound(cols)))
     assert torch.equal(view.cpu(), x)
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("cols", [5, 600, 3001, 17000])
+def test_zero_rows_without_eps(dtype, cols):
+    """eps = 0: a row of zeros stays zero, its gradient is dh alone; others as ever."""
+    g = gen(cols)
+    x, w, dy, dh = (randn(s, dtype, g) for s in ((3, cols), (cols,), (3, cols), (3, cols)))
+    x[1] = 0
+    y = torch.empty(3, cols, dtype=dtype, device=DEV)
+    q, s = torch.empty(3, cols, dtype=torch.int8, device=DEV), torch.empty(3, device=DEV)
+    tcu.tcu_rms_norm(x.to(DEV), cols, None, 0, w.to(DEV), None, 0, y, cols, q, cols, s, 3, cols,
+                     0.0)
+    assert bool((y[1] == 0).all()) and bool((q[1] == 0).all()) and float(s[1]) == 0
+    tiny = 2.0 ** -24 if dtype == torch.float16 else 0.0
+    _, y64 = norm64(x[::2], None, w, 0.0)
+    within(y[::2], y64, y64.abs() * (ROUND[dtype] + sum_bound(cols)) + tiny)
+    dx, dw = torch.empty(3, cols, dtype=dtype, device=DEV), torch.empty(cols, device=DEV)
+    work = torch.empty(tcu.tcu_rms_norm_grad_work(3, cols), dtype=torch.uint8, device=DEV)
+    tcu.tcu_rms_norm_grad(dy.to(DEV), cols, x.to(DEV), cols, w.to(DEV), dh.to(DEV), cols, dx, cols,
+                          dw, work, 3, cols, 0.0)
+    assert torch.equal(dx[1].cpu(), dh[1])
+    _, w64, _, wm = norm_grad64(dy[::2], x[::2], w, dh[::2], 0.0)
+    within(dw, w64, wm * (sum_bound(cols) + 64 * F32))
