@@ -79,25 +79,26 @@ struct FewArgs {
   bool narrow;                     // T is formed here
 };
 
-// One value of T: row i / r, rank i % r, by one wave.
-template <int ELEM>
+// One value of T: row i / r, rank i % r, by one wave, 512 kU elements of both
+// operands in flight (a memory latency each: 16 x 8192 x 8192 int8 rank 16 23.7 us with
+// 8, 24.6 with 4).
+template <int ELEM, int kU>
 __device__ __forceinline__ void narrow_value(const FewArgs &a, int i) {
   const int m = i / a.r, j = i - m * a.r, g = a.ids[m];
   if (g < 0 || g >= a.G) return;
   const int lane = threadIdx.x & 63;
-  const unsigned char *x = a.XA + 2 * ((int64_t)m * a.ldxa + 8 * lane);
-  const unsigned char *f = a.A + 2 * (((int64_t)g * a.r + j) * a.K + 8 * lane);
+  const unsigned char *x = a.XA + 2 * (int64_t)m * a.ldxa;
+  const unsigned char *f = a.A + 2 * ((int64_t)g * a.r + j) * a.K;
   float s = 0.f;
-  auto add = [&](const Raw8<ELEM> &xr, const Raw8<ELEM> &fr) {
+  auto add = [&](const Raw8<ELEM> &xr, const Raw8<ELEM> &fr, int from) __attribute__((always_inline)) {
     float xv[8], fv[8];
     unpack8<ELEM>(xr, xv);
     unpack8<ELEM>(fr, fv);
 #pragma unroll
-    for (int e = 0; e < 8; ++e) s += xv[e] * fv[e];
+    for (int e = 0; e < 8; ++e) s += e >= from ? xv[e] * fv[e] : 0.f;
   };
-  int k = 0;
-  constexpr int kU = 4;
-  for (; k + 512 * kU <= a.K; k += 512 * kU) {
+  int k = 8 * lane;
+  for (; k - 8 * lane + 512 * kU <= a.K; k += 512 * kU) {
     Raw8<ELEM> xr[kU], fr[kU];
 #pragma unroll
     for (int u = 0; u < kU; ++u) {
@@ -105,11 +106,26 @@ __device__ __forceinline__ void narrow_value(const FewArgs &a, int i) {
       fr[u].v[0] = load16_any(f + 2 * (k + 512 * u));
     }
 #pragma unroll
-    for (int u = 0; u < kU; ++u) add(xr[u], fr[u]);
+    for (int u = 0; u < kU; ++u) add(xr[u], fr[u], 0);
   }
-  for (; k < a.K; k += 512) {
-    const int valid = a.K - k - 8 * lane;
-    if (valid > 0) add(load8<ELEM>(x + 2 * k, valid), load8<ELEM>(f + 2 * k, valid));
+  if (a.K >= 8) {
+    // the rest four vectors at once: one that would pass the end begins at the last
+    // eight elements, those before its own left out
+    constexpr int kRest = 4;
+    for (; k - 8 * lane < a.K; k += 512 * kRest) {
+      Raw8<ELEM> xr[kRest], fr[kRest];
+#pragma unroll
+      for (int u = 0; u < kRest; ++u) {
+        const int at = min(k + 512 * u, a.K - 8);
+        xr[u].v[0] = load16_any(x + 2 * at);
+        fr[u].v[0] = load16_any(f + 2 * at);
+      }
+#pragma unroll
+      for (int u = 0; u < kRest; ++u)
+        add(xr[u], fr[u], k + 512 * u - min(k + 512 * u, a.K - 8));
+    }
+  } else if (lane == 0) {
+    add(load8<ELEM>(x, a.K), load8<ELEM>(f, a.K), 0);
   }
   s = wave_sum(s);
   if (lane == 0) a.T[(int64_t)m * a.tld + j] = s * a.alpha[g];
@@ -122,6 +138,8 @@ __global__ __launch_bounds__(64 * kWaves) void few_kernel(FewArgs a) {
   // 8-bit W and more than 32 rows: a second step's registers are not there
   constexpr bool kAhead = ES == 2 || kMB <= 2;
   constexpr bool kI8 = ES == 1;
+  // (8 would leave room for one workgroup where two fit)
+  constexpr int kNarrowAhead = kI8 || kMB > 2 ? 8 : 4;
   typedef Step<ES> S;
   typedef typename std::conditional<kI8, i32x4, f32x4>::type Acc;
   constexpr int kRowLds = S::kStrip + 4;
@@ -187,7 +205,7 @@ __global__ __launch_bounds__(64 * kWaves) void few_kernel(FewArgs a) {
     const int all = a.narrow ? a.M * a.r : 0;
     const int groups = gridDim.x * gridDim.y;
     for (int i = blockIdx.y * gridDim.x + blockIdx.x + w * groups; i < all; i += groups * kWaves)
-      narrow_value<ELEM>(a, i);
+      narrow_value<ELEM, kNarrowAhead>(a, i);
   };
   int s = s_begin + w;
   if constexpr (kAhead) {
@@ -244,36 +262,78 @@ __global__ __launch_bounds__(64 * kWaves) void few_kernel(FewArgs a) {
 }
 
 // Y = the ranges' sums (scaled, 8-bit) + T B^T, rounded once.
-template <int ELEM, int OUT, bool kQ8>
+// kAtOnce ranges' sums and kHeld vectors of 8 ranks are loaded together: no more than
+// there are (200 x 2048 x 2048, two ranges: 16.1 us of a call, 17.2 with eight).
+template <int ELEM, int OUT, bool kQ8, int kAtOnce, int kHeld>
 __global__ __launch_bounds__(256) void join_kernel(FewArgs f, const unsigned char *__restrict__ B,
                                                    const float *__restrict__ xscale,
                                                    const float *__restrict__ wscale,
                                                    unsigned char *__restrict__ Y, int64_t ldy) {
   const int n = blockIdx.x * 256 + threadIdx.x, m = blockIdx.y;
   if (n >= f.N) return;
+  // What the sums do not wait for goes first: the row's adapter, the ranges' sums,
+  // the scales, then the adapter's ranks (8 x 4096 x 4096 3.1 us, one after the
+  // other 4.6).
+  const int g = f.G > 0 ? f.ids[m] : -1;
+  const bool adapted = g >= 0 && g < f.G;
   const unsigned *p = f.parts + (int64_t)m * f.N + n;
   const int64_t range = (int64_t)f.M * f.N;
+  // (no branch around a load: the compiler would wait for it there)
+  // (no branch around a load: the compiler would wait for it there)
+  unsigned u[kAtOnce];
+#pragma unroll
+  for (int i = 0; i < kAtOnce; ++i) u[i] = p[min(i, f.splits - 1) * range];
+  const float scale = kQ8 ? xscale[m] : 1.f, col_scale = kQ8 ? wscale[n] : 1.f;
+  const unsigned char *b = B + 2 * (((int64_t)g * f.N + n) * f.r);
+  const float *t = f.T + (int64_t)m * f.tld;
+  const int whole = f.r & ~7;      // ranks in whole vectors
+  struct Held {
+    u32x4 b[kHeld];
+    float t[8 * kHeld];
+  } held = {};
+  // ranks j0 .. of the whole vectors, the last ones again past them
+  auto load = [&](int j0) __attribute__((always_inline)) {
+#pragma unroll
+    for (int i = 0; i < kHeld; ++i) {
+      const int j = min(j0 + 8 * i, whole - 8);
+      held.b[i] = load16_any(b + 2 * j);
+#pragma unroll
+      for (int e = 0; e < 8; ++e) held.t[8 * i + e] = t[j + e];
+    }
+  };
+  if (adapted && whole > 0) load(0);
   float v;
   if constexpr (kQ8) {
     int sum = 0;
-    for (int s = 0; s < f.splits; ++s) sum += (int)p[s * range];
-    v = (float)sum * xscale[m] * wscale[n];
+#pragma unroll
+    for (int i = 0; i < kAtOnce; ++i) sum += i < f.splits ? (int)u[i] : 0;
+    for (int s = kAtOnce; s < f.splits; ++s) sum += (int)p[s * range];
+    v = (float)sum * scale * col_scale;
   } else {
     v = 0.f;
-    for (int s = 0; s < f.splits; ++s) v += bitcast<float>(p[s * range]);
+#pragma unroll
+    for (int i = 0; i < kAtOnce; ++i) v += i < f.splits ? bitcast<float>(u[i]) : 0.f;
+    for (int s = kAtOnce; s < f.splits; ++s) v += bitcast<float>(p[s * range]);
   }
-  const int g = f.G > 0 ? f.ids[m] : -1;
-  if (g >= 0 && g < f.G) {
-    const unsigned char *b = B + 2 * (((int64_t)g * f.N + n) * f.r);
-    const float *t = f.T + (int64_t)m * f.tld;
+  if (adapted) {
     float low = 0.f;
-    for (int j = 0; j < f.r; j += 8) {
+    for (int j0 = 0; j0 < whole; j0 += 8 * kHeld) {
+      if (j0 > 0) load(j0);
+#pragma unroll
+      for (int i = 0; i < kHeld; ++i) {
+        float x[8];
+        unpack8<ELEM>(Raw8<ELEM>{held.b[i]}, x);
+        if (j0 + 8 * i < whole)
+#pragma unroll
+          for (int e = 0; e < 8; ++e) low += held.t[8 * i + e] * x[e];
+      }
+    }
+    if (whole < f.r) {
       float x[8];
-      const int valid = f.r - j;
-      unpack8<ELEM>(load8<ELEM>(b + 2 * j, valid), x);
+      unpack8<ELEM>(load8<ELEM>(b + 2 * whole, f.r - whole), x);
 #pragma unroll
       for (int e = 0; e < 8; ++e)
-        if (e < valid) low += t[j + e] * x[e];
+        if (whole + e < f.r) low += t[whole + e] * x[e];
     }
     v += low;
   }
@@ -342,9 +402,24 @@ hipError_t few(const AdapterArgs &a, float *T, int tld, hipStream_t stream) {
   }
   const hipError_t e = hipGetLastError();
   if (e != hipSuccess) return e;
-  hipLaunchKernelGGL((join_kernel<ELEM, OUT, kQ8>),
-                     dim3((unsigned)((a.N + 255) / 256), (unsigned)a.M), dim3(256), 0, stream, f,
-                     (const unsigned char *)a.B, a.xscale, a.wscale, (unsigned char *)a.Y, a.ldy);
+  auto join = [&](auto at_once, auto held) {
+    hipLaunchKernelGGL(
+        (join_kernel<ELEM, OUT, kQ8, decltype(at_once)::value, decltype(held)::value>),
+        dim3((unsigned)((a.N + 255) / 256), (unsigned)a.M), dim3(256), 0, stream, f,
+        (const unsigned char *)a.B, a.xscale, a.wscale, (unsigned char *)a.Y, a.ldy);
+  };
+  auto join_ranks = [&](auto at_once) {
+    if (a.r <= 16)
+      join(at_once, std::integral_constant<int, 2>{});
+    else
+      join(at_once, std::integral_constant<int, 4>{});
+  };
+  if (splits <= 2)
+    join_ranks(std::integral_constant<int, 2>{});
+  else if (splits <= 4)
+    join_ranks(std::integral_constant<int, 4>{});
+  else
+    join_ranks(std::integral_constant<int, 8>{});
   return hipGetLastError();
 }
 
@@ -356,16 +431,18 @@ bool few_ok(int dtype, const AdapterArgs &a) {
 }
 
 // What forming T here adds: one value a wave goes under the loads of W, each more
-// takes a memory latency, about a microsecond, for every 2048 elements of K and
-// every 512 of the rest (188 x 6976 x 512 rank 64: 56 us with T here, 37 with it
-// apart; 148 x 2845 x 369 rank 64 int8 102 / 37; 256 x 8192 x 256 rank 16 22 / 27).
+// takes a loaded memory's latency for as much of K as a wave has in flight (us, T here / apart:
+// 188 x 6976 x 512 rank 64 50.6 / 33.9; 148 x 2845 x 369 rank 64 int8 83.1 / 39.4;
+// 64 x 4096 x 512 rank 64 int8 37.5 / 26.9; 256 x 8192 x 256 rank 16 20.0 / 24.2;
+// 128 x 4096 x 1024 rank 32 15.3 / 21.4).
 double few_narrow_us(const AdapterArgs &a, bool q8) {
   const int64_t strips = (a.N + strip_cols(q8) - 1) / strip_cols(q8);
   const int64_t waves = strips * few_splits(a.M, a.K, a.N, q8) *
                         ((a.M + kFewBlock - 1) / kFewBlock) * kWaves;
   const int64_t values = a.G > 0 ? (a.M * a.r + waves - 1) / waves : 0;
-  const int64_t latencies = a.K / 2048 + (a.K % 2048 + 511) / 512;
-  return values > 1 ? (double)((values - 1) * latencies) * 1.05 : 0.0;
+  const int64_t deep = q8 || a.M > 32 ? 4096 : 2048;
+  const int64_t latencies = a.K / deep + (a.K % deep + 2047) / 2048;
+  return values > 1 ? (double)((values - 1) * latencies) * 1.6 : 0.0;
 }
 
 // Us, here / tiles with the narrow product's launch, W not in the caches: bf16
