@@ -28,7 +28,7 @@ __host__ __device__ constexpr int64_t rank_pad(int64_t r) { return r <= 16 ? 16 
 // wave turns them into the matrix cores' operands through its own part of LDS,
 // 16-byte chunks XOR-swizzled by the row, without barriers.
 //
-// Which rows a workgroup takes it finds out by itself (kFromIds: up to kScanRows
+// Which rows a workgroup takes it finds out by itself (kHeld > 0: up to kScanRows
 // rows and kScanAdapters adapters): it counts every adapter's rows, and with
 // them the pieces of 16 rows before its own, then places its adapter's
 // rows.  Larger calls, and those that need the order elsewhere, read it off
@@ -46,15 +46,22 @@ struct Narrow {
   int K;
 };
 
-// Inclusive sum over a workgroup's lanes in their order; part: a word of LDS per wave.
+// Inclusive sum over a wave's lanes in their order, in its registers.
+__device__ __forceinline__ int wave_scan(int v) {
+  v += __builtin_amdgcn_update_dpp(0, v, 0x111, 0xf, 0xf, false);   // from 1, 2, 4 and 8
+  v += __builtin_amdgcn_update_dpp(0, v, 0x112, 0xf, 0xf, false);   // lanes below, in rows
+  v += __builtin_amdgcn_update_dpp(0, v, 0x114, 0xf, 0xf, false);   // of 16
+  v += __builtin_amdgcn_update_dpp(0, v, 0x118, 0xf, 0xf, false);
+  v += __builtin_amdgcn_update_dpp(0, v, 0x142, 0xa, 0xf, false);   // rows 0 and 2 to 1 and 3
+  v += __builtin_amdgcn_update_dpp(0, v, 0x143, 0xc, 0xf, false);   // the lower half to the upper
+  return v;
+}
+
+// The same over a workgroup's lanes; part: a word of LDS per wave.
 template <int kThreads>
 __device__ __forceinline__ int block_scan(int v, int *part) {
   const int lane = threadIdx.x & 63, w = threadIdx.x >> 6;
-#pragma unroll
-  for (int s = 1; s < 64; s <<= 1) {
-    const int o = __shfl_up(v, s);
-    v += lane >= s ? o : 0;
-  }
+  v = wave_scan(v);
   __syncthreads();   // earlier reads of part
   if (lane == 63) part[w] = v;
   __syncthreads();
@@ -78,105 +85,116 @@ __device__ __forceinline__ void load_ids(const int *__restrict__ ids, int m0, in
 
 // f(place, row) for every row of the tile that names g, its place among them in
 // the order of the rows; returns how many there are.  tab: LDS, a word for each
-// wave and held row, and one more.
+// wave and held row, free when this is called.  Every wave adds up the whole
+// table for itself: no second wait.
 template <int kThreads, int kHeld, typename F>
 __device__ __forceinline__ int place_rows(const int (&held)[kHeld], int g, int m0, int *tab, F f) {
-  constexpr int kWaves = kThreads / 64, kWords = kWaves * kHeld;
-  static_assert(kWords == 128, "two words a lane");
-  const int lane = threadIdx.x & 63, w = threadIdx.x >> 6;
-  __syncthreads();   // earlier reads of tab
+  constexpr int kWaves = kThreads / 64, kWords = kWaves * kHeld, kPer = kWords > 64 ? 2 : 1;
+  static_assert(kWords == 128 || kWords <= 64, "one or two words a lane");
+  const int lane = threadIdx.x & 63, w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  unsigned long long votes[kHeld];
 #pragma unroll
   for (int i = 0; i < kHeld; ++i) {
-    const int n = __popcll(__ballot(held[i] == g));
-    if (lane == 0) tab[i * kWaves + w] = n;
+    votes[i] = __ballot(held[i] == g);
+    if (lane == 0) tab[i * kWaves + w] = __popcll(votes[i]);
   }
   __syncthreads();
-  if (w == 0) {
-    const int a = tab[2 * lane], b = tab[2 * lane + 1];
-    int v = a + b;
-#pragma unroll
-    for (int s = 1; s < 64; s <<= 1) {
-      const int o = __shfl_up(v, s);
-      v += lane >= s ? o : 0;
-    }
-    tab[2 * lane] = v - a - b;
-    tab[2 * lane + 1] = v - b;
-    if (lane == 63) tab[kWords] = v;
-  }
-  __syncthreads();
+  const int a = kPer == 2 || lane < kWords ? tab[kPer * lane] : 0;
+  const int sum = kPer == 2 ? a + tab[2 * lane + 1] : a;
+  const int upto = wave_scan(sum), before = upto - sum;
 #pragma unroll
   for (int i = 0; i < kHeld; ++i) {
-    const unsigned long long votes = __ballot(held[i] == g);
+    const int word = i * kWaves + w, from = word / kPer;
+    int at = __builtin_amdgcn_readlane(before, from);
+    if (kPer == 2 && (word & 1)) at += __builtin_amdgcn_readlane(a, from);
     if (held[i] == g)
-      f(tab[i * kWaves + w] + __popcll(votes & ((1ull << lane) - 1)),
-        m0 + kThreads * i + (int)threadIdx.x);
+      f(at + __popcll(votes[i] & ((1ull << lane) - 1)), m0 + kThreads * i + (int)threadIdx.x);
   }
-  return tab[kWords];
+  return __builtin_amdgcn_readlane(upto, 63);
 }
 
-// The adapter of piece `piece` and the rows of it (up to kPiece of them, to
-// rows[]); returns how many there are, 0 if there is no such piece.
+// The adapter of piece `piece` (to g) and the rows of it (up to kPiece of them, to
+// rows[]); returns how many there are, 0 if there is no such piece.  kHeld: every
+// lane looks through so many rows' numbers, 0: read off the order.
 struct Piece {
-  int bins[kScanAdapters], part[8], tab[129], rows[kPiece], g, chunk, n;
+  int bins[kScanAdapters], part[8], tab[kScanHeld * 8], rows[kPiece], g, chunk, n;
 };
-template <bool kFromIds>
+template <int kHeld>
 __device__ __forceinline__ int find_piece(Piece &s, const int *__restrict__ ids,
                                           const int *__restrict__ order,
-                                          const int *__restrict__ start, int M, int G, int piece) {
-  const int t = threadIdx.x;
-  int held[kScanHeld];
+                                          const int *__restrict__ start, int M, int G, int piece,
+                                          int &g) {
+  const int t = threadIdx.x, lane = t & 63;
+  int held[kHeld > 0 ? kHeld : 1], chunk, n;
   if (t == 0) s.n = 0;
-  if constexpr (kFromIds) {
+  auto found = [&]() {
+    __syncthreads();
+    g = s.g;
+    chunk = s.chunk;
+    n = s.n;
+  };
+  if constexpr (kHeld > 0) {
     load_ids<kNarrowThreads>(ids, 0, M, G, held);
     s.bins[t] = 0;
     __syncthreads();
     // (sums of counts: any order gives the same).  A wave whose rows all name one
     // adapter adds them at once: one by one its lanes would queue at one address.
 #pragma unroll
-    for (int i = 0; i < kScanHeld; ++i) {
+    for (int i = 0; i < kHeld; ++i) {
       if (kNarrowThreads * i >= M) break;
       const int lead = __builtin_amdgcn_readfirstlane(held[i]);
       if (__all(held[i] == lead)) {
-        if ((t & 63) == 0 && lead >= 0) atomicAdd(&s.bins[lead], 64);
+        if (lane == 0 && lead >= 0) atomicAdd(&s.bins[lead], 64);
       } else if (held[i] >= 0) {
         atomicAdd(&s.bins[held[i]], 1);
       }
     }
     __syncthreads();
-    const int n = s.bins[t], pieces = (n + kPiece - 1) / kPiece;
-    const int before = block_scan<kNarrowThreads>(pieces, s.part) - pieces;
-    if (piece >= before && piece < before + pieces) {
-      s.g = t;
-      s.chunk = piece - before;
-      s.n = min(n - s.chunk * kPiece, kPiece);
+    if (G <= 64) {
+      // every wave for itself
+      const int rows = s.bins[lane], pieces = (rows + kPiece - 1) / kPiece;
+      const int before = wave_scan(pieces) - pieces;
+      const unsigned long long hit = __ballot(piece >= before && piece < before + pieces);
+      if (hit == 0) return 0;
+      g = __builtin_ctzll(hit);
+      chunk = piece - __builtin_amdgcn_readlane(before, g);
+      n = min(__builtin_amdgcn_readlane(rows, g) - chunk * kPiece, kPiece);
+    } else {
+      const int rows = s.bins[t], pieces = (rows + kPiece - 1) / kPiece;
+      const int before = block_scan<kNarrowThreads>(pieces, s.part) - pieces;
+      if (piece >= before && piece < before + pieces) {
+        s.g = t;
+        s.chunk = piece - before;
+        s.n = min(rows - s.chunk * kPiece, kPiece);
+      }
+      found();
     }
   } else {
     int base = 0;
     for (int g0 = 0; g0 < G && base <= piece; g0 += kNarrowThreads) {
-      const int g = g0 + t, n = g < G ? start[g + 1] - start[g] : 0;
-      const int pieces = (n + kPiece - 1) / kPiece;
+      const int at = g0 + t, rows = at < G ? start[at + 1] - start[at] : 0;
+      const int pieces = (rows + kPiece - 1) / kPiece;
       const int upto = block_scan<kNarrowThreads>(pieces, s.part), before = base + upto - pieces;
       if (piece >= before && piece < before + pieces) {
-        s.g = g;
+        s.g = at;
         s.chunk = piece - before;
-        s.n = min(n - s.chunk * kPiece, kPiece);
+        s.n = min(rows - s.chunk * kPiece, kPiece);
       }
       __syncthreads();   // s.part has been read
       if (t == kNarrowThreads - 1) s.part[0] = upto;
       __syncthreads();
       base += s.part[0];
     }
+    found();
   }
-  __syncthreads();
-  const int n = s.n;
   if (n == 0) return 0;
-  const int from = s.chunk * kPiece;
-  if constexpr (kFromIds) {
-    place_rows<kNarrowThreads>(held, s.g, 0, s.tab, [&](int at, int m) {
+  const int from = chunk * kPiece;
+  if constexpr (kHeld > 0) {
+    place_rows<kNarrowThreads>(held, g, 0, s.tab, [&](int at, int m) {
       if (at >= from && at < from + n) s.rows[at - from] = m;
     });
   } else {
-    if (t < n) s.rows[t] = order[start[s.g] + from + t];
+    if (t < n) s.rows[t] = order[start[g] + from + t];
   }
   __syncthreads();
   return n;
@@ -184,7 +202,7 @@ __device__ __forceinline__ int find_piece(Piece &s, const int *__restrict__ ids,
 
 // Two workgroups a compute unit: the few pieces past a whole round that short last
 // pieces make would cost a second one.
-template <int ELEM, int kBlocks, bool kFromIds>
+template <int ELEM, int kBlocks, int kHeld>
 __global__ __launch_bounds__(kNarrowThreads, 4) void narrow_kernel(Narrow n0, Narrow n1,
                                                       const float *__restrict__ alpha,
                                                       const int *__restrict__ ids,
@@ -201,9 +219,10 @@ __global__ __launch_bounds__(kNarrowThreads, 4) void narrow_kernel(Narrow n0, Na
   const int c = lane & 15, q = lane >> 4;
   const int lr = lane >> 3, lc = lane & 7;      // a load's row and chunk
   Piece &found = *(Piece *)lds;
-  const int count = find_piece<kFromIds>(found, ids, order, start, M, G, first + blockIdx.x);
+  int g;
+  const int count = find_piece<kHeld>(found, ids, order, start, M, G, first + blockIdx.x, g);
   if (count == 0) return;
-  const int g = __builtin_amdgcn_readfirstlane(found.g);
+  g = __builtin_amdgcn_readfirstlane(g);
   const int row = found.rows[c < count ? c : count - 1];
   __syncthreads();   // the search's LDS is free
   const unsigned char *x[2];
@@ -306,7 +325,7 @@ __global__ __launch_bounds__(kNarrowThreads, 4) void narrow_kernel(Narrow n0, Na
 constexpr int kGroupThreads = 1024, kGroupHeld = 8, kGroupTile = kGroupThreads * kGroupHeld;
 __device__ __forceinline__ void group_rows(const int *__restrict__ ids, int *__restrict__ start,
                                            int *__restrict__ order, int M, int G, int g) {
-  __shared__ int part[kGroupThreads / 64], tab[129];
+  __shared__ int part[kGroupThreads / 64], tab[128];
   const int lane = threadIdx.x & 63, w = threadIdx.x >> 6;
   int held[kGroupHeld];
   int below = 0;
@@ -325,6 +344,7 @@ __device__ __forceinline__ void group_rows(const int *__restrict__ ids, int *__r
   if (threadIdx.x == 0) start[g] = at;
   for (int64_t m0 = 0; m0 < M; m0 += kGroupTile) {
     if (M > kGroupTile) load_ids<kGroupThreads>(ids, (int)m0, M, G, held);   // else still there
+    if (m0 > 0) __syncthreads();   // reads of tab
     at += place_rows<kGroupThreads>(held, g, (int)m0, tab,
                                     [&](int place, int m) { order[at + place] = m; });
   }
@@ -851,14 +871,14 @@ hipError_t narrow(const Narrow &n0, const Narrow &n1, const float *alpha, const 
   const int rp = (int)rank_pad(r);
   // pieces: every adapter's last one may be short
   const int64_t most = (M + kPiece - 1) / kPiece + G - 1;
-  auto go = [&](auto blocks, auto from_ids) {
+  auto go = [&](auto blocks, auto held) {
     constexpr int kBlocks = decltype(blocks)::value;
     // a launch counts its work items in 32 bits
     constexpr int64_t kMost = 1 << 22;
     const int64_t pieces = most < M ? most : M;
     for (int64_t first = 0;
          first < pieces && (first == 0 || hipPeekAtLastError() == hipSuccess); first += kMost)
-      hipLaunchKernelGGL((narrow_kernel<ELEM, kBlocks, decltype(from_ids)::value>),
+      hipLaunchKernelGGL((narrow_kernel<ELEM, kBlocks, decltype(held)::value>),
                          dim3((unsigned)(pieces - first < kMost ? pieces - first : kMost),
                               n1.X ? 2 : 1, rp / (16 * kBlocks)),
                          dim3(kNarrowThreads), 0, stream, n0, n1, alpha, ids, order, start, (int)M,
@@ -866,9 +886,11 @@ hipError_t narrow(const Narrow &n0, const Narrow &n1, const float *alpha, const 
   };
   auto by_order = [&](auto blocks) {
     if (order)
-      go(blocks, std::false_type{});
+      go(blocks, std::integral_constant<int, 0>{});
+    else if (M <= 4 * kNarrowThreads)
+      go(blocks, std::integral_constant<int, 4>{});
     else
-      go(blocks, std::true_type{});
+      go(blocks, std::integral_constant<int, kScanHeld>{});
   };
   if (rp == 16)
     by_order(std::integral_constant<int, 1>{});
@@ -894,7 +916,7 @@ hipError_t prepare(const Transpose &t0, const Transpose &t1, const int32_t *ids,
 }
 
 // The narrow product's launch beside a product of few tiles.
-constexpr double kNarrowUs = 9;
+constexpr double kNarrowUs = 7.5;
 
 template <int ELEM, int DT, int OUT, bool kQ8>
 hipError_t project(const AdapterArgs &a, const Scratch &s, hipStream_t stream, int num_cus) {
