@@ -21,7 +21,7 @@ __host__ __device__ constexpr int64_t rank_pad(int64_t r) { return r <= 16 ? 16 
 
 // ---------------------------------------------------------------------------
 // T[m][j] = alpha[g] sum_k X[m][k] F_g[j][k] (F_g: r x K, rows contiguous), zeros
-// from rank r on to rank_pad.  A workgroup takes up to 16 rows of one
+// from rank r on to rank_pad.  A workgroup takes up to 16 kR rows of one
 // adapter, wherever they lie, and 16 or 32 ranks; its 8 waves take every eighth 64
 // elements of K, and their sums are added in their order.  A load instruction
 // fetches 8 whole lines of 128 bytes (X from memory once, F from the caches); a
@@ -30,13 +30,13 @@ __host__ __device__ constexpr int64_t rank_pad(int64_t r) { return r <= 16 ? 16 
 //
 // Which rows a workgroup takes it finds out by itself (kHeld > 0: up to kScanRows
 // rows and kScanAdapters adapters): it counts every adapter's rows, and with
-// them the pieces of 16 rows before its own, then places its adapter's
+// them the pieces before its own, then places its adapter's
 // rows.  Larger calls, and those that need the order elsewhere, read it off
 // group_kernel's.  (A launch of group_kernel takes 5 to 9 us of a call; taking
 // rows as they lie, a product for each adapter of a block, 60 us for 128 rows of
 // 16 adapters in turn.)
 // ---------------------------------------------------------------------------
-constexpr int kNarrowThreads = 512, kScanHeld = 16, kPiece = 16;
+constexpr int kNarrowThreads = 512, kScanHeld = 16;
 constexpr int64_t kScanRows = kNarrowThreads * kScanHeld, kScanAdapters = kNarrowThreads;
 
 struct Narrow {
@@ -117,9 +117,9 @@ __device__ __forceinline__ int place_rows(const int (&held)[kHeld], int g, int m
 // rows[]); returns how many there are, 0 if there is no such piece.  kHeld: every
 // lane looks through so many rows' numbers, 0: read off the order.
 struct Piece {
-  int bins[kScanAdapters], part[8], tab[kScanHeld * 8], rows[kPiece], g, chunk, n;
+  int bins[kScanAdapters], part[8], tab[kScanHeld * 8], rows[32], g, chunk, n;
 };
-template <int kHeld>
+template <int kHeld, int kPiece>
 __device__ __forceinline__ int find_piece(Piece &s, const int *__restrict__ ids,
                                           const int *__restrict__ order,
                                           const int *__restrict__ start, int M, int G, int piece,
@@ -202,7 +202,7 @@ __device__ __forceinline__ int find_piece(Piece &s, const int *__restrict__ ids,
 
 // Two workgroups a compute unit: the few pieces past a whole round that short last
 // pieces make would cost a second one.
-template <int ELEM, int kBlocks, int kHeld>
+template <int ELEM, int kBlocks, int kHeld, int kR>
 __global__ __launch_bounds__(kNarrowThreads, 4) void narrow_kernel(Narrow n0, Narrow n1,
                                                       const float *__restrict__ alpha,
                                                       const int *__restrict__ ids,
@@ -210,8 +210,8 @@ __global__ __launch_bounds__(kNarrowThreads, 4) void narrow_kernel(Narrow n0, Na
                                                       const int *__restrict__ start, int M, int r,
                                                       int rp, int G, int first) {
   constexpr int DT = ELEM == TCU_ELEM_F16 ? TCU_F16_F32 : TCU_BF16_F32;
-  constexpr int kWaves = kNarrowThreads / 64, kStep = 64, kPart = (1 + kBlocks) * 2048;
-  static_assert(kBlocks * 1024 <= kPart, "a wave's sums");
+  constexpr int kWaves = kNarrowThreads / 64, kStep = 64, kPart = (kR + kBlocks) * 2048;
+  static_assert(kBlocks * kR * 1024 <= kPart, "a wave's sums");
   static_assert(sizeof(Piece) <= kWaves * kPart, "the search");
   __shared__ __attribute__((aligned(128))) unsigned char lds[kWaves * kPart];
   const Narrow n = blockIdx.y == 0 ? n0 : n1;
@@ -220,15 +220,18 @@ __global__ __launch_bounds__(kNarrowThreads, 4) void narrow_kernel(Narrow n0, Na
   const int lr = lane >> 3, lc = lane & 7;      // a load's row and chunk
   Piece &found = *(Piece *)lds;
   int g;
-  const int count = find_piece<kHeld>(found, ids, order, start, M, G, first + blockIdx.x, g);
+  const int count =
+      find_piece<kHeld, 16 * kR>(found, ids, order, start, M, G, first + blockIdx.x, g);
   if (count == 0) return;
   g = __builtin_amdgcn_readfirstlane(g);
-  const int row = found.rows[c < count ? c : count - 1];
-  __syncthreads();   // the search's LDS is free
-  const unsigned char *x[2];
+  int row[kR];
+  const unsigned char *x[2 * kR];
 #pragma unroll
-  for (int h = 0; h < 2; ++h)
-    x[h] = n.X + 2 * ((int64_t)__shfl(row, 8 * h + lr) * n.ldx + 8 * lc);
+  for (int i = 0; i < kR; ++i) row[i] = found.rows[min(16 * i + c, count - 1)];
+#pragma unroll
+  for (int h = 0; h < 2 * kR; ++h)
+    x[h] = n.X + 2 * ((int64_t)found.rows[min(8 * h + lr, count - 1)] * n.ldx + 8 * lc);
+  __syncthreads();   // the search's LDS is free
   unsigned char *const mine_lds = lds + w * kPart;
   unsigned char *const put = mine_lds + lr * 128 + 16 * (lc ^ lr);
   const unsigned char *get[2];
@@ -238,7 +241,7 @@ __global__ __launch_bounds__(kNarrowThreads, 4) void narrow_kernel(Narrow n0, Na
   const float al = alpha[g];
   const int j0 = blockIdx.z * (16 * kBlocks);
   const unsigned char *f[kBlocks][2];
-  f32x4 acc[kBlocks];
+  f32x4 acc[kBlocks][kR];
 #pragma unroll
   for (int b = 0; b < kBlocks; ++b) {
 #pragma unroll
@@ -246,48 +249,54 @@ __global__ __launch_bounds__(kNarrowThreads, 4) void narrow_kernel(Narrow n0, Na
       const int j = j0 + 16 * b + 8 * h + lr;
       f[b][h] = fg + 2 * (int64_t)(j < r ? j : r - 1) * n.K;
     }
-    acc[b] = f32x4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+    for (int i = 0; i < kR; ++i) acc[b][i] = f32x4{0.f, 0.f, 0.f, 0.f};
   }
   struct Chunk {
-    u32x4 x[2], f[kBlocks][2];
+    u32x4 x[2 * kR], f[kBlocks][2];
   };
   auto load = [&](int k, Chunk &v) __attribute__((always_inline)) {
     if (k + kStep <= n.K) {
 #pragma unroll
-      for (int h = 0; h < 2; ++h) {
-        v.x[h] = load16_any(x[h] + 2 * k);
+      for (int h = 0; h < 2 * kR; ++h) v.x[h] = load16_any(x[h] + 2 * k);
+#pragma unroll
+      for (int h = 0; h < 2; ++h)
 #pragma unroll
         for (int b = 0; b < kBlocks; ++b) v.f[b][h] = load16_any(f[b][h] + 2 * k);
-      }
     } else {
       // zeros past K
       const int valid = n.K - k - 8 * lc;
 #pragma unroll
-      for (int h = 0; h < 2; ++h) {
-        v.x[h] = load8<ELEM>(x[h] + 2 * k, valid).v[0];
+      for (int h = 0; h < 2 * kR; ++h) v.x[h] = load8<ELEM>(x[h] + 2 * k, valid).v[0];
+#pragma unroll
+      for (int h = 0; h < 2; ++h)
 #pragma unroll
         for (int b = 0; b < kBlocks; ++b) v.f[b][h] = load8<ELEM>(f[b][h] + 2 * k, valid).v[0];
-      }
     }
   };
   auto multiply = [&](const Chunk &v) __attribute__((always_inline)) {
 #pragma unroll
-    for (int h = 0; h < 2; ++h) {
-      *(u32x4 *)(put + 1024 * h) = v.x[h];
+    for (int h = 0; h < 2 * kR; ++h) *(u32x4 *)(put + 1024 * h) = v.x[h];
+#pragma unroll
+    for (int h = 0; h < 2; ++h)
 #pragma unroll
       for (int b = 0; b < kBlocks; ++b)
-        *(u32x4 *)(put + 2048 * (1 + b) + 1024 * h) = v.f[b][h];
-    }
+        *(u32x4 *)(put + 2048 * (kR + b) + 1024 * h) = v.f[b][h];
 #pragma unroll
     for (int h = 0; h < 2; ++h) {
-      const u32x4 xf = *(const u32x4 *)get[h];
+      u32x4 xf[kR];
 #pragma unroll
-      for (int b = 0; b < kBlocks; ++b)
-        acc[b] = mfma_k32(DT, *(const u32x4 *)(get[h] + 2048 * (1 + b)), xf, acc[b]);
+      for (int i = 0; i < kR; ++i) xf[i] = *(const u32x4 *)(get[h] + 2048 * i);
+#pragma unroll
+      for (int b = 0; b < kBlocks; ++b) {
+        const u32x4 ff = *(const u32x4 *)(get[h] + 2048 * (kR + b));
+#pragma unroll
+        for (int i = 0; i < kR; ++i) acc[b][i] = mfma_k32(DT, ff, xf[i], acc[b][i]);
+      }
     }
   };
   // kAhead chunks in flight
-  constexpr int kAhead = kBlocks == 1 ? 4 : 2, kNext = kWaves * kStep;
+  constexpr int kAhead = kBlocks == 1 && kR == 1 ? 4 : 2, kNext = kWaves * kStep;
   Chunk v[kAhead];
   int k = w * kStep;
 #pragma unroll
@@ -303,17 +312,20 @@ __global__ __launch_bounds__(kNarrowThreads, 4) void narrow_kernel(Narrow n0, Na
     }
   }
 #pragma unroll
-  for (int b = 0; b < kBlocks; ++b) *(f32x4 *)(mine_lds + b * 1024 + 16 * lane) = acc[b];
+  for (int b = 0; b < kBlocks; ++b)
+#pragma unroll
+    for (int i = 0; i < kR; ++i)
+      *(f32x4 *)(mine_lds + (b * kR + i) * 1024 + 16 * lane) = acc[b][i];
   __syncthreads();
-  if (w < kBlocks) {
+  if (w < kBlocks * kR) {
     f32x4 v = *(const f32x4 *)(lds + w * 1024 + 16 * lane);
 #pragma unroll
     for (int u = 1; u < kWaves; ++u) v += *(const f32x4 *)(lds + u * kPart + w * 1024 + 16 * lane);
-    // ranks j .. j + 3 of row c
-    const int j = j0 + 16 * w + 4 * q;
+    // ranks j .. j + 3 of the piece's row `at`
+    const int i = w % kR, at = 16 * i + c, j = j0 + 16 * (w / kR) + 4 * q;
 #pragma unroll
     for (int e = 0; e < 4; ++e) v[e] = j + e < r ? v[e] * al : 0.f;
-    if (c < count) *(f32x4 *)(n.T + (int64_t)row * rp + j) = v;
+    if (at < count) *(f32x4 *)(n.T + (int64_t)row[kR == 2 && i == 1 ? kR - 1 : 0] * rp + j) = v;
   }
 }
 
@@ -657,8 +669,8 @@ __global__ __launch_bounds__(kGroupThreads) void prepare_kernel(Transpose t0, Tr
 
 // ---------------------------------------------------------------------------
 // D_g(j, c) = sum over g's rows of T[m][j] X[m][c], the rows in the order of
-// group_kernel cut into chunks.  A workgroup takes one chunk, 128 columns and
-// every gridDim.z'th adapter,
+// group_kernel cut into chunks.  A workgroup takes one chunk, 128 columns, 16 or 32
+// ranks and every `beside`th adapter,
 // its 4 waves every fourth group of 4 rows: binary32 matrix products over 4 rows,
 // a lane holding 8 columns of one of them (16 bytes), value e of the 16 lanes
 // being columns e, 8 + e, .. of product e.  An adapter whose rows lie in one
@@ -680,7 +692,8 @@ __global__ __launch_bounds__(256) void factor_kernel(Factor f0, Factor f1,
                                                      const int *__restrict__ order,
                                                      const int *__restrict__ start, int r, int rp,
                                                      int G, int chunk, int cols0) {
-  __shared__ f32x4 sums[4][8][64];
+  // (rows of 65: the reads below go across them)
+  __shared__ f32x4 sums[4][8][65];
   const bool second = (int)blockIdx.x >= cols0;
   const Factor f = second ? f1 : f0;
   const int c0 = ((int)blockIdx.x - (second ? cols0 : 0)) * kFactorCols;
@@ -690,15 +703,17 @@ __global__ __launch_bounds__(256) void factor_kernel(Factor f0, Factor f1,
   const int end = begin + chunk < count ? begin + chunk : count;
   const int col = c0 + 8 * c, valid = f.C - col;
   const int64_t rc = (int64_t)r * f.C;
-  // this workgroup's adapters with rows in the chunk: every gridDim.z'th
-  for (int g0 = blockIdx.z; g0 < G; g0 += 64 * gridDim.z) {
-    const int gl = g0 + lane * (int)gridDim.z;
+  // this workgroup's ranks, and its adapters with rows in the chunk: every beside'th
+  const int rank_blocks = rp / (16 * kBlocks), beside = gridDim.z / rank_blocks;
+  const int zg = blockIdx.z / rank_blocks, j0 = (blockIdx.z - zg * rank_blocks) * (16 * kBlocks);
+  for (int g0 = zg; g0 < G; g0 += 64 * beside) {
+    const int gl = g0 + lane * beside;
     const int b0 = gl < G ? start[gl] : 0, b1 = gl < G ? start[gl + 1] : 0;
     unsigned long long here = __ballot(b0 < b1 && b0 < end && b1 > begin);
     while (here != 0) {
       const int from = __builtin_ctzll(here);
       here &= here - 1;
-      const int g = g0 + from * (int)gridDim.z;
+      const int g = g0 + from * beside;
       const int s0 = __builtin_amdgcn_readlane(b0, from), s1 = __builtin_amdgcn_readlane(b1, from);
       const int at = s0 > begin ? s0 : begin, to = s1 < end ? s1 : end;
       float *out;
@@ -710,68 +725,67 @@ __global__ __launch_bounds__(256) void factor_kernel(Factor f0, Factor f1,
         dj = f.C;
         dc = 1;
       }
-      for (int j0 = 0; j0 < rp; j0 += 16 * kBlocks) {
-        f32x4 acc[kBlocks][8];
+      f32x4 acc[kBlocks][8];
 #pragma unroll
-        for (int b = 0; b < kBlocks; ++b)
+      for (int b = 0; b < kBlocks; ++b)
 #pragma unroll
-          for (int e = 0; e < 8; ++e) acc[b][e] = f32x4{0.f, 0.f, 0.f, 0.f};
-        // kU groups of 4 rows, their loads in flight together; past the run's end
-        // (not `whole`) zeros
-        constexpr int kU = 4;
-        auto rows = [&](int m0, auto whole) __attribute__((always_inline)) {
-          constexpr bool kWhole = decltype(whole)::value;
-          Raw8<ELEM> xr[kU];
-          float t[kU][kBlocks];
-          int m[kU];
+        for (int e = 0; e < 8; ++e) acc[b][e] = f32x4{0.f, 0.f, 0.f, 0.f};
+      // kU groups of 4 rows, their loads in flight together; past the run's end
+      // (not `whole`) zeros
+      constexpr int kU = 4;
+      auto rows = [&](int m0, auto whole) __attribute__((always_inline)) {
+        constexpr bool kWhole = decltype(whole)::value;
+        Raw8<ELEM> xr[kU];
+        float t[kU][kBlocks];
+        int m[kU];
 #pragma unroll
-          for (int u = 0; u < kU; ++u) {
-            const int i = m0 + 16 * u + q;
-            m[u] = order[kWhole || i < to ? i : to - 1];
-          }
+        for (int u = 0; u < kU; ++u) {
+          const int i = m0 + 16 * u + q;
+          m[u] = order[kWhole || i < to ? i : to - 1];
+        }
 #pragma unroll
-          for (int u = 0; u < kU; ++u) {
-            const bool in = kWhole || m0 + 16 * u + q < to;
-            xr[u] = load8<ELEM>(f.X + 2 * ((int64_t)m[u] * f.ldx + col),
-                                kWhole ? 8 : in ? valid : 0);
+        for (int u = 0; u < kU; ++u) {
+          const bool in = kWhole || m0 + 16 * u + q < to;
+          xr[u] = load8<ELEM>(f.X + 2 * ((int64_t)m[u] * f.ldx + col),
+                              kWhole ? 8 : in ? valid : 0);
 #pragma unroll
-            for (int b = 0; b < kBlocks; ++b)
-              t[u][b] = in ? f.T[(int64_t)m[u] * rp + j0 + 16 * b + c] : 0.f;
-          }
+          for (int b = 0; b < kBlocks; ++b)
+            t[u][b] = in ? f.T[(int64_t)m[u] * rp + j0 + 16 * b + c] : 0.f;
+        }
 #pragma unroll
-          for (int u = 0; u < kU; ++u) {
-            float x[8];
-            unpack8<ELEM>(xr[u], x);
+        for (int u = 0; u < kU; ++u) {
+          float x[8];
+          unpack8<ELEM>(xr[u], x);
 #pragma unroll
-            for (int b = 0; b < kBlocks; ++b)
+          for (int b = 0; b < kBlocks; ++b)
 #pragma unroll
-              for (int e = 0; e < 8; ++e)
-                acc[b][e] = __builtin_amdgcn_mfma_f32_16x16x4f32(t[u][b], x[e], acc[b][e], 0, 0, 0);
-          }
-        };
-        int m0 = at + 4 * w;
-        if (c0 + kFactorCols <= f.C)
-          for (; m0 + 16 * (kU - 1) + 4 <= to; m0 += 16 * kU) rows(m0, std::true_type{});
-        for (; m0 < to; m0 += 16 * kU) rows(m0, std::false_type{});
-        // the waves' sums, 16 ranks at a time: lane holds ranks 4 q .. of column 8 c + e
+            for (int e = 0; e < 8; ++e)
+              acc[b][e] = __builtin_amdgcn_mfma_f32_16x16x4f32(t[u][b], x[e], acc[b][e], 0, 0, 0);
+        }
+      };
+      int m0 = at + 4 * w;
+      if (c0 + kFactorCols <= f.C)
+        for (; m0 + 16 * (kU - 1) + 4 <= to; m0 += 16 * kU) rows(m0, std::true_type{});
+      for (; m0 < to; m0 += 16 * kU) rows(m0, std::false_type{});
+      // The waves' sums, 16 ranks at a time: a lane holds ranks 4 q .. of column
+      // 8 c + e, and stores ranks 4 w .. of one of 64 columns side by side.
 #pragma unroll
-        for (int b = 0; b < kBlocks; ++b) {
-          __syncthreads();
+      for (int b = 0; b < kBlocks; ++b) {
+        __syncthreads();
 #pragma unroll
-          for (int e = 0; e < 8; ++e) sums[w][e][lane] = acc[b][e];
-          __syncthreads();
+        for (int e = 0; e < 8; ++e) sums[w][e][lane] = acc[b][e];
+        __syncthreads();
 #pragma unroll
-          for (int h = 0; h < 2; ++h) {
-            const int e = 2 * w + h;
-            f32x4 v = sums[0][e][lane];
+        for (int h = 0; h < 2; ++h) {
+          const int e = lane & 7, at_c = 8 * h + (lane >> 3) + 16 * w;
+          f32x4 v = sums[0][e][at_c];
 #pragma unroll
-            for (int u = 1; u < 4; ++u) v += sums[u][e][lane];
-            const int cc = col + e, j = j0 + 16 * b + 4 * q;
-            if (cc < f.C) {
+          for (int u = 1; u < 4; ++u) v += sums[u][e][at_c];
+          const int cc = c0 + 64 * h + lane, j = j0 + 16 * b + 4 * w;
+          if (cc < f.C) {
 #pragma unroll
-              for (int k = 0; k < 4; ++k)
-                if (j + k < r) out[(j + k) * dj + cc * dc] = v[k];
-            }
+            for (int k = 0; k < 4; ++k)
+              if (j + k < r) out[(j + k) * dj + cc * dc] = v[k];
           }
         }
       }
@@ -810,13 +824,17 @@ __global__ __launch_bounds__(256) void finish_kernel(Factor f0, Factor f1,
   }
 }
 
-// Rows of a chunk: enough workgroups of 128 columns for the chip, and
-// parts that stay small beside what is read.
-int chunk_rows(int64_t M, int64_t K, int64_t N) {
+// Ranks of a workgroup of factor_kernel.
+constexpr int factor_ranks(int64_t rp) { return rp == 16 ? 16 : 32; }
+
+// Rows of a chunk: enough workgroups of 128 columns for the chip, and parts (2 r
+// rows of binary32 a chunk) that stay small beside what is read (4000 rows, K = N
+// = 2048, rank 64: XXCHUNK).
+int chunk_rows(int64_t M, int64_t K, int64_t N, int64_t r) {
   const int64_t strips = (K + kFactorCols - 1) / kFactorCols + (N + kFactorCols - 1) / kFactorCols;
-  int64_t rows = M * strips / 1024;
-  rows = (rows + 63) / 64 * 64;
-  return (int)(rows < 64 ? 64 : rows);
+  const int64_t rp = rank_pad(r), least = (4 * r + 63) / 64 * 64;
+  const int64_t rows = (M * strips * (rp / factor_ranks(rp)) / 1024 + 63) / 64 * 64;
+  return (int)(rows < least ? least : rows);
 }
 
 // Scratch: T of X and of dY, the rows in their adapters' order, the adapters
@@ -842,7 +860,7 @@ Scratch scratch(void *work, int64_t M, int64_t K, int64_t N, int64_t r, int64_t 
   s.order = (int *)take(M * 4);
   s.at = take(G * r * K * 2);
   s.bt = take(G * r * N * 2);
-  const int64_t chunk = chunk_rows(M, K, N), chunks = (M + chunk - 1) / chunk;
+  const int64_t chunk = chunk_rows(M, K, N, r), chunks = (M + chunk - 1) / chunk;
   // padded ranks and the gradients' parts are not of the same call
   const int64_t pad = round256(G * (N > K ? N : K) * rank_pad(r) * 2);
   const int64_t pa = round256(2 * chunks * r * K * 4), pb = round256(2 * chunks * r * N * 4);
@@ -863,39 +881,53 @@ hipError_t group(const int32_t *ids, const Scratch &s, int64_t M, int64_t G, hip
   return hipGetLastError();
 }
 
+constexpr int64_t kWidePieces = 512;
+
 // T of one product, or of two (n1.X not null); order null: found by the kernel.
 template <int ELEM>
 hipError_t narrow(const Narrow &n0, const Narrow &n1, const float *alpha, const int32_t *ids,
                   const int *order, const int *start, int64_t M, int64_t r, int64_t G,
                   hipStream_t stream) {
   const int rp = (int)rank_pad(r);
-  // pieces: every adapter's last one may be short
-  const int64_t most = (M + kPiece - 1) / kPiece + G - 1;
-  auto go = [&](auto blocks, auto held) {
-    constexpr int kBlocks = decltype(blocks)::value;
+  auto go = [&](auto blocks, auto held, auto rows) {
+    constexpr int kBlocks = decltype(blocks)::value, kR = decltype(rows)::value;
+    // pieces: every adapter's last one may be short
+    const int64_t most = (M + 16 * kR - 1) / (16 * kR) + G - 1;
     // a launch counts its work items in 32 bits
     constexpr int64_t kMost = 1 << 22;
     const int64_t pieces = most < M ? most : M;
     for (int64_t first = 0;
          first < pieces && (first == 0 || hipPeekAtLastError() == hipSuccess); first += kMost)
-      hipLaunchKernelGGL((narrow_kernel<ELEM, kBlocks, decltype(held)::value>),
+      hipLaunchKernelGGL((narrow_kernel<ELEM, kBlocks, decltype(held)::value, kR>),
                          dim3((unsigned)(pieces - first < kMost ? pieces - first : kMost),
                               n1.X ? 2 : 1, rp / (16 * kBlocks)),
                          dim3(kNarrowThreads), 0, stream, n0, n1, alpha, ids, order, start, (int)M,
                          (int)r, rp, (int)G, (int)first);
   };
+  typedef std::integral_constant<int, 1> One;
+  typedef std::integral_constant<int, 2> Two;
+  // Pieces of 32 rows read F half as often; of 16 rows they are more, for the chip
+  // to be full and an adapter's last one to waste less.
+  const int64_t all = (M / 16 + G) * (n1.X ? 2 : 1) * (rp > 32 ? rp / 32 : 1);
+  const bool wide = all > kWidePieces && n0.K >= 64;
+  auto by_rows = [&](auto blocks, auto held) {
+    if (wide)
+      go(blocks, held, Two{});
+    else
+      go(blocks, held, One{});
+  };
   auto by_order = [&](auto blocks) {
     if (order)
-      go(blocks, std::integral_constant<int, 0>{});
+      by_rows(blocks, std::integral_constant<int, 0>{});
     else if (M <= 4 * kNarrowThreads)
-      go(blocks, std::integral_constant<int, 4>{});
+      by_rows(blocks, std::integral_constant<int, 4>{});
     else
-      go(blocks, std::integral_constant<int, kScanHeld>{});
+      by_rows(blocks, std::integral_constant<int, kScanHeld>{});
   };
   if (rp == 16)
-    by_order(std::integral_constant<int, 1>{});
+    by_order(One{});
   else
-    by_order(std::integral_constant<int, 2>{});
+    by_order(Two{});
   return hipGetLastError();
 }
 
@@ -993,7 +1025,7 @@ hipError_t grad_go(const AdapterGradArgs &a, hipStream_t stream) {
                          a.M > 0 ? a.ids : (const int32_t *)s.order, s, a.M, a.G, stream);
   if (e != hipSuccess) return e;
   const unsigned char *X = (const unsigned char *)a.X, *dY = (const unsigned char *)a.dY;
-  const int chunk = chunk_rows(a.M, a.K, a.N);
+  const int chunk = chunk_rows(a.M, a.K, a.N, a.r);
   const Factor fa{X, s.dt, a.dA, s.parts_a, a.ldx, a.K, 1, (int)a.K};
   const Factor fb{dY, s.t, a.dB, s.parts_b, a.lddy, 1, a.r, (int)a.N};
   if (a.M > 0) {
@@ -1005,7 +1037,8 @@ hipError_t grad_go(const AdapterGradArgs &a, hipStream_t stream) {
     const int cb = (int)((a.N + kFactorCols - 1) / kFactorCols);
     // a chunk's adapters side by side, about as many workgroups as it has adapters
     const int64_t chunks = (a.M + chunk - 1) / chunk, beside = a.G / chunks + 1;
-    const dim3 grid(ca + cb, (unsigned)chunks, (unsigned)(beside < 16 ? beside : 16));
+    const int rank_blocks = rp / factor_ranks(rp);
+    const dim3 grid(ca + cb, (unsigned)chunks, (unsigned)(beside < 16 ? beside : 16) * rank_blocks);
     if (rp == 16)
       hipLaunchKernelGGL((factor_kernel<ELEM, 1>), grid, dim3(256), 0, stream, fa, fb,
                          s.order, s.start, (int)a.r, rp, (int)a.G, chunk, ca);
