@@ -681,7 +681,7 @@ __global__ __launch_bounds__(kGroupThreads) void prepare_kernel(Transpose t0, Tr
 struct Factor {
   const unsigned char *X;
   const float *T;
-  float *D, *parts;      // parts: chunk, first or last, r, C
+  float *D, *parts;      // parts: chunk, first or last, then as one of D
   int64_t ldx, dj, dc;   // D_g(j, c) at D + g r C + j dj + c dc
   int C;
 };
@@ -692,8 +692,8 @@ __global__ __launch_bounds__(256) void factor_kernel(Factor f0, Factor f1,
                                                      const int *__restrict__ order,
                                                      const int *__restrict__ start, int r, int rp,
                                                      int G, int chunk, int cols0) {
-  // (rows of 65: the reads below go across them)
-  __shared__ f32x4 sums[4][8][65];
+  // (a lane's place c + 17 q: the reads below go across the lanes)
+  __shared__ f32x4 sums[4][8][68];
   const bool second = (int)blockIdx.x >= cols0;
   const Factor f = second ? f1 : f0;
   const int c0 = ((int)blockIdx.x - (second ? cols0 : 0)) * kFactorCols;
@@ -716,15 +716,9 @@ __global__ __launch_bounds__(256) void factor_kernel(Factor f0, Factor f1,
       const int g = g0 + from * beside;
       const int s0 = __builtin_amdgcn_readlane(b0, from), s1 = __builtin_amdgcn_readlane(b1, from);
       const int at = s0 > begin ? s0 : begin, to = s1 < end ? s1 : end;
-      float *out;
-      int64_t dj = f.dj, dc = f.dc;
-      if (s0 >= begin && s1 <= end) {
-        out = f.D + g * rc;
-      } else {
-        out = f.parts + (2 * (int64_t)blockIdx.y + (s0 >= begin)) * rc;
-        dj = f.C;
-        dc = 1;
-      }
+      float *const out = s0 >= begin && s1 <= end
+                             ? f.D + g * rc
+                             : f.parts + (2 * (int64_t)blockIdx.y + (s0 >= begin)) * rc;
       f32x4 acc[kBlocks][8];
 #pragma unroll
       for (int b = 0; b < kBlocks; ++b)
@@ -768,24 +762,33 @@ __global__ __launch_bounds__(256) void factor_kernel(Factor f0, Factor f1,
         for (; m0 + 16 * (kU - 1) + 4 <= to; m0 += 16 * kU) rows(m0, std::true_type{});
       for (; m0 < to; m0 += 16 * kU) rows(m0, std::false_type{});
       // The waves' sums, 16 ranks at a time: a lane holds ranks 4 q .. of column
-      // 8 c + e, and stores ranks 4 w .. of one of 64 columns side by side.
+      // 8 c + e, and stores four ranks of a column, its neighbours what lies beside
+      // them: the next columns (dc = 1) or the column's other ranks (dj = 1; with
+      // the ranks a stride apart 300 rows of 20 adapters, K = N = 2048, rank 64 took
+      // 34.7 us, 19.7 so).
 #pragma unroll
       for (int b = 0; b < kBlocks; ++b) {
         __syncthreads();
 #pragma unroll
-        for (int e = 0; e < 8; ++e) sums[w][e][lane] = acc[b][e];
+        for (int e = 0; e < 8; ++e) sums[w][e][c + 17 * q] = acc[b][e];
         __syncthreads();
 #pragma unroll
         for (int h = 0; h < 2; ++h) {
-          const int e = lane & 7, at_c = 8 * h + (lane >> 3) + 16 * w;
-          f32x4 v = sums[0][e][at_c];
+          const int at = threadIdx.x + 256 * h;
+          const int x = f.dc == 1 ? 64 * h + lane : at >> 2, p = f.dc == 1 ? w : at & 3;
+          const int from = (x >> 3) + 17 * p;
+          f32x4 v = sums[0][x & 7][from];
 #pragma unroll
-          for (int u = 1; u < 4; ++u) v += sums[u][e][at_c];
-          const int cc = c0 + 64 * h + lane, j = j0 + 16 * b + 4 * w;
-          if (cc < f.C) {
+          for (int u = 1; u < 4; ++u) v += sums[u][x & 7][from];
+          const int cc = c0 + x, j = j0 + 16 * b + 4 * p;
+          if (cc >= f.C) continue;
+          float *const o = out + j * f.dj + cc * f.dc;
+          if (f.dj == 1 && (r & 3) == 0) {
+            if (j < r) *(f32x4 *)o = v;
+          } else {
 #pragma unroll
             for (int k = 0; k < 4; ++k)
-              if (j + k < r) out[(j + k) * dj + cc * dc] = v[k];
+              if (j + k < r) o[k * f.dj] = v[k];
           }
         }
       }
@@ -794,34 +797,43 @@ __global__ __launch_bounds__(256) void factor_kernel(Factor f0, Factor f1,
 }
 
 // Adapters without rows: zeros.  Adapters whose rows lie in several chunks: the
-// sum of their parts.
+// sum of their parts, V (one value or four) at a time.
+template <typename V>
+__device__ __forceinline__ void finish(const Factor &f, const int *__restrict__ start, int64_t rc,
+                                       int G, int chunk) {
+  for (int g = blockIdx.z; g < G; g += gridDim.z) {
+    const int s0 = start[g], s1 = start[g + 1];
+    const int first = s0 / chunk, last = s1 > s0 ? (s1 - 1) / chunk : first;
+    if (s1 > s0 && first == last) continue;
+    const int64_t n = rc * 4 / (int64_t)sizeof(V);
+    V *const D = (V *)(f.D + g * rc);
+    for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < n;
+         i += (int64_t)gridDim.x * 256) {
+      V v = V{};
+      if (s1 > s0) {
+        const V *p = (const V *)(f.parts + 2 * (int64_t)first * rc) + i;
+        v = p[n];
+        p += 2 * n;
+        int k = first + 1;
+        for (; k + 4 <= last + 1; k += 4, p += 8 * n) {
+          const V u0 = p[0], u1 = p[2 * n], u2 = p[4 * n], u3 = p[6 * n];
+          v = v + u0 + u1 + u2 + u3;
+        }
+        for (; k <= last; ++k, p += 2 * n) v += p[0];
+      }
+      D[i] = v;
+    }
+  }
+}
 __global__ __launch_bounds__(256) void finish_kernel(Factor f0, Factor f1,
                                                      const int *__restrict__ start, int r, int G,
                                                      int chunk) {
   const Factor f = blockIdx.y == 0 ? f0 : f1;
   const int64_t rc = (int64_t)r * f.C;
-  for (int g = blockIdx.z; g < G; g += gridDim.z) {
-    const int s0 = start[g], s1 = start[g + 1];
-    const int first = s0 / chunk, last = s1 > s0 ? (s1 - 1) / chunk : first;
-    if (s1 > s0 && first == last) continue;
-    for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < rc;
-         i += (int64_t)gridDim.x * 256) {
-      float v = 0.f;
-      if (s1 > s0) {
-        const float *p = f.parts + 2 * (int64_t)first * rc + i;
-        v = p[rc];
-        p += 2 * rc;
-        int k = first + 1;
-        for (; k + 4 <= last + 1; k += 4, p += 8 * rc) {
-          const float u0 = p[0], u1 = p[2 * rc], u2 = p[4 * rc], u3 = p[6 * rc];
-          v = v + u0 + u1 + u2 + u3;
-        }
-        for (; k <= last; ++k, p += 2 * rc) v += p[0];
-      }
-      const int64_t j = i / f.C, c = i - j * f.C;
-      f.D[g * rc + j * f.dj + c * f.dc] = v;
-    }
-  }
+  if ((rc & 3) == 0)
+    finish<f32x4>(f, start, rc, G, chunk);
+  else
+    finish<float>(f, start, rc, G, chunk);
 }
 
 // Ranks of a workgroup of factor_kernel.
@@ -829,7 +841,7 @@ constexpr int factor_ranks(int64_t rp) { return rp == 16 ? 16 : 32; }
 
 // Rows of a chunk: enough workgroups of 128 columns for the chip, and parts (2 r
 // rows of binary32 a chunk) that stay small beside what is read (4000 rows, K = N
-// = 2048, rank 64: XXCHUNK).
+// = 2048, rank 64: factors and join 52 + 14 us with 128 rows, 39 + 13 with 256).
 int chunk_rows(int64_t M, int64_t K, int64_t N, int64_t r) {
   const int64_t strips = (K + kFactorCols - 1) / kFactorCols + (N + kFactorCols - 1) / kFactorCols;
   const int64_t rp = rank_pad(r), least = (4 * r + 63) / 64 * 64;
@@ -1048,8 +1060,8 @@ hipError_t grad_go(const AdapterGradArgs &a, hipStream_t stream) {
     e = hipGetLastError();
     if (e != hipSuccess) return e;
   }
-  const int64_t most = a.r * (a.K > a.N ? a.K : a.N);
-  hipLaunchKernelGGL(finish_kernel, dim3(most < 512 * 256 ? (unsigned)((most + 255) / 256) : 512, 2,
+  const int64_t most = (a.r * (a.K > a.N ? a.K : a.N) + 1023) / 1024;
+  hipLaunchKernelGGL(finish_kernel, dim3((unsigned)(most < 512 ? most : 512), 2,
                                          (unsigned)(a.G < 1024 ? a.G : 1024)),
                      dim3(256), 0, stream, fa, fb, s.start, (int)a.r, (int)a.G, chunk);
   return hipGetLastError();
