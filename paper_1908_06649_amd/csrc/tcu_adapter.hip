@@ -919,7 +919,10 @@ hipError_t narrow(const Narrow &n0, const Narrow &n1, const float *alpha, const 
   typedef std::integral_constant<int, 1> One;
   typedef std::integral_constant<int, 2> Two;
   // Pieces of 32 rows read F half as often; of 16 rows they are more, for the chip
-  // to be full and an adapter's last one to waste less.
+  // to be full and an adapter's last one to waste less (us of a call, 16 / 32 rows: 6000 x
+  // 1000 x 300 rank 64 40.6 / 32.5, 8192 x 8192 x 8192 rank 32 872 / 867, 8000 x
+  // 256 x 256 rank 16 25.0 / 23.7; below 512 pieces 4000 x 5000 x 512 rank 32
+  // 60.4 / 63.0).
   const int64_t all = (M / 16 + G) * (n1.X ? 2 : 1) * (rp > 32 ? rp / 32 : 1);
   const bool wide = all > kWidePieces && n0.K >= 64;
   auto by_rows = [&](auto blocks, auto held) {
