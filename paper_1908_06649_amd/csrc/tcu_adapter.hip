@@ -610,15 +610,18 @@ __global__ __launch_bounds__(256) void pad_ranks_kernel(const unsigned short *__
 }
 
 // out (cols x rows) of every adapter = in (rows x cols), 16-bit values, in `tiles`
-// tiles of 4096: 32 along the shorter side, the rank's, 128 along the other.
+// tiles of 4096: 32 along the shorter side, the rank's, 128 along the other, or 16
+// and 256 where the shorter one has no more (27 adapters of 5966 x 16: gradients and
+// input's gradient 69.4 us, 75.2 with the wider tile half empty).
 struct Transpose {
   const unsigned short *in;
   unsigned short *out;
   int64_t rows, cols, tiles;
 };
 __host__ __device__ constexpr int64_t tiles_of(int64_t rows, int64_t cols) {
-  return rows < cols ? (rows + 31) / 32 * ((cols + 127) / 128)
-                     : (rows + 127) / 128 * ((cols + 31) / 32);
+  return rows < cols ? rows <= 16 ? (cols + 255) / 256 : (rows + 31) / 32 * ((cols + 127) / 128)
+         : cols <= 16 ? (rows + 255) / 256
+                      : (rows + 127) / 128 * ((cols + 31) / 32);
 }
 template <int kR, int kC>
 __device__ __forceinline__ void transpose_tiles(const Transpose &a, int64_t t, int64_t step,
@@ -653,7 +656,7 @@ __global__ __launch_bounds__(kGroupThreads) void prepare_kernel(Transpose t0, Tr
                                                                 int *__restrict__ start,
                                                                 int *__restrict__ order, int M,
                                                                 int G) {
-  __shared__ unsigned short tile[128 * 34];
+  __shared__ unsigned short tile[256 * 18];   // the largest of the four
   const int groups = order ? G : 0;
   if ((int)blockIdx.x < groups) {
     group_rows(ids, start, order, M, G, blockIdx.x);
@@ -661,10 +664,16 @@ __global__ __launch_bounds__(kGroupThreads) void prepare_kernel(Transpose t0, Tr
   }
   const int64_t t = (int)blockIdx.x - groups, step = (int)gridDim.x - groups;
   auto transpose = [&](const Transpose &a) {
-    if (a.rows < a.cols)
-      transpose_tiles<32, 128>(a, t, step, tile);
-    else
+    if (a.rows < a.cols) {
+      if (a.rows <= 16)
+        transpose_tiles<16, 256>(a, t, step, tile);
+      else
+        transpose_tiles<32, 128>(a, t, step, tile);
+    } else if (a.cols <= 16) {
+      transpose_tiles<256, 16>(a, t, step, tile);
+    } else {
       transpose_tiles<128, 32>(a, t, step, tile);
+    }
   };
   transpose(t0);
   transpose(t1);
@@ -1053,9 +1062,13 @@ hipError_t grad_go(const AdapterGradArgs &a, hipStream_t stream) {
     if (e != hipSuccess) return e;
     const int ca = (int)((a.K + kFactorCols - 1) / kFactorCols);
     const int cb = (int)((a.N + kFactorCols - 1) / kFactorCols);
-    // a chunk's adapters side by side, about as many workgroups as it has adapters
-    const int64_t chunks = (a.M + chunk - 1) / chunk, beside = a.G / chunks + 1;
+    // a chunk's adapters side by side, about as many workgroups as it has adapters, and
+    // up to one for each while the chip has room (645 rows of 4, K = 192, N = 1408, rank
+    // 32, with the input's gradient: 44.3 us, 48.7 with one)
     const int rank_blocks = rp / factor_ranks(rp);
+    const int64_t chunks = (a.M + chunk - 1) / chunk, one = (ca + cb) * chunks * rank_blocks;
+    int64_t beside = a.G / chunks + 1;
+    if (beside * one < 512) beside = 512 / one < a.G ? 512 / one : a.G;
     const dim3 grid(ca + cb, (unsigned)chunks, (unsigned)(beside < 16 ? beside : 16) * rank_blocks);
     if (rp == 16)
       hipLaunchKernelGGL((factor_kernel<ELEM, 1>), grid, dim3(256), 0, stream, fa, fb,
