@@ -471,6 +471,7 @@ TCU_MAX_RANK = 128
 
 _ELEMS = {}
 _BF16 = _F32 = _I32 = _I8 = None
+_NO_DEVICE = -2     # before the first tensor
 
 
 def _elem_code(where: str, dtype) -> int:
@@ -492,30 +493,28 @@ def _addresses(where: str, views, vectors, work, nbytes: int):
     contiguous, all on the current HIP device, and work holds nbytes.  A tensor
     may be None where the call allows it.  Returns the device index and the
     addresses (None for absent tensors), work's last."""
-    dev, ptrs = -1, []
+    dev, ptrs = _NO_DEVICE, []
     for t, dtype, rows, cols, ld in views:
         if t is None:
             ptrs.append(None)
             continue
         d = t.get_device()
-        if dev < 0:
-            dev = d
-        if t.dtype != dtype or t.shape != (rows, cols) or d != dev or t.stride() != (ld, 1):
-            _check_view(where, t, dtype, rows, cols, ld, dev)
+        if d != dev:
+            dev = _first_device(where, dev, d)
+        if t.dtype != dtype or t.shape != (rows, cols) or t.stride() != (ld, 1):
+            _check_view(where, t, dtype, rows, cols, ld)
         ptrs.append(t.data_ptr() or None)
     for t, dtype, n in vectors:
         if t is None:
             ptrs.append(None)
             continue
         d = t.get_device()
-        if dev < 0:
-            dev = d
+        if d != dev:
+            dev = _first_device(where, dev, d)
         if t.dtype != dtype:
             raise ValueError(f"{where}: expected {dtype}, got {t.dtype}")
         if t.numel() != n or not t.is_contiguous():
             raise ValueError(f"{where}: expected {n} contiguous elements, got {tuple(t.shape)}")
-        if d != dev:
-            raise ValueError(f"{where}: all tensors must be on the same HIP device")
         ptrs.append(t.data_ptr() or None)
     if work is not None:
         if nbytes < 0:
@@ -531,7 +530,14 @@ def _addresses(where: str, views, vectors, work, nbytes: int):
     return dev, ptrs
 
 
-def _check_view(where, t, dtype, rows, cols, ld, dev):
+def _first_device(where, dev, d):
+    """d, the first tensor's device; a host tensor's is -1, also of the first."""
+    if dev != _NO_DEVICE or d < 0:
+        raise ValueError(f"{where}: all tensors must be on the same HIP device")
+    return d
+
+
+def _check_view(where, t, dtype, rows, cols, ld):
     """The general checks of a view (a pitch counts only between rows)."""
     if t.dtype != dtype:
         raise ValueError(f"{where}: expected {dtype}, got {t.dtype}")
@@ -540,8 +546,6 @@ def _check_view(where, t, dtype, rows, cols, ld, dev):
     st = t.stride()
     if rows and cols and ((st[1] != 1 and cols > 1) or (st[0] != ld and rows > 1)):
         raise ValueError(f"{where}: strides {st} do not match rows of pitch {ld}")
-    if t.get_device() != dev:
-        raise ValueError(f"{where}: all tensors must be on the same HIP device")
 
 
 def _stream_of(dev: int, stream_ptr):
