@@ -854,11 +854,13 @@ constexpr int factor_ranks(int64_t rp) { return rp == 16 ? 16 : 32; }
 // Rows of a chunk: enough workgroups of 128 columns for the chip, and parts (2 r
 // rows of binary32 a chunk) that stay small beside what is read (4000 rows, K = N
 // = 2048, rank 64: factors and join 52 + 14 us with 128 rows, 39 + 13 with 256).
+// All rows at most, so that it fits the kernels' int.
 int chunk_rows(int64_t M, int64_t K, int64_t N, int64_t r) {
   const int64_t strips = (K + kFactorCols - 1) / kFactorCols + (N + kFactorCols - 1) / kFactorCols;
   const int64_t rp = rank_pad(r), least = (4 * r + 63) / 64 * 64;
   const int64_t rows = (M * strips * (rp / factor_ranks(rp)) / 1024 + 63) / 64 * 64;
-  return (int)(rows < least ? least : rows);
+  const int64_t all = M < least ? least : M;
+  return (int)(rows < least ? least : rows < all ? rows : all);
 }
 
 // Scratch: T of X and of dY, the rows in their adapters' order, the adapters

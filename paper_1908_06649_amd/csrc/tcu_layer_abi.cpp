@@ -86,11 +86,13 @@ Operand vec(const void *p, int64_t n, int64_t es, int align, bool out = false) {
 
 int64_t blocks(int64_t n, int64_t s) { return (n + s - 1) / s; }
 
-// Whether sizes are in range, G * r * max(K, N) 16-bit values among them.
+// Whether sizes are in range: the operands of M rows, a byte a value at least,
+// and G * r * max(K, N) 16-bit values among them.
 int check_sizes(int64_t M, int64_t K, int64_t N, int64_t r, int64_t G) {
-  if (!dim_ok(M) || K < 0 || N < 0 || K > TCU_MAX_ADAPTED_DIM || N > TCU_MAX_ADAPTED_DIM || G < 0 || G > TCU_MAX_ADAPTERS || r < 1 ||
-      r > TCU_MAX_RANK)
+  if (!dim_ok(M) || K < 0 || N < 0 || K > TCU_MAX_ADAPTED_DIM || N > TCU_MAX_ADAPTED_DIM ||
+      G < 0 || G > TCU_MAX_ADAPTERS || r < 1 || r > TCU_MAX_RANK)
     return TCU_ERR_SHAPE;
+  if (M * std::max(K, N) >= kMaxExtent) return TCU_ERR_SHAPE;
   if (G * r * std::max(K, N) >= kMaxExtent / 4) return TCU_ERR_SHAPE;
   return adapter_work_bytes(M, K, N, r, G) < kMaxExtent ? TCU_OK : TCU_ERR_SHAPE;
 }

@@ -1,0 +1,53 @@
+"""The operators around a layer's products at the ends of their documented sizes, in
+a process of their own on the recording runtime (tests/recording.py)."""
+import shutil
+
+import pytest
+
+from paper_1908_06649_amd import tcu
+
+import recording as rec
+
+pytestmark = pytest.mark.skipif(shutil.which("g++") is None, reason="needs g++")
+P = rec.ptr
+ROWS = 1 << 30      # TCU_MAX_RECT_DIM
+DIM = 1 << 24       # TCU_MAX_ADAPTED_DIM
+
+
+@pytest.fixture(scope="module")
+def so(tmp_path_factory):
+    return rec.build(tmp_path_factory.mktemp("recording"))
+
+
+# every size within its own limit; the row operands of the first four pass 2^40 bytes, the
+# last one's work does (T of both sides: 2 x 2^30 x 128 binary32 values)
+SIZES = [(ROWS, 1 << 18, 1 << 18, 16, 4), (ROWS, DIM, DIM, 16, 0), (ROWS, DIM, 1, 16, 4),
+         (ROWS, 1, DIM, 128, 65536), (ROWS, 512, 512, 128, 4)]
+WITHIN = [(ROWS, 1, 1, 1, 1), (1, DIM, DIM, 16, 4), (1, DIM, DIM, 1, 0), (65535, DIM, DIM, 16, 1)]
+
+
+def test_work_of_extreme_sizes(so):
+    answers = rec.run(so, [dict(fn="tcu_adapter_work", args=list(s)) for s in SIZES + WITHIN])
+    got = [a["rc"] for a in answers]
+    assert got[:len(SIZES)] == [-1] * len(SIZES)
+    for size, n in zip(WITHIN, got[len(SIZES):]):
+        M, K, N, r, G = size
+        # T of both sides and the rows' order at least
+        assert M * r * 8 + M * 4 <= n < 1 << 40, size
+
+
+@pytest.mark.parametrize("size", SIZES)
+def test_calls_of_extreme_sizes_are_refused(so, size):
+    M, K, N, r, G = size
+    tail = [M, K, N, r, G]
+    jobs = [
+        dict(fn="tcu_adapter_gemm", args=[P(0), K, P(1), N, P(2), P(3), P(4), P(5), P(6), N, P(7),
+                                          *tail, 2, None]),
+        dict(fn="tcu_adapter_gemm_q8", args=[P(0), K, P(4), P(1), N, P(4), P(2), K, P(3), P(3),
+                                             P(4), P(5), P(6), N, P(7), *tail, None]),
+        dict(fn="tcu_adapter_grad", args=[P(0), K, P(1), N, P(2), P(2), P(4), P(5), P(6), P(3),
+                                          P(7), *tail, 2, None]),
+        dict(fn="tcu_adapter_input_grad", args=[P(0), N, P(1), K, P(2), P(3), P(4), P(5), P(6), K,
+                                                P(7), *tail, 2, None])]
+    for answer in rec.run(so, jobs):
+        assert answer["rc"] == tcu.TCU_ERR_SHAPE and answer["launches"] == []
