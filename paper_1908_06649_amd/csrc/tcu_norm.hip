@@ -420,31 +420,34 @@ __global__ __launch_bounds__(1024) void rms_norm_grad_long_kernel(NormGradArgs a
   }
 }
 
-// dw = the sum of `parts` rows of partial sums: a workgroup takes 32 columns,
-// its 32 half waves every 32nd part, four loads in flight.
+// dw = the sum of `parts` rows of partial sums: a workgroup takes every gridDim.x'th
+// 32 columns, its 32 half waves every 32nd part, four loads in flight.
 __global__ __launch_bounds__(1024) void norm_dw_kernel(const float *__restrict__ work,
                                                        float *__restrict__ dw, int parts,
                                                        int64_t cols) {
   __shared__ float lds[32][33];
   const int c = threadIdx.x & 31, h = threadIdx.x >> 5;
-  const int64_t col = (int64_t)blockIdx.x * 32 + c;
-  float v = 0.f;
-  if (col < cols) {
-    int p = h;
-    for (; p + 96 < parts; p += 128) {
-      const float *at = work + p * cols + col;
-      const float u0 = at[0], u1 = at[32 * cols], u2 = at[64 * cols], u3 = at[96 * cols];
-      v = v + u0 + u1 + u2 + u3;
+  for (int64_t col0 = (int64_t)blockIdx.x * 32; col0 < cols; col0 += (int64_t)gridDim.x * 32) {
+    const int64_t col = col0 + c;
+    float v = 0.f;
+    if (col < cols) {
+      int p = h;
+      for (; p + 96 < parts; p += 128) {
+        const float *at = work + p * cols + col;
+        const float u0 = at[0], u1 = at[32 * cols], u2 = at[64 * cols], u3 = at[96 * cols];
+        v = v + u0 + u1 + u2 + u3;
+      }
+      for (; p < parts; p += 32) v += work[p * cols + col];
     }
-    for (; p < parts; p += 32) v += work[p * cols + col];
-  }
-  lds[h][c] = v;
-  __syncthreads();
-  if (h == 0 && col < cols) {
-    v = 0.f;
+    lds[h][c] = v;
+    __syncthreads();
+    if (h == 0 && col < cols) {
+      v = 0.f;
 #pragma unroll
-    for (int i = 0; i < 32; ++i) v += lds[i][c];
-    dw[col] = v;
+      for (int i = 0; i < 32; ++i) v += lds[i][c];
+      dw[col] = v;
+    }
+    __syncthreads();   // read before the next columns overwrite
   }
 }
 
@@ -520,7 +523,7 @@ hipError_t grad_go(const NormGradArgs &a, hipStream_t stream) {
     const hipError_t e = hipGetLastError();
     if (e != hipSuccess) return e;
   }
-  hipLaunchKernelGGL(norm_dw_kernel, dim3((unsigned)((a.cols + 31) / 32)), dim3(1024), 0, stream,
+  hipLaunchKernelGGL(norm_dw_kernel, dim3(grid_for((a.cols + 31) / 32)), dim3(1024), 0, stream,
                      a.work, a.dw, parts, a.cols);
   return hipGetLastError();
 }

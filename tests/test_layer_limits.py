@@ -51,3 +51,17 @@ def test_calls_of_extreme_sizes_are_refused(so, size):
                                                 P(7), *tail, 2, None])]
     for answer in rec.run(so, jobs):
         assert answer["rc"] == tcu.TCU_ERR_SHAPE and answer["launches"] == []
+
+
+@pytest.mark.parametrize("rows", [0, 1, 600])
+@pytest.mark.parametrize("cols", [(1 << 27) - 32, 1 << 27, (1 << 27) + 1, 1 << 30])
+def test_norm_gradient_of_long_rows(so, rows, cols):
+    """Work items of a launch count in 32 bits."""
+    if rows * cols >= 1 << 38:     # (their bytes would pass 2^40)
+        rows = 200
+    args = [P(0), cols, P(1), cols, P(2), P(3), cols, P(4), cols, P(5), P(6), rows, cols, 1e-5, 2,
+            None]
+    answer = rec.run(so, [dict(fn="tcu_rms_norm_grad", args=args)])[0]
+    assert answer["rc"] == tcu.TCU_OK
+    assert len(answer["launches"]) == (2 if rows else 1)
+    assert all(0 < la["blocks"] * la["threads"] < 1 << 32 for la in answer["launches"])
