@@ -2,7 +2,9 @@
 // output, and its gradient (tcu_rms_norm, tcu_rms_norm_grad).
 //
 //   h = x + res,  y = h rstd w,  rstd = 1 / sqrt(mean(h^2) + eps)
-//   dx = rstd (g - h rstd^2 mean(g h)) + dh,  g = dy w;   dw = sum_rows dy h rstd
+//   dx = rstd (g - n mean(g n)) + dh,  g = dy w,  n = h rstd;   dw = sum_rows dy n
+//
+// (rstd^2 is never formed: without an eps it leaves binary32 where rstd does not.)
 //
 // Both are bound by memory: a row is read once, kept in registers while its
 // sums are formed, and written once (8192 x 8192 bf16 with a residual: 104 us,
@@ -326,7 +328,7 @@ __global__ __launch_bounds__(kT < 256 ? 256 : kT) void rms_norm_grad_kernel(Norm
     ss = row_sum<kT>(ss, lds);
     gh = row_sum<kT>(gh, lds + (kT > 64 ? 8 : 0));
     const float rstd = rstd_of(ss, a.cols, a.eps);
-    const float c = rstd * rstd * (gh / (float)a.cols);
+    const float c = rstd * (gh / (float)a.cols);   // mean(g n)
 #pragma unroll
     for (int i = 0; i < kV; ++i) {
       const Window n = window<kT, kV>(t, i, (int)a.cols);
@@ -338,8 +340,9 @@ __global__ __launch_bounds__(kT < 256 ? 256 : kT) void rms_norm_grad_kernel(Norm
       unpack8<ELEM>(dh[i], r);
 #pragma unroll
       for (int e = 0; e < 8; ++e) {
-        dw[i][e] += d[e] * (x[e] * rstd);
-        r[e] += rstd * (d[e] * f[e] - x[e] * c);
+        const float hn = x[e] * rstd;
+        dw[i][e] += d[e] * hn;
+        r[e] += rstd * (d[e] * f[e] - hn * c);
       }
       store8<ELEM>((unsigned char *)a.dx + (row * a.lddx + n.col) * ES, r, 8);
     }
@@ -398,7 +401,7 @@ __global__ __launch_bounds__(1024) void rms_norm_grad_long_kernel(NormGradArgs a
     ss = row_sum<kT>(ss, lds);
     gh = row_sum<kT>(gh, lds + 16);
     const float rstd = rstd_of(ss, a.cols, a.eps);
-    const float c = rstd * rstd * (gh / (float)a.cols);
+    const float c = rstd * (gh / (float)a.cols);   // mean(g n)
     const bool first = row == blockIdx.x;
     for (int64_t col = 8 * threadIdx.x; col < a.cols; col += 8 * kT) {
       const int valid = (int)(a.cols - col < 8 ? a.cols - col : 8);
@@ -411,8 +414,9 @@ __global__ __launch_bounds__(1024) void rms_norm_grad_long_kernel(NormGradArgs a
         unpack8<TCU_ELEM_F32>(load8<TCU_ELEM_F32>((unsigned char *)(part + col), valid), s);
 #pragma unroll
       for (int e = 0; e < 8; ++e) {
-        s[e] += d[e] * (x[e] * rstd);
-        r[e] += rstd * (d[e] * f[e] - x[e] * c);
+        const float hn = x[e] * rstd;
+        s[e] += d[e] * hn;
+        r[e] += rstd * (d[e] * f[e] - hn * c);
       }
       store8<TCU_ELEM_F32>((unsigned char *)(part + col), s, valid);
       store8<ELEM>((unsigned char *)a.dx + (row * a.lddx + col) * ES, r, valid);

@@ -2,7 +2,7 @@
 import pytest
 import torch
 
-from layer_util import DEV, F32
+from layer_util import DEV, F32, ROUND, gen, norm64, norm_grad64, randn, within
 from paper_1908_06649_amd import tcu
 
 pytestmark = pytest.mark.gpu
@@ -34,3 +34,35 @@ def test_gradient_of_columns_past_a_launch():
         want += term
         size += term.abs()
     assert bool(((dw.double() - want).abs() <= size * (rel + 4 * F32)).all())
+
+
+def sum_bound(cols):
+    """Relative error of a binary32 sum of squares and what follows it: a lane adds
+    at most 64 terms of a row (of its 8192 vectors' worth), then trees."""
+    return (64 + cols / 1024 + 16) * F32
+
+
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
+@pytest.mark.parametrize("cols", [5, 600, 1020, 3001, 9000, 17000])
+def test_small_rows_without_eps(dtype, cols):
+    """eps = 0 and values near 2^-66: rstd is 2^66, its square not in binary32's range."""
+    g = gen(cols)
+    x, dy, dh = (randn((4, cols), dtype, g) for _ in range(3))
+    w = randn((cols,), dtype, g)
+    x[1:3] *= 2.0 ** -66
+    y, dx = (torch.empty(4, cols, dtype=dtype, device=DEV) for _ in range(2))
+    tcu.tcu_rms_norm(x.to(DEV), cols, None, 0, w.to(DEV), None, 0, y, cols, None, 0, None, 4, cols,
+                     0.0)
+    dw = torch.empty(cols, device=DEV)
+    work = torch.empty(tcu.tcu_rms_norm_grad_work(4, cols), dtype=torch.uint8, device=DEV)
+    tcu.tcu_rms_norm_grad(dy.to(DEV), cols, x.to(DEV), cols, w.to(DEV), dh.to(DEV), cols, dx, cols,
+                          dw, work, 4, cols, 0.0)
+    # The squares near 2^-132 are multiples of 2^-149, and so is their mean: each off by
+    # 2^-150, rstd by half of twice that over the mean, which is above 2^-135 here.
+    low = 2.0 ** -15
+    h64, y64 = norm64(x, None, w, 0.0)
+    assert float(h64.pow(2).mean(1).min()) > 2.0 ** -135
+    within(y, y64, y64.abs() * (ROUND[dtype] + sum_bound(cols) + low))
+    x64, w64, xm, wm = norm_grad64(dy, x, w, dh, 0.0)
+    within(dx, x64, x64.abs() * ROUND[dtype] + xm * (2 * sum_bound(cols) + 3 * low))
+    within(dw, w64, wm * (sum_bound(cols) + 64 * F32 + low))
