@@ -372,8 +372,9 @@ typedef enum tcu_elem {
  * written; qscale (rows binary32 values) goes with q.  h may be exactly x or
  * exactly res (same base and pitch): the residual is then added in place.
  * A row of zeros has y = 0, q = 0 and qscale = 0 (and a gradient dx = dh),
- * also for eps = 0: there every row whose squares' mean is 0 in binary32.  A row with a value that is
- * not finite has qscale = NaN and q = 0; no other row is affected.
+ * also for eps = 0: there every row whose squares' mean is 0 in binary32.  A row
+ * with a value of h or y that is not finite has qscale = NaN and q = 0; no other
+ * row is affected.
  *   0 <= rows <= TCU_MAX_RECT_DIM; 1 <= cols <= TCU_MAX_RECT_DIM (rows = 0: no-op);
  *   eps >= 0, finite; elem: a tcu_elem, of x, res, w, h and y.
  * Errors: TCU_ERR_NULL, TCU_ERR_SHAPE (also eps), TCU_ERR_UNSUPPORTED (elem),

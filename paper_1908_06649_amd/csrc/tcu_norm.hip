@@ -22,7 +22,7 @@ namespace {
 constexpr int kWaveCols = 1024, kBlockCols = 16384;
 // Up to so many rows, fewer than the chip has compute units, a row is 16 waves'.
 constexpr int kFewNormRows = 256;
-constexpr unsigned kInfBits = 0x7f800000u;
+constexpr unsigned kInfBits = 0x7f800000u, kNormalBits = 0x00800000u;
 
 // Sum and unsigned maximum over the kT threads of a row (64: a wave, else the
 // workgroup, through LDS).
@@ -56,19 +56,31 @@ __device__ __forceinline__ unsigned row_max(unsigned v, float *lds) {
   return v;
 }
 
-// What the 8-bit output of a row needs: the largest |h w| as bits, which order
-// like the values, NaN above infinity.
+// The larger of m and |v| as bits, which order like the values, NaN above infinity.
+__device__ __forceinline__ unsigned max_bits(unsigned m, float v) {
+  const unsigned b = bitcast<unsigned>(v) & 0x7fffffffu;
+  return b > m ? b : m;
+}
+
+// A row's largest |y| is its largest |h w| times rstd, unless h w has left binary32's
+// normal range, which y need not have (or is not finite): then it is looked for among
+// the |h rstd w|.
+__device__ __forceinline__ bool is_normal(unsigned bits) {
+  return bits >= kNormalBits && bits < kInfBits;
+}
+
+// What the 8-bit output of a row needs, from the bits of its largest |y|.
 struct Quant {
   float pre, inv, scale;   // q = rint(y * pre * inv)
 };
-__device__ __forceinline__ Quant quant_of(unsigned max_hw, float rstd) {
-  const float amax = __builtin_bit_cast(float, max_hw) * rstd;
+__device__ __forceinline__ Quant quant_of(unsigned max_y) {
+  const float amax = bitcast<float>(max_y);
   Quant k;
   // 127 / amax stays finite down to the smallest maxima
   k.pre = amax < 0x1p-96f ? 0x1p96f : 1.f;
   k.scale = amax / 127.f;
   k.inv = amax > 0.f ? 127.f / (amax * k.pre) : 0.f;
-  if (max_hw >= kInfBits) {
+  if (max_y >= kInfBits) {
     k.scale = __builtin_nanf("");
     k.inv = 0.f;
   }
@@ -188,18 +200,32 @@ __global__ __launch_bounds__(kT < 256 ? 256 : kT) void rms_norm_kernel(NormArgs 
     const float rstd = rstd_of(row_sum<kT>(ss, lds), a.cols, a.eps);
     Quant k{};
     if (a.q) {
-      unsigned m = 0u;
+      // Once over h w, and again over h rstd w where those do not do.  One body for both,
+      // kept by hiding from the compiler which it is: the registers of a second one made
+      // 8192 x 8192 with a residual and three outputs take 132 us, not 124.
+      unsigned m;
+      int pass = 0;
+      while (true) {
+        asm volatile("" : "+v"(pass));
+        const bool scaled = __builtin_amdgcn_readfirstlane(pass) != 0;
+        const float r = scaled ? rstd : 1.f;
+        m = 0u;
 #pragma unroll
-      for (int i = 0; i < kV; ++i) {
-        float f[8];
-        unpack8<ELEM>(w[i], f);
+        for (int i = 0; i < kV; ++i) {
+          float f[8];
+          unpack8<ELEM>(w[i], f);
 #pragma unroll
-        for (int e = 0; e < 8; ++e) {
-          const unsigned b = __builtin_bit_cast(unsigned, h[i][e] * f[e]) & 0x7fffffffu;
-          m = b > m ? b : m;
+          for (int e = 0; e < 8; ++e) m = max_bits(m, h[i][e] * r * f[e]);
         }
+        m = __builtin_amdgcn_readfirstlane(row_max<kT>(m, lds));
+        if (scaled) break;
+        if (is_normal(m)) {
+          m = bitcast<unsigned>(bitcast<float>(m) * rstd);
+          break;
+        }
+        pass = 1;
       }
-      k = quant_of(row_max<kT>(m, lds), rstd);
+      k = quant_of(m);
       if (t == 0) a.qscale[row] = k.scale;
     }
 #pragma unroll
@@ -213,7 +239,8 @@ __global__ __launch_bounds__(kT < 256 ? 256 : kT) void rms_norm_kernel(NormArgs 
   }
 }
 
-// Rows of any length: read once for the sums, once more for the outputs.
+// Rows of any length: read once for the sums, once more for the outputs (and between
+// them for an 8-bit output's scale where h w has left binary32's range).
 template <int ELEM>
 __global__ __launch_bounds__(1024) void rms_norm_long_kernel(NormArgs a) {
   constexpr int ES = elem_bytes<ELEM>, kT = 1024;
@@ -232,16 +259,27 @@ __global__ __launch_bounds__(1024) void rms_norm_long_kernel(NormArgs a) {
 #pragma unroll
       for (int e = 0; e < 8; ++e) {
         ss += h[e] * h[e];
-        if (a.q) {
-          const unsigned b = __builtin_bit_cast(unsigned, h[e] * f[e]) & 0x7fffffffu;
-          m = b > m ? b : m;
-        }
+        if (a.q) m = max_bits(m, h[e] * f[e]);
       }
     }
     const float rstd = rstd_of(row_sum<kT>(ss, lds), a.cols, a.eps);
     Quant k{};
     if (a.q) {
-      k = quant_of(row_max<kT>(m, lds), rstd);
+      m = row_max<kT>(m, lds);
+      if (is_normal(m)) {
+        m = bitcast<unsigned>(bitcast<float>(m) * rstd);
+      } else {
+        m = 0u;
+        for (int64_t col = 8 * threadIdx.x; col < a.cols; col += 8 * kT) {
+          const int valid = (int)(a.cols - col < 8 ? a.cols - col : 8);
+          load_h<ELEM>(x + col * ES, res ? res + col * ES : nullptr, valid, h);
+          unpack8<ELEM>(load8<ELEM>(w + col * ES, valid), f);
+#pragma unroll
+          for (int e = 0; e < 8; ++e) m = max_bits(m, h[e] * rstd * f[e]);
+        }
+        m = row_max<kT>(m, lds);
+      }
+      k = quant_of(m);
       if (threadIdx.x == 0) a.qscale[row] = k.scale;
     }
     for (int64_t col = 8 * threadIdx.x; col < a.cols; col += 8 * kT) {

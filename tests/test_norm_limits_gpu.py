@@ -66,3 +66,46 @@ def test_small_rows_without_eps(dtype, cols):
     x64, w64, xm, wm = norm_grad64(dy, x, w, dh, 0.0)
     within(dx, x64, x64.abs() * ROUND[dtype] + xm * (2 * sum_bound(cols) + 3 * low))
     within(dw, w64, wm * (sum_bound(cols) + 64 * F32 + low))
+
+
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
+@pytest.mark.parametrize("cols", [5, 600, 1020, 3001, 9000, 17000])
+@pytest.mark.parametrize("size,weight,eps", [(1e13, 1e27, 1e-5), (1e-20, 1e-22, 1e-38)])
+def test_eight_bits_where_products_of_h_and_w_leave_the_range(dtype, cols, size, weight, eps):
+    """h w near 1e40 or 1e-42, beyond binary32, and y near 1e27 or 1e-23, inside."""
+    g = gen(cols)
+    x, w = randn((4, cols), dtype, g, size), randn((cols,), dtype, g, weight)
+    y = torch.empty(4, cols, dtype=dtype, device=DEV)
+    q, s = torch.empty(4, cols, dtype=torch.int8, device=DEV), torch.empty(4, device=DEV)
+    tcu.tcu_rms_norm(x.to(DEV), cols, None, 0, w.to(DEV), None, 0, y, cols, q, cols, s, 4, cols,
+                     eps)
+    _, y64 = norm64(x, None, w, eps)
+    # squares near 1e-40 are off by 2^-150 each, of a mean whose eps is 1e-38 > 2^-127; eps is
+    # rounded to a multiple of 2^-149 too
+    rel = sum_bound(cols) + 2.0 ** -21
+    within(y, y64, y64.abs() * (ROUND[dtype] + rel))
+    top = y64.abs().amax(1)
+    within(s, top / 127, top / 127 * rel)
+    off = (q.cpu().double() * (top / 127)[:, None] - y64).abs()
+    assert float((off - (0.5 + 127 * 4 * rel) * (top / 127)[:, None]).max()) <= 0
+    assert bool((q.abs().amax(1) == 127).all())
+
+
+@pytest.mark.parametrize("cols", [5, 600, 3001, 17000])
+def test_eight_bits_of_a_row_that_overflows(cols):
+    """Finite h and w, y beyond binary32: the row has no scale, the others have theirs."""
+    g = gen(cols)
+    x, w = randn((3, cols), torch.float32, g), randn((cols,), torch.float32, g)
+    x[1] = 0
+    x[1, 2] = cols            # the norm brings it to sqrt(cols)
+    w[2] = 3e38
+    x[0, 2] = x[2, 2] = 1e-4
+    q, s = torch.empty(3, cols, dtype=torch.int8, device=DEV), torch.empty(3, device=DEV)
+    tcu.tcu_rms_norm(x.to(DEV), cols, None, 0, w.to(DEV), None, 0, None, 0, q, cols, s, 3, cols,
+                     1e-5)
+    assert bool(torch.isnan(s[1])) and bool((q[1] == 0).all())
+    for row in (0, 2):
+        _, y64 = norm64(x[row:row + 1], None, w, 1e-5)
+        top = y64.abs().amax(1)
+        within(s[row:row + 1], top / 127, top / 127 * sum_bound(cols))
+        assert int(q[row, 2]) == 127
