@@ -473,7 +473,7 @@ struct AdapterTail {
     }
     if (any == 0) return;
     static_assert(FM % 2 == 0, "blocks in pairs");
-    // binary16: 2^e brings the row's largest |T| to [2^14, 2^15)
+    // binary16: 2^e brings the row's largest finite |T| to [2^14, 2^15)
     int ex[FM];
     if constexpr (ELEM == TCU_ELEM_F16) {
 #pragma unroll
@@ -486,7 +486,7 @@ struct AdapterTail {
 #pragma unroll
             for (int i = 0; i < 4; ++i) {
               const unsigned b = v[i] & 0x7fffffffu;
-              top = b > top ? b : top;
+              top = b > top && b < 0x7f800000u ? b : top;
             }
           }
 #pragma unroll
@@ -494,9 +494,7 @@ struct AdapterTail {
           const unsigned o = __shfl_xor(top, s);
           top = o > top ? o : top;
         }
-        ex[fm] = top == 0u || top >= 0x7f800000u
-                     ? 0
-                     : __builtin_amdgcn_frexp_expf(bitcast<float>(top)) - 15;
+        ex[fm] = top == 0u ? 0 : __builtin_amdgcn_frexp_expf(bitcast<float>(top)) - 15;
       }
     }
     const bool narrow = rp == 16;
