@@ -461,7 +461,8 @@ int tcu_adapter_input_grad(const void *dY, int64_t lddy, const void *Wt, int64_t
                            const void *A, const void *B, const float *alpha, const int32_t *ids,
                            void *dX, int64_t lddx, void *work, int64_t M, int64_t K, int64_t N,
                            int64_t r, int64_t G, int dtype, void *hip_stream);
-/* Bytes of work that any of the four takes (-1: a size out of range). */
+/* Bytes of work that any of the four takes (-1: a size out of range), of M rows or
+ * of fewer. */
 int64_t tcu_adapter_work(int64_t M, int64_t K, int64_t N, int64_t r, int64_t G);
 
 /* Clipping of gradients by their common norm:

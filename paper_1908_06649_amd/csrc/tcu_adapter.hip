@@ -853,16 +853,28 @@ constexpr int factor_ranks(int64_t rp) { return rp == 16 ? 16 : 32; }
 // rows of binary32 a chunk) that stay small beside what is read (4000 rows, K = N
 // = 2048, rank 64: factors and join 52 + 14 us with 128 rows, 39 + 13 with 256).
 // All rows at most, so that it fits the kernels' int.
-int chunk_rows(int64_t M, int64_t K, int64_t N, int64_t r) {
+int64_t factor_groups(int64_t K, int64_t N, int64_t r) {
   const int64_t strips = (K + kFactorCols - 1) / kFactorCols + (N + kFactorCols - 1) / kFactorCols;
-  const int64_t rp = rank_pad(r), least = (4 * r + 63) / 64 * 64;
-  const int64_t rows = (M * strips * (rp / factor_ranks(rp)) / 1024 + 63) / 64 * 64;
+  return strips * (rank_pad(r) / factor_ranks(rank_pad(r)));
+}
+int64_t least_chunk(int64_t r) { return (4 * r + 63) / 64 * 64; }
+int chunk_rows(int64_t M, int64_t K, int64_t N, int64_t r) {
+  const int64_t least = least_chunk(r);
+  const int64_t rows = (M * factor_groups(K, N, r) / 1024 + 63) / 64 * 64;
   const int64_t all = M < least ? least : M;
   return (int)(rows < least ? least : rows < all ? rows : all);
 }
+// Chunks of M rows or fewer at most: a chunk has `least` rows, and 64 / 65 of a 1024th
+// of the rows' share (rounded down before it is rounded up).
+int64_t most_chunks(int64_t M, int64_t K, int64_t N, int64_t r) {
+  const int64_t groups = factor_groups(K, N, r);
+  const int64_t a = M / least_chunk(r), b = groups > 0 ? 1040 / groups : 0;
+  return (a < b ? a : b) + 1;
+}
 
 // Scratch: T of X and of dY, the rows in their adapters' order, the adapters
-// transposed or with padded ranks, the parts of the factors' gradients.
+// transposed or with padded ranks, the parts of the factors' gradients.  No smaller
+// than that of fewer rows: a program keeps one for its largest batch.
 struct Scratch {
   unsigned char *at, *bt, *padded;
   float *t, *dt, *parts_a, *parts_b;
@@ -884,7 +896,7 @@ Scratch scratch(void *work, int64_t M, int64_t K, int64_t N, int64_t r, int64_t 
   s.order = (int *)take(M * 4);
   s.at = take(G * r * K * 2);
   s.bt = take(G * r * N * 2);
-  const int64_t chunk = chunk_rows(M, K, N, r), chunks = (M + chunk - 1) / chunk;
+  const int64_t chunks = most_chunks(M, K, N, r);
   // padded ranks and the gradients' parts are not of the same call
   const int64_t pad = round256(G * (N > K ? N : K) * rank_pad(r) * 2);
   const int64_t pa = round256(2 * chunks * r * K * 4), pb = round256(2 * chunks * r * N * 4);

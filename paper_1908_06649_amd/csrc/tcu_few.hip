@@ -456,10 +456,15 @@ double few_us(const AdapterArgs &a, bool q8) {
   return 6 + blocks * (double)a.K * (double)a.N * (q8 ? 1 : 2) / 3.2e6;
 }
 
+// Of M rows and of fewer, whatever ranges they are cut into: at most 16, at most the
+// steps there are, and few_splits' workgroups hold 2^20 (8 bits: 2^21) sums beside
+// half a range's.
 int64_t few_work_bytes(int64_t M, int64_t K, int64_t N, int64_t r) {
-  if (M > kFewRows) return 0;
-  const int64_t a = parts_bytes(M, K, N, false), b = parts_bytes(M, K, N, true);
-  return (a > b ? a : b) + M * r * 4;
+  const int64_t m = M < kFewRows ? M : kFewRows;
+  const int64_t steps = (K + 32 * kWaves - 1) / (32 * kWaves);
+  const int64_t ranges = steps < 1 ? 1 : steps > 16 ? 16 : steps;
+  const int64_t cut = ranges * m * N, full = ((int64_t)1 << 21) + m * N;
+  return ((cut < full ? cut : full) * 4 + 255) / 256 * 256 + m * r * 4;
 }
 
 hipError_t launch_few(int dtype, const AdapterArgs &a, float *T, int tld, hipStream_t stream) {

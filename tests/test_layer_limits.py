@@ -1,5 +1,6 @@
 """The operators around a layer's products at the ends of their documented sizes, in
 a process of their own on the recording runtime (tests/recording.py)."""
+import random
 import shutil
 
 import pytest
@@ -65,3 +66,19 @@ def test_norm_gradient_of_long_rows(so, rows, cols):
     assert answer["rc"] == tcu.TCU_OK
     assert len(answer["launches"]) == (2 if rows else 1)
     assert all(0 < la["blocks"] * la["threads"] < 1 << 32 for la in answer["launches"])
+
+
+def test_work_of_more_rows_is_enough_for_fewer(so):
+    """A program keeps the scratch of its largest batch."""
+    rng = random.Random(3)
+    jobs = []
+    for _ in range(3000):
+        K, N = (int(2 ** rng.uniform(0, 17)) for _ in range(2))
+        rest = [K, N, rng.choice([1, 4, 8, 16, 20, 32, 64, 128]), int(2 ** rng.uniform(0, 8)) - 1]
+        M = int(2 ** rng.uniform(0, 14))
+        jobs += [dict(fn="tcu_adapter_work", args=[m, *rest]) for m in (rng.randint(0, M), M)]
+    for M in range(1, 512):
+        jobs += [dict(fn="tcu_adapter_work", args=[m, 4096, 4096, 16, 4]) for m in (M, 512)]
+    got = [a["rc"] for a in rec.run(so, jobs)]
+    for fewer, more, job in zip(got[::2], got[1::2], jobs[1::2]):
+        assert 0 <= fewer <= more, job
