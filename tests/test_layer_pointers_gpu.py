@@ -1,0 +1,101 @@
+"""The layer operators with pointer checks on (TCU_KNOB_CHECK_POINTERS), through the C
+ABI: every operand in turn on the host is TCU_ERR_POINTER before any launch, outputs
+untouched and nothing counted; valid calls run."""
+import ctypes
+
+import numpy as np
+import pytest
+import torch
+
+from paper_1908_06649_amd import tcu
+
+pytestmark = pytest.mark.gpu
+DEV = "cuda"
+M, K, N, R, G = 40, 64, 96, 16, 3
+BF16, F32, I32, I8 = torch.bfloat16, torch.float32, torch.int32, torch.int8
+
+
+def operand(shape, dtype):
+    return torch.zeros(shape, dtype=dtype, device=DEV)
+
+
+FACTORS = {"A": ((G, R, K), BF16), "B": ((G, N, R), BF16), "alpha": ((G,), F32), "ids": ((M,), I32)}
+WORK = ((1 << 22,), torch.uint8)
+
+# name -> (operands, arguments from their addresses)
+CALLS = {
+    "tcu_rms_norm": (
+        dict(x=((M, K), BF16), res=((M, K), BF16), w=((K,), BF16), h=((M, K), BF16),
+             y=((M, K), BF16), q=((M, K), I8), scale=((M,), F32)),
+        lambda p: (p["x"], K, p["res"], K, p["w"], p["h"], K, p["y"], K, p["q"], K, p["scale"], M,
+                   K, 1e-5, 2, None)),
+    "tcu_rms_norm_grad": (
+        dict(dy=((M, K), BF16), h=((M, K), BF16), w=((K,), BF16), dh=((M, K), BF16),
+             dx=((M, K), BF16), dw=((K,), F32), work=WORK),
+        lambda p: (p["dy"], K, p["h"], K, p["w"], p["dh"], K, p["dx"], K, p["dw"], p["work"], M, K,
+                   1e-5, 2, None)),
+    "tcu_adapter_gemm": (
+        dict(X=((M, K), BF16), W=((K, N), BF16), **FACTORS, Y=((M, N), F32), work=WORK),
+        lambda p: (p["X"], K, p["W"], N, p["A"], p["B"], p["alpha"], p["ids"], p["Y"], N, p["work"],
+                   M, K, N, R, G, tcu.TCU_BF16_F32, None)),
+    "tcu_adapter_gemm_q8": (
+        dict(Xq=((M, K), I8), xscale=((M,), F32), Wq=((K, N), I8), wscale=((N,), F32),
+             X=((M, K), BF16), **FACTORS, Y=((M, N), BF16), work=WORK),
+        lambda p: (p["Xq"], K, p["xscale"], p["Wq"], N, p["wscale"], p["X"], K, p["A"], p["B"],
+                   p["alpha"], p["ids"], p["Y"], N, p["work"], M, K, N, R, G, None)),
+    "tcu_adapter_grad": (
+        dict(X=((M, K), BF16), dY=((M, N), BF16), **FACTORS, dA=((G, R, K), F32),
+             dB=((G, N, R), F32), work=WORK),
+        lambda p: (p["X"], K, p["dY"], N, p["A"], p["B"], p["alpha"], p["ids"], p["dA"], p["dB"],
+                   p["work"], M, K, N, R, G, 2, None)),
+    "tcu_adapter_input_grad": (
+        dict(dY=((M, N), BF16), Wt=((N, K), BF16), **FACTORS, dX=((M, K), BF16), work=WORK),
+        lambda p: (p["dY"], N, p["Wt"], K, p["A"], p["B"], p["alpha"], p["ids"], p["dX"], K,
+                   p["work"], M, K, N, R, G, tcu.TCU_BF16_BF16, None)),
+    "tcu_clip_grads": (
+        dict(g0=((500,), F32), g1=((300,), BF16), out0=((500,), F32), out1=((300,), BF16),
+             result=((2,), F32), work=WORK),
+        lambda p: ((ctypes.c_void_p * 2)(p["g0"], p["g1"]), (ctypes.c_void_p * 2)(p["out0"], p["out1"]),
+                   (ctypes.c_int64 * 2)(500, 300), (ctypes.c_int32 * 2)(0, 2), 2, 1.0, p["result"],
+                   p["work"], None)),
+}
+
+
+@pytest.mark.parametrize("name", CALLS)
+def test_host_operands_are_refused(name, knobs):
+    knobs(tcu.TCU_KNOB_CHECK_POINTERS, 1)
+    L = tcu.lib()
+    host = np.zeros(1 << 22, dtype=np.uint8)
+    hp = host.ctypes.data
+    assert hp % 16 == 0 and L.tcu_check_device_range(hp, 1024) == tcu.TCU_ERR_POINTER
+    shapes, args = CALLS[name]
+    tensors = {k: operand(*v) for k, v in shapes.items()}
+    addresses = {k: t.data_ptr() for k, t in tensors.items()}
+    for t in tensors.values():
+        t.fill_(1)
+    assert all(L.tcu_check_device_range(addresses[k], t.numel() * t.element_size()) == tcu.TCU_OK
+               for k, t in tensors.items())
+    tcu.tcu_reset_calls()
+    for k in tensors:
+        assert getattr(L, name)(*args({**addresses, k: hp})) == tcu.TCU_ERR_POINTER, k
+    torch.cuda.synchronize()
+    assert tcu.tcu_calls() == 0 and not host.any()
+    assert all(bool((t == 1).all()) for t in tensors.values())
+    assert getattr(L, name)(*args(addresses)) == tcu.TCU_OK
+    torch.cuda.synchronize()
+    if "adapter" in name:
+        assert tcu.tcu_calls() > 0
+
+
+def test_calls_allocate_nothing():
+    """Device memory in use is the same before and after each call."""
+    for name, (shapes, args) in CALLS.items():
+        tensors = {k: operand(*v) for k, v in shapes.items()}
+        call = args({k: t.data_ptr() for k, t in tensors.items()})
+        assert getattr(tcu.lib(), name)(*call) == tcu.TCU_OK
+        torch.cuda.synchronize()
+        free = torch.cuda.mem_get_info()[0]
+        for _ in range(3):
+            assert getattr(tcu.lib(), name)(*call) == tcu.TCU_OK
+        torch.cuda.synchronize()
+        assert torch.cuda.mem_get_info()[0] == free, name
