@@ -374,7 +374,8 @@ typedef enum tcu_elem {
  * A row of zeros has y = 0, q = 0 and qscale = 0 (and a gradient dx = dh),
  * also for eps = 0: there every row whose squares' mean is 0 in binary32.  A row
  * with a value of h or y that is not finite has qscale = NaN and q = 0; no other
- * row is affected.
+ * row is affected.  A finite row whose squares' sum passes binary32's range
+ * (values near 2^64) is taken as one of infinite norm: y = 0.
  *   0 <= rows <= TCU_MAX_RECT_DIM; 1 <= cols <= TCU_MAX_RECT_DIM (rows = 0: no-op);
  *   eps >= 0, finite; elem: a tcu_elem, of x, res, w, h and y.
  * Errors: TCU_ERR_NULL, TCU_ERR_SHAPE (also eps), TCU_ERR_UNSUPPORTED (elem),
@@ -405,9 +406,11 @@ int64_t tcu_rms_norm_grad_work(int64_t rows, int64_t cols);
  *   Y: M x N, pitch ldy, overwritten.
  * The rows of an adapter may lie in any order.  No row's result depends on
  * another row or on an adapter it does not name, also where those hold values
- * that are not finite.  X A^T is summed in binary32 and enters the second
- * product with at least 16 significant bits where Y is bfloat16 and 22
- * otherwise; the sum of both parts is formed in binary32 and rounded once.
+ * that are not finite.  (Beside an infinity of B_g the row's result may be NaN
+ * where the formula's is infinite: X A^T enters as a sum.)  X A^T is summed in
+ * binary32 and enters the second product with at least 16 significant bits where
+ * Y is bfloat16 and 22 otherwise; the sum of both parts is formed in binary32 and
+ * rounded once.
  *   0 <= M <= TCU_MAX_RECT_DIM, 0 <= K, N <= TCU_MAX_ADAPTED_DIM (M = 0 or
  *   N = 0: a no-op);  0 <= G <= TCU_MAX_ADAPTERS;  1 <= r <= TCU_MAX_RANK;
  *   A, B, alpha and ids may be NULL if G = 0.

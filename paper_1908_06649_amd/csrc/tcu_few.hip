@@ -281,7 +281,6 @@ __global__ __launch_bounds__(256) void join_kernel(FewArgs f, const unsigned cha
   const unsigned *p = f.parts + (int64_t)m * f.N + n;
   const int64_t range = (int64_t)f.M * f.N;
   // (no branch around a load: the compiler would wait for it there)
-  // (no branch around a load: the compiler would wait for it there)
   unsigned u[kAtOnce];
 #pragma unroll
   for (int i = 0; i < kAtOnce; ++i) u[i] = p[min(i, f.splits - 1) * range];
@@ -427,7 +426,7 @@ hipError_t few(const AdapterArgs &a, float *T, int tld, hipStream_t stream) {
 
 }  // namespace
 
-// A strip's loads take 8 columns at least; a launch's blocks count in 31 bits.
+// A lane's load takes 8 bytes of a row of W: 4 columns of 16 bits, 8 of 8.
 bool few_ok(int dtype, const AdapterArgs &a) {
   return a.M <= kFewRows && a.K > 0 && a.N >= (dtype == TCU_I8_I32 ? 8 : 4);
 }

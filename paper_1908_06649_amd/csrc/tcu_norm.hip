@@ -9,7 +9,7 @@
 // Both are bound by memory: a row is read once, kept in registers while its
 // sums are formed, and written once (8192 x 8192 bf16 with a residual: 104 us,
 // 5.2 TB/s, a little over the rate of a copy of 1 GiB; the gradient 6007 x 4100 41 us, 4.8
-// TB/s, and 4.7 us for the parts of dw).  A row of up to 1024 elements is one
+// TB/s, and 4.8 us for the parts of dw).  A row of up to 1024 elements is one
 // wave's, up to 16384 a workgroup's (kV vectors of eight elements per lane, the
 // smallest number that holds the row); longer rows, and those of fewer than
 // eight, are read twice.  Sums are binary32.
@@ -20,7 +20,10 @@ namespace tcu {
 namespace {
 
 constexpr int kWaveCols = 1024, kBlockCols = 16384;
-// Up to so many rows, fewer than the chip has compute units, a row is 16 waves'.
+// Up to so many rows, no more than the chip has compute units, a row of more than 2048
+// columns is 16 waves' (us, bf16 with a residual, 4 waves / 16: 16 x 8192 3.9 / 3.3, 256 x
+// 8192 5.2 / 4.7, 256 x 4096 3.8 / 3.6, 384 x 4096 4.2 / 4.6, 1024 x 8192 12.2 / 13.3;
+// 256 x 2048 3.2 / 3.4).
 constexpr int kFewNormRows = 256;
 constexpr unsigned kInfBits = 0x7f800000u, kNormalBits = 0x00800000u;
 
@@ -552,6 +555,10 @@ hipError_t grad_go(const NormGradArgs &a, hipStream_t stream) {
         hipLaunchKernelGGL((rms_norm_grad_kernel<ELEM, 64, 2>), dim3(parts), dim3(256), 0, stream,
                            a);
     } else if (vectors(a.cols, 256) <= (ELEM == TCU_ELEM_F32 ? 2 : 3)) {
+      // As long as the next row's loads have registers; then 8 waves, whose rows have half
+      // the vectors (us, bf16, 4 waves / 8: 6007 x 4096 35.7 / 37.2, 2000 x 6144 23.1 /
+      // 26.0, 6007 x 8192 80.7 / 79.1, 6007 x 12288 127 / 123, 2000 x 16384 67 / 61; just
+      // past the bound 4 are faster, 6007 x 6200 54.5 / 61.7).
       with_vectors<3>(vectors(a.cols, 256), [&](auto v) {
         hipLaunchKernelGGL((rms_norm_grad_kernel<ELEM, 256, decltype(v)::value>), dim3(parts),
                            dim3(256), 0, stream, a);
