@@ -1,6 +1,6 @@
 """The layer operators with pointer checks on (TCU_KNOB_CHECK_POINTERS), through the C
 ABI: every operand in turn on the host is TCU_ERR_POINTER before any launch, outputs
-untouched and nothing counted; valid calls run."""
+untouched and nothing counted; valid calls run, and are captured into a graph."""
 import ctypes
 
 import numpy as np
@@ -87,15 +87,37 @@ def test_host_operands_are_refused(name, knobs):
         assert tcu.tcu_calls() > 0
 
 
-def test_calls_allocate_nothing():
-    """Device memory in use is the same before and after each call."""
-    for name, (shapes, args) in CALLS.items():
-        tensors = {k: operand(*v) for k, v in shapes.items()}
-        call = args({k: t.data_ptr() for k, t in tensors.items()})
-        assert getattr(tcu.lib(), name)(*call) == tcu.TCU_OK
+@pytest.mark.parametrize("name", CALLS)
+def test_calls_allocate_nothing(name):
+    """A capture refuses allocations; its replays do what the call does."""
+    shapes, args = CALLS[name]
+    tensors = {k: operand(*v) for k, v in shapes.items()}
+
+    def fill():
+        g = torch.Generator(device=DEV).manual_seed(1)
+        for k, t in tensors.items():
+            if k == "ids":
+                t.copy_(torch.randint(-1, G, t.shape, generator=g, device=DEV, dtype=I32))
+            elif t.is_floating_point():
+                t.normal_(generator=g)
+            else:
+                t.random_(-9 if t.dtype == I8 else 0, 9, generator=g)
+
+    def call():
+        st = torch.cuda.current_stream().cuda_stream
+        assert getattr(tcu.lib(), name)(*args({k: t.data_ptr() for k, t in tensors.items()})[:-1],
+                                        st) == tcu.TCU_OK
+
+    fill()
+    call()
+    torch.cuda.synchronize()
+    want = {k: t.clone() for k, t in tensors.items() if k != "work"}
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        call()
+    for _ in range(3):
+        fill()
         torch.cuda.synchronize()
-        free = torch.cuda.mem_get_info()[0]
-        for _ in range(3):
-            assert getattr(tcu.lib(), name)(*call) == tcu.TCU_OK
+        graph.replay()
         torch.cuda.synchronize()
-        assert torch.cuda.mem_get_info()[0] == free, name
+        assert all(torch.equal(tensors[k], t) for k, t in want.items())
