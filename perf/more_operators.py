@@ -240,7 +240,8 @@ def _decoded(q, words, cols):
     """The values in binary32 of codes and scale words."""
     table = torch.tensor(MAGNITUDES + tuple(-m for m in MAGNITUDES), device=DEVICE)
     v = table[torch.stack((q & 15, q >> 4), 2).int()].view(q.shape[0], -1, 32)
-    e = words.t().contiguous().view(torch.uint8).float() - 127.0
+    e = (words.t()[:, :, None] >> torch.tensor([0, 8, 16, 24], device=DEVICE)) & 255
+    e = e.flatten(1).float() - 127.0
     return (v * torch.exp2(e)[:, :, None]).flatten(1)[:, :cols]
 
 
