@@ -149,11 +149,9 @@ def _pack(W):
     G = _groups(cols)
     v = torch.zeros((rows, G * 128), device=DEVICE)
     v[:, :cols] = W.float()
-    v = v.view(rows, G * 4, 32)
-    e = _block_exponent(v)
-    m = (v * torch.exp2(-e)).abs()
-    mid = torch.tensor([0.25, 0.75, 1.25, 1.75, 2.5, 3.5, 5.0], device=DEVICE)
-    code = torch.bucketize(m, mid, out_int32=True).to(torch.uint8)
+    e = _block_exponent(v.view(rows, G * 4, 32))
+    v = _rounded(v).view(rows, G * 4, 32) * torch.exp2(-e)
+    code = torch.bucketize(v.abs(), torch.tensor(MAGNITUDES, device=DEVICE)).to(torch.uint8)
     code += torch.where(v < 0, 8, 0).to(torch.uint8)
     code = code.view(rows, G * 64, 2)
     scale = (e + 127).to(torch.uint8).view(rows, G * 4)
