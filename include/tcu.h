@@ -20,6 +20,9 @@
  *   - tcu_poly_eval: batch polynomial evaluation (Theorem 11).
  *   - tcu_rms_norm, tcu_adapter_gemm and tcu_clip_grads with their gradients:
  *     the operators around a model layer's products.
+ *   - tcu_mx4_quant, tcu_mx4_gemm and tcu_mx4_linear: products of matrices in
+ *     4 bits; tcu_qk_norm and tcu_qk_norm_grad: what queries and keys go
+ *     through between their projection and the attention.
  *
  * Throughout, s = sqrt(m) is the unit size (a machine parameter of the
  * model), n is the row count of a tall call and N the order of the square
@@ -487,6 +490,117 @@ int tcu_clip_grads(const void *const *grads, void *const *outs, const int64_t *c
                    void *work, void *hip_stream);
 /* Bytes of its work. */
 int64_t tcu_clip_grads_work(void);
+
+/* ---- products in 4 bits ----
+ *
+ * The format: values of 4 bits (e2m1: a sign and one of 0, 1/2, 1, 3/2, 2, 3, 4, 6)
+ * with a power-of-two scale for every 32 consecutive values along the contracted
+ * index (e8m0: 2^(byte - 127); byte 255 makes its block NaN).  A matrix of `rows`
+ * rows of `cols` values is held as
+ *   codes:  TCU_MX4_ROW_BYTES(cols) bytes a row, pitch in bytes: value c of a row in
+ *           byte c / 2, the even ones in the low half;
+ *   scales: TCU_MX4_ROW_WORDS(cols) x rows words of 32 bits, pitch in words: the
+ *           word of group g (values 128 g ..) and row r at scale[g * lds + r], the
+ *           byte of its values 128 g + 32 b .. in bits 8 b ...
+ * Rows are whole groups of 128 values: the values past cols are there, and are zeros
+ * of scale byte 0 as tcu_mx4_quant writes them (a product reads them).
+ * Base pointers of codes are 16-byte aligned and their pitches multiples of 16 of at
+ * most TCU_MAX_MX4_PITCH bytes; scales need their words' alignment.  Other operands,
+ * pitches, streams, overlap, scratch and capture: as the operators of an adapted
+ * layer above.  Results are the same on every call. */
+#define TCU_MX4_ROW_WORDS(cols) (((int64_t)(cols) + 127) / 128)
+#define TCU_MX4_ROW_BYTES(cols) (64 * TCU_MX4_ROW_WORDS(cols))
+#define TCU_MAX_MX4_PITCH ((int64_t)1 << 29)
+#define TCU_MAX_MX4_DIM ((int64_t)1 << 28)
+
+/* x (rows x cols, pitch ldx) in 4 bits, along its rows (q, scale) or along its columns
+ * (qt, tscale: the matrix x^T, cols x rows) or both in one pass; a pair that is NULL is
+ * not written.  Of a block whose largest magnitude is amax:
+ *   e = floor(log2 amax) - 2 (at least -127; -127 for amax = 0),  byte = e + 127
+ *   code = x / 2^e rounded to nearest even, magnitudes above 6 to 6, with x's sign
+ * A block with a value that is not finite has byte 255 and codes 0.
+ *   0 <= rows, cols <= TCU_MAX_MX4_DIM (0: a no-op); elem: a tcu_elem, of x.
+ * Errors: TCU_ERR_NULL, TCU_ERR_SHAPE, TCU_ERR_UNSUPPORTED (elem), TCU_ERR_ALIGN,
+ * TCU_ERR_OVERLAP, TCU_ERR_POINTER, TCU_ERR_NO_DEVICE, TCU_ERR_HIP. */
+int tcu_mx4_quant(const void *x, int64_t ldx, void *q, int64_t ldq, uint32_t *scale, int64_t lds,
+                  void *qt, int64_t ldqt, uint32_t *tscale, int64_t ldts, int64_t rows,
+                  int64_t cols, int elem, void *hip_stream);
+
+/* y (rows x cols, pitch ldy): the values that (q, scale) stands for, rounded once to
+ * elem.  Sizes and errors as tcu_mx4_quant. */
+int tcu_mx4_dequant(const void *q, int64_t ldq, const uint32_t *scale, int64_t lds, void *y,
+                    int64_t ldy, int64_t rows, int64_t cols, int elem, void *hip_stream);
+
+/* C (M x N, pitch ldc) = A B^T (flags = 0) or C + A B^T (TCU_ACCUMULATE) of A (M x K)
+ * and B (N x K) in 4 bits: products of codes and scales are exact and summed in
+ * binary32; the sum, with the stored C, is rounded once to elem.  With
+ * X, W and dY brought to 4 bits both ways, Y = X W^T, dX = dY (W^T)^T and
+ * dW = dY^T (X^T)^T are the three products of a layer in training.
+ *   0 <= M, N, K <= TCU_MAX_MX4_DIM (M = 0 or N = 0: a no-op; K = 0: zeros, or C as it
+ *   is); elem: a tcu_elem, of C.
+ * Errors as above.  Cost accounting as tcu_gemm_rect. */
+int tcu_mx4_gemm(const void *A, int64_t lda, const uint32_t *ascale, int64_t ldas, const void *B,
+                 int64_t ldb, const uint32_t *bscale, int64_t ldbs, void *C, int64_t ldc,
+                 void *work, int64_t M, int64_t K, int64_t N, int flags, int elem,
+                 void *hip_stream);
+
+/* The same with a 16-bit left operand: Y = [Y +] q(X) W^T, q(X) what tcu_mx4_quant
+ * makes of X (M x K, pitch ldx, xelem TCU_ELEM_F16 or TCU_ELEM_BF16) along its rows; a
+ * layer with weights in 4 bits.  elem, of Y: TCU_ELEM_F32 or xelem. */
+int tcu_mx4_linear(const void *X, int64_t ldx, const void *W, int64_t ldw,
+                   const uint32_t *wscale, int64_t ldws, void *Y, int64_t ldy, void *work,
+                   int64_t M, int64_t K, int64_t N, int flags, int xelem, int elem,
+                   void *hip_stream);
+/* Bytes of work that either takes (-1: a size out of range), of M rows or of fewer. */
+int64_t tcu_mx4_work(int64_t M, int64_t K, int64_t N);
+
+/* ---- norms of queries and keys with their rotation ----
+ *
+ * For every token t and every head of its queries (hq) and keys (hk), over the head's
+ * `dim` elements:
+ *   v = x * rstd * w,  rstd = 1 / sqrt(mean(x^2) + eps)       (w: wq or wk)
+ *   y = v with its first `rot` elements turned in pairs by the angles
+ *       pos[t] * freq[i], i < rot / 2:
+ *       (y_a, y_b) = (v_a cos - v_b sin, v_a sin + v_b cos),
+ *       (a, b) = (i, i + rot / 2), or (2 i, 2 i + 1) with TCU_ROPE_ADJACENT
+ * formed in binary32 and rounded once; the angles are formed so that they are right to
+ * binary32 at any int32 position.  Head h of token t begins at t * ld + h * hd of its
+ * operand (pitches in elements, no alignment asked of them): token by token (hd < ld, as
+ * views of packed queries, keys and values) or head by head (ld < hd).  yq may be exactly q and yk exactly k.
+ * A head of zeros has y = 0, also for eps = 0 (as tcu_rms_norm).
+ *   0 <= tokens <= TCU_MAX_RECT_DIM; 0 <= hq, hk <= TCU_MAX_HEADS (operands of no
+ *   heads may be NULL); 1 <= dim <= TCU_MAX_HEAD_DIM; 0 <= rot <= dim, even (rot = 0:
+ *   freq and pos may be NULL); eps >= 0, finite; elem: a tcu_elem, of q, k, wq, wk, yq
+ *   and yk.  freq: rot / 2 binary32 values; pos: int32.
+ * Errors: TCU_ERR_NULL, TCU_ERR_SHAPE, TCU_ERR_UNSUPPORTED (elem, flags),
+ * TCU_ERR_ALIGN, TCU_ERR_OVERLAP, TCU_ERR_POINTER, TCU_ERR_NO_DEVICE, TCU_ERR_HIP.
+ * Alignment: q, k, yq and yk need their elements' alignment (a packed row's keys begin
+ * where its queries end); wq and wk are 16-byte aligned. */
+#define TCU_ROPE_ADJACENT 1
+#define TCU_MAX_HEAD_DIM 1024
+#define TCU_MAX_HEADS 65536
+int tcu_qk_norm(const void *q, int64_t ldq, int64_t hdq, const void *k, int64_t ldk, int64_t hdk,
+                const void *wq, const void *wk, const float *freq, const int32_t *pos, void *yq,
+                int64_t ldyq, int64_t hdyq, void *yk, int64_t ldyk, int64_t hdyk, int64_t tokens,
+                int64_t hq, int64_t hk, int64_t dim, int64_t rot, float eps, int flags, int elem,
+                void *hip_stream);
+
+/* Its gradients, from q and k as they went in.  With dv = dy turned back, g = dv * w and
+ * n = x * rstd:
+ *   dx = rstd * (g - n * mean(g * n));  dw = sum over tokens and heads of dv * n
+ * dq and dk have q's and k's type and are rounded once; dwq and dwk are `dim` binary32
+ * values each, overwritten (zeros for tokens = 0; NULL where there are no heads), summed
+ * in an order that depends on the sizes alone.  dq may be exactly dyq or q, dk exactly
+ * dyk or k.  Errors as tcu_qk_norm. */
+int tcu_qk_norm_grad(const void *dyq, int64_t lddyq, int64_t hddyq, const void *dyk,
+                     int64_t lddyk, int64_t hddyk, const void *q, int64_t ldq, int64_t hdq,
+                     const void *k, int64_t ldk, int64_t hdk, const void *wq, const void *wk,
+                     const float *freq, const int32_t *pos, void *dq, int64_t lddq, int64_t hddq,
+                     void *dk, int64_t lddk, int64_t hddk, float *dwq, float *dwk, void *work,
+                     int64_t tokens, int64_t hq, int64_t hk, int64_t dim, int64_t rot, float eps,
+                     int flags, int elem, void *hip_stream);
+/* Bytes of its work (-1: a size out of range), of as many tokens or fewer. */
+int64_t tcu_qk_norm_grad_work(int64_t tokens, int64_t hq, int64_t hk, int64_t dim);
 
 /* ---- cost accounting (Theorem 2 proof; Section 5 weak model) ----
  * tcu_calls:        logical tensor-unit calls issued (1 per tall call,

@@ -22,7 +22,8 @@ PROBE_LIB = os.path.join(HERE, "libtcu_probe.so")
 BUILD_DIR = os.path.join(ROOT, "_build")
 SOURCES = ["tcu_abi.cpp", "tcu_tall.hip", "tcu_gemm.hip", "tcu_poly.hip", "tcu_tc.hip",
            "tcu_dft.hip", "tcu_layer_abi.cpp", "tcu_norm.hip", "tcu_adapter.hip", "tcu_few.hip",
-           "tcu_clip.hip"]
+           "tcu_clip.hip", "tcu_mx4_abi.cpp", "tcu_mx4.hip", "tcu_mx4_gemm.hip",
+           "tcu_heads_abi.cpp", "tcu_heads.hip"]
 ARCH = "gfx950"
 
 COMMON = ["-O3", "-std=c++17", "-fPIC", "-fvisibility=hidden",

@@ -1,0 +1,278 @@
+// Matrices to 4 bits and back (tcu_mx4_quant, tcu_mx4_dequant).
+//
+//   e = floor(log2 max|x|) - 2 over a block of 32,  code = x / 2^e to nearest even on
+//   0, 1/2, 1, 3/2, 2, 3, 4, 6, clamped to 6;  scale byte e + 127
+//
+// Both are bound by memory: x is read once, also where it is written along its rows
+// and along its columns.  Along the rows a lane holds eight values, four lanes a
+// block, 16 a group of 128 with its word of four scales; a workgroup takes 32 rows of
+// 512 columns, so that the words, which lie group by group, fill whole lines.  Along
+// the columns a tile of 128 x 128 goes through LDS, where a lane takes 32 rows of two
+// columns.
+#include <algorithm>
+
+#include "tcu_mx4_dev.h"
+
+namespace tcu {
+namespace {
+
+// ------------------------------------------------------------- along the rows
+constexpr int kRowTile = 32, kColTile = 512;
+
+template <int ELEM>
+__global__ __launch_bounds__(256) void quant_rows_kernel(Mx4QuantArgs a, int64_t col_tiles) {
+  constexpr int ES = elem_bytes<ELEM>;
+  __shared__ unsigned words[4][kRowTile];
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+  const int64_t r0 = (int64_t)blockIdx.x / col_tiles * kRowTile;
+  const int64_t c0 = (int64_t)blockIdx.x % col_tiles * kColTile;
+  const int64_t col = c0 + lane * 8;
+  const int64_t groups = mx4_groups(a.cols);
+  const int valid = (int)min((int64_t)8, max((int64_t)0, a.cols - col));
+  constexpr int kMine = kRowTile / 4;
+  Raw8<ELEM> raw[kMine];
+#pragma unroll
+  for (int i = 0; i < kMine; ++i) {
+    const int64_t r = r0 + wave * kMine + i;
+    raw[i] = Raw8<ELEM>{};
+    if (r < a.rows && valid > 0)
+      raw[i] = load8<ELEM>((const unsigned char *)a.x + (r * a.ldx + col) * ES, valid);
+  }
+#pragma unroll
+  for (int i = 0; i < kMine; ++i) {
+    const int64_t r = r0 + wave * kMine + i;
+    float x[8];
+    unpack8<ELEM>(raw[i], x);
+    unsigned m = 0;
+#pragma unroll
+    for (int e = 0; e < 8; ++e) m = umax(m, abs_bits(x[e]));
+    const unsigned byte = scale_byte(quad_max(m));
+    const unsigned c = codes8(x, byte);
+    if (r < a.rows && col < groups * 128) *(unsigned *)(a.q + r * a.ldq + (col >> 1)) = c;
+    const unsigned word = quads_or(byte << (8 * ((lane >> 2) & 3)));
+    if ((lane & 15) == 0) words[lane >> 4][wave * kMine + i] = word;
+  }
+  __syncthreads();
+  if (threadIdx.x < 4 * kRowTile) {
+    const int g = threadIdx.x / kRowTile, i = threadIdx.x % kRowTile;
+    const int64_t r = r0 + i, group = c0 / 128 + g;
+    if (r < a.rows && group < groups) a.s[group * a.lds + r] = words[g][i];
+  }
+}
+
+// --------------------------------------------------- along the columns, or both
+constexpr int kTile = 128;
+
+// LDS: a tile's values as they are stored, rows of 128 and one bank more; then the
+// columns' codes.
+template <int ELEM>
+constexpr int kTilePitch = kTile *elem_bytes<ELEM> + 4;
+
+template <int ELEM, bool kRows>
+__global__ __launch_bounds__(256) void quant_both_kernel(Mx4QuantArgs a, int64_t col_tiles) {
+  constexpr int ES = elem_bytes<ELEM>, kPitch = kTilePitch<ELEM>;
+  __shared__ __attribute__((aligned(16))) unsigned char tile[kTile * kPitch];
+  __shared__ unsigned words[kTile];
+  __shared__ __attribute__((aligned(16))) unsigned char codes[kTile * 64];
+  __shared__ unsigned char bytes[kTile * 4];
+  const int t = threadIdx.x, lane = t & 63, wave = t >> 6;
+  const int64_t r0 = (int64_t)blockIdx.x / col_tiles * kTile;
+  const int64_t c0 = (int64_t)blockIdx.x % col_tiles * kTile;
+  {
+    const int64_t col = c0 + (t & 15) * 8;
+    const int valid = (int)min((int64_t)8, max((int64_t)0, a.cols - col));
+    Raw8<ELEM> raw[8];
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+      const int64_t r = r0 + i * 16 + (t >> 4);
+      raw[i] = Raw8<ELEM>{};
+      if (r < a.rows && valid > 0)
+        raw[i] = load8<ELEM>((const unsigned char *)a.x + (r * a.ldx + col) * ES, valid);
+    }
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+      const int row = i * 16 + (t >> 4);
+      unsigned *p = (unsigned *)(tile + row * kPitch + (t & 15) * 8 * ES);
+#pragma unroll
+      for (int d = 0; d < 2 * ES; ++d) p[d] = raw[i].v[d >> 2][d & 3];
+      if constexpr (kRows) {
+        float x[8];
+        unpack8<ELEM>(raw[i], x);
+        unsigned m = 0;
+#pragma unroll
+        for (int e = 0; e < 8; ++e) m = umax(m, abs_bits(x[e]));
+        const unsigned byte = scale_byte(quad_max(m));
+        const unsigned c = codes8(x, byte);
+        if (r0 + row < a.rows) *(unsigned *)(a.q + (r0 + row) * a.ldq + c0 / 2 + (t & 15) * 4) = c;
+        const unsigned word = quads_or(byte << (8 * ((t >> 2) & 3)));
+        if ((t & 15) == 0) words[row] = word;
+      }
+    }
+  }
+  __syncthreads();
+  if constexpr (kRows) {
+    if (t < kTile && r0 + t < a.rows) a.s[c0 / 128 * a.lds + r0 + t] = words[t];
+  }
+  // wave w: rows 32 w .. of columns 2 lane, 2 lane + 1
+  {
+    const unsigned char *p = tile + 32 * wave * kPitch + lane * 2 * ES;
+    unsigned m0 = 0, m1 = 0;
+    float x0[32], x1[32];
+#pragma unroll
+    for (int i = 0; i < 32; ++i) {
+      if constexpr (ELEM == TCU_ELEM_F32) {
+        x0[i] = ((const float *)(p + i * kPitch))[0];
+        x1[i] = ((const float *)(p + i * kPitch))[1];
+      } else {
+        const unsigned v = *(const unsigned *)(p + i * kPitch);
+        if constexpr (ELEM == TCU_ELEM_F16) {
+          x0[i] = (float)bitcast<_Float16>((unsigned short)(v & 0xffffu));
+          x1[i] = (float)bitcast<_Float16>((unsigned short)(v >> 16));
+        } else {
+          x0[i] = bf16_to_f32(v & 0xffffu);
+          x1[i] = bitcast<float>(v & 0xffff0000u);
+        }
+      }
+      m0 = umax(m0, abs_bits(x0[i]));
+      m1 = umax(m1, abs_bits(x1[i]));
+    }
+    const unsigned b0 = scale_byte(m0), b1 = scale_byte(m1);
+    u32x4 q0, q1;
+#pragma unroll
+    for (int d = 0; d < 4; ++d) {
+      float y0[8], y1[8];
+#pragma unroll
+      for (int e = 0; e < 8; ++e) {
+        y0[e] = x0[8 * d + e];
+        y1[e] = x1[8 * d + e];
+      }
+      q0[d] = codes8(y0, b0);
+      q1[d] = codes8(y1, b1);
+    }
+    *(u32x4 *)(codes + (2 * lane) * 64 + wave * 16) = q0;
+    *(u32x4 *)(codes + (2 * lane + 1) * 64 + wave * 16) = q1;
+    bytes[(2 * lane) * 4 + wave] = (unsigned char)b0;
+    bytes[(2 * lane + 1) * 4 + wave] = (unsigned char)b1;
+  }
+  __syncthreads();
+#pragma unroll
+  for (int i = 0; i < 2; ++i) {
+    const int64_t c = c0 + i * 64 + (t >> 2);
+    if (c < a.cols)
+      *(u32x4 *)(a.qt + c * a.ldqt + r0 / 2 + (t & 3) * 16) =
+          *(const u32x4 *)(codes + (i * 64 + (t >> 2)) * 64 + (t & 3) * 16);
+  }
+  if (t < kTile && c0 + t < a.cols)
+    a.ts[r0 / 128 * a.ldts + c0 + t] = *(const unsigned *)(bytes + t * 4);
+}
+
+// ----------------------------------------------------------------------- back
+template <int ELEM>
+__global__ __launch_bounds__(256) void dequant_kernel(Mx4DequantArgs a, int64_t col_tiles) {
+  constexpr int ES = elem_bytes<ELEM>;
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+  const int64_t r0 = (int64_t)blockIdx.x / col_tiles * kRowTile;
+  const int64_t col = (int64_t)blockIdx.x % col_tiles * kColTile + lane * 8;
+  const int valid = (int)min((int64_t)8, a.cols - col);
+  if (valid <= 0) return;
+  constexpr int kMine = kRowTile / 4;
+  unsigned c[kMine], byte[kMine];
+#pragma unroll
+  for (int i = 0; i < kMine; ++i) {
+    const int64_t r = min(r0 + wave * kMine + i, a.rows - 1);
+    c[i] = *(const unsigned *)(a.q + r * a.ldq + (col >> 1));
+    byte[i] = (a.s[(col >> 7) * a.lds + r] >> (8 * ((lane >> 2) & 3))) & 255u;
+  }
+#pragma unroll
+  for (int i = 0; i < kMine; ++i) {
+    const int64_t r = r0 + wave * kMine + i;
+    // a scale of 2^-127 is no normal number: the value is formed 2^32 times larger
+    const bool low = byte[i] < 32u;
+    const float scale = byte[i] == 255u ? __builtin_nanf("")
+                                        : bitcast<float>((low ? byte[i] + 32u : byte[i]) << 23);
+    const float down = low ? 0x1p-32f : 1.f;
+    float x[8];
+#pragma unroll
+    for (int e = 0; e < 8; ++e) {
+      const unsigned k = (c[i] >> (4 * e)) & 15u, mag = k & 7u;
+      // e2m1: exponent field 0 has steps of a half, then 2^(field - 1) (1 + m / 2)
+      const float v = mag < 2u ? 0.5f * (float)mag
+                               : bitcast<float>(((mag >> 1) + 126u) << 23 | (mag & 1u) << 22);
+      x[e] = bitcast<float>(bitcast<unsigned>(v) | (k & 8u) << 28) * scale * down;
+    }
+    if (r < a.rows) store8<ELEM>((unsigned char *)a.y + (r * a.ldy + col) * ES, x, valid);
+  }
+}
+
+// Workgroups of a launch count in 2^31 here and threads in 32 bits: more tiles of
+// rows than that are launched in turn.
+template <typename F>
+hipError_t by_rows(int64_t rows, int64_t row_tile, int64_t col_tiles, F launch) {
+  if (col_tiles == 0) return hipSuccess;
+  const int64_t most = std::max<int64_t>(1, ((int64_t)1 << 23) / col_tiles);
+  for (int64_t r = 0; r < rows; r += most * row_tile) {
+    const int64_t n = std::min(rows - r, most * row_tile);
+    launch(r, n, (unsigned)((n + row_tile - 1) / row_tile * col_tiles));
+    const hipError_t e = hipGetLastError();
+    if (e != hipSuccess) return e;
+  }
+  return hipSuccess;
+}
+
+template <int ELEM>
+hipError_t quant(const Mx4QuantArgs &a, hipStream_t stream) {
+  const int tile = a.qt ? kTile : kRowTile, width = a.qt ? kTile : kColTile;
+  const int64_t col_tiles = (a.cols + width - 1) / width;
+  return by_rows(a.rows, tile, col_tiles, [&](int64_t r, int64_t n, unsigned blocks) {
+    Mx4QuantArgs p = a;
+    p.x = (const unsigned char *)a.x + r * a.ldx * elem_bytes<ELEM>;
+    p.rows = n;
+    if (a.q) {
+      p.q += r * a.ldq;
+      p.s += r;
+    }
+    if (a.qt) {
+      p.qt += r / 2;
+      p.ts += r / 128 * a.ldts;
+    }
+    if (!a.qt)
+      quant_rows_kernel<ELEM><<<blocks, 256, 0, stream>>>(p, col_tiles);
+    else if (a.q)
+      quant_both_kernel<ELEM, true><<<blocks, 256, 0, stream>>>(p, col_tiles);
+    else
+      quant_both_kernel<ELEM, false><<<blocks, 256, 0, stream>>>(p, col_tiles);
+  });
+}
+
+template <int ELEM>
+hipError_t dequant(const Mx4DequantArgs &a, hipStream_t stream) {
+  const int64_t col_tiles = (a.cols + kColTile - 1) / kColTile;
+  return by_rows(a.rows, kRowTile, col_tiles, [&](int64_t r, int64_t n, unsigned blocks) {
+    Mx4DequantArgs p = a;
+    p.q += r * a.ldq;
+    p.s += r;
+    p.y = (unsigned char *)a.y + r * a.ldy * elem_bytes<ELEM>;
+    p.rows = n;
+    dequant_kernel<ELEM><<<blocks, 256, 0, stream>>>(p, col_tiles);
+  });
+}
+
+}  // namespace
+
+hipError_t launch_mx4_quant(int elem, const Mx4QuantArgs &a, hipStream_t stream) {
+  switch (elem) {
+    case TCU_ELEM_F32: return quant<TCU_ELEM_F32>(a, stream);
+    case TCU_ELEM_F16: return quant<TCU_ELEM_F16>(a, stream);
+    default: return quant<TCU_ELEM_BF16>(a, stream);
+  }
+}
+
+hipError_t launch_mx4_dequant(int elem, const Mx4DequantArgs &a, hipStream_t stream) {
+  switch (elem) {
+    case TCU_ELEM_F32: return dequant<TCU_ELEM_F32>(a, stream);
+    case TCU_ELEM_F16: return dequant<TCU_ELEM_F16>(a, stream);
+    default: return dequant<TCU_ELEM_BF16>(a, stream);
+  }
+}
+
+}  // namespace tcu

@@ -30,6 +30,21 @@ and the operators around a layer's products:
     tcu_clip_grads(grads, outs, max_norm, result, work)
                                  outs = grads * min(1, max_norm / (norm + 1e-6))
 
+products in 4 bits (codes and power-of-two scales of blocks of 32, include/tcu.h) and
+what queries and keys go through after their projection:
+
+    tcu_mx4_quant(x, ldx, q, ldq, scale, lds, qt, ldqt, tscale, ldts, rows, cols)
+                                 x in 4 bits along its rows and along its columns
+    tcu_mx4_dequant(q, ldq, scale, lds, y, ldy, rows, cols)
+    tcu_mx4_gemm(A, lda, ascale, ldas, B, ldb, bscale, ldbs, C, ldc, work, M, K, N, flags)
+                                 C (M x N) = [C +] A (M x K) @ B (N x K)^T
+    tcu_mx4_linear(X, ldx, W, ldw, wscale, ldws, Y, ldy, work, M, K, N, flags)
+                                 the same with a 16-bit left operand
+    tcu_qk_norm(q, k, wq, wk, freq, pos, yq, yk, tokens, hq, hk, dim, rot, eps, flags)
+                                 every head's RMS norm, its pairs turned by the position
+    tcu_qk_norm_grad(dyq, dyk, q, k, wq, wk, freq, pos, dq, dk, dwq, dwk, work, tokens, hq, hk,
+                     dim, rot, eps, flags)
+
 The element types are taken from the tensors: (float16 -> float32),
 (bfloat16 -> float32), (bfloat16 -> bfloat16) or (int8 -> int32).  Calls are
 issued on torch's current stream and are asynchronous.
@@ -113,6 +128,16 @@ SIGNATURES = {
     "tcu_adapter_work": (_i64, [_i64, _i64, _i64, _i64, _i64]),
     "tcu_clip_grads": (_int, [_vp, _vp, _vp, _vp, _i64, ctypes.c_float, _vp, _vp, _vp]),
     "tcu_clip_grads_work": (_i64, []),
+    "tcu_mx4_quant": (_int, [_vp, _i64] * 5 + [_i64, _i64, _int, _vp]),
+    "tcu_mx4_dequant": (_int, [_vp, _i64] * 3 + [_i64, _i64, _int, _vp]),
+    "tcu_mx4_gemm": (_int, [_vp, _i64] * 5 + [_vp, _i64, _i64, _i64, _int, _int, _vp]),
+    "tcu_mx4_linear": (_int, [_vp, _i64] * 4 + [_vp, _i64, _i64, _i64, _int, _int, _int, _vp]),
+    "tcu_mx4_work": (_i64, [_i64, _i64, _i64]),
+    "tcu_qk_norm": (_int, [_vp, _i64, _i64] * 2 + [_vp] * 4 + [_vp, _i64, _i64] * 2 +
+                    [_i64] * 5 + [ctypes.c_float, _int, _int, _vp]),
+    "tcu_qk_norm_grad": (_int, [_vp, _i64, _i64] * 4 + [_vp] * 4 + [_vp, _i64, _i64] * 2 +
+                         [_vp] * 3 + [_i64] * 5 + [ctypes.c_float, _int, _int, _vp]),
+    "tcu_qk_norm_grad_work": (_i64, [_i64, _i64, _i64, _i64]),
     "tcu_calls": (_i64, []),
     "tcu_square_calls": (_i64, []),
     "tcu_work": (_i64, []),
@@ -470,14 +495,15 @@ TCU_MAX_ADAPTERS = 1 << 16
 TCU_MAX_RANK = 128
 
 _ELEMS = {}
-_BF16 = _F32 = _I32 = _I8 = None
+_BF16 = _F32 = _I32 = _I8 = _U8 = None
 _NO_DEVICE = -2     # before the first tensor
 
 
 def _elem_code(where: str, dtype) -> int:
-    global _BF16, _F32, _I32, _I8
+    global _BF16, _F32, _I32, _I8, _U8
     if not _ELEMS:
         import torch
+        _U8 = torch.uint8
         _BF16, _F32, _I32, _I8 = torch.bfloat16, torch.float32, torch.int32, torch.int8
         _ELEMS.update({torch.float32: TCU_ELEM_F32, torch.float16: TCU_ELEM_F16,
                        torch.bfloat16: TCU_ELEM_BF16})
@@ -703,6 +729,160 @@ def tcu_clip_grads(grads, outs, max_norm: float, result, work,
     _check(L.tcu_clip_grads(tables[0].buffer_info()[0], tables[-1].buffer_info()[0],
                             counts.buffer_info()[0], elems.buffer_info()[0], n, max_norm, pres,
                             pwork, _stream_of(dev, stream_ptr)), where)
+
+
+# ------------------------------------------------------------- products in 4 bits
+TCU_MAX_MX4_PITCH = 1 << 29
+TCU_MAX_MX4_DIM = 1 << 28
+
+
+def tcu_mx4_row_words(cols: int) -> int:
+    """Scale words of a row of cols values in 4 bits (TCU_MX4_ROW_WORDS)."""
+    return (cols + 127) // 128
+
+
+def tcu_mx4_row_bytes(cols: int) -> int:
+    """Bytes of codes of a row of cols values in 4 bits (TCU_MX4_ROW_BYTES)."""
+    return 64 * tcu_mx4_row_words(cols)
+
+
+def _mx4(q, ldq, scale, lds, rows, cols):
+    """The views of a matrix in 4 bits: codes uint8, scales int32."""
+    words = (cols + 127) // 128
+    return (q, _U8, rows, 64 * words, ldq), (scale, _I32, words, rows, lds)
+
+
+def tcu_mx4_quant(x, ldx: int, q, ldq: int, scale, lds: int, qt, ldqt: int, tscale, ldts: int,
+                  rows: int, cols: int, stream_ptr: int | None = None) -> None:
+    """x (rows x cols) in 4 bits along its rows (q: uint8, rows x tcu_mx4_row_bytes(cols);
+    scale: int32, tcu_mx4_row_words(cols) x rows) and along its columns (qt, tscale: of
+    x^T); either pair may be None."""
+    where, t = "tcu_mx4_quant", x.dtype
+    elem = _elem_code(where, t)
+    dev, (px, pq, ps, pqt, pts) = _addresses(
+        where, ((x, t, rows, cols, ldx),) + _mx4(q, ldq, scale, lds, rows, cols) +
+        _mx4(qt, ldqt, tscale, ldts, cols, rows), (), None, 0)
+    _check((_lib or lib()).tcu_mx4_quant(px, ldx, pq, ldq, ps, lds, pqt, ldqt, pts, ldts, rows,
+                                         cols, elem, _stream_of(dev, stream_ptr)), where)
+
+
+def tcu_mx4_dequant(q, ldq: int, scale, lds: int, y, ldy: int, rows: int, cols: int,
+                    stream_ptr: int | None = None) -> None:
+    """y (rows x cols) = the values that (q, scale) stands for."""
+    where, t = "tcu_mx4_dequant", y.dtype
+    elem = _elem_code(where, t)
+    dev, (py, pq, ps) = _addresses(
+        where, ((y, t, rows, cols, ldy),) + _mx4(q, ldq, scale, lds, rows, cols), (), None, 0)
+    _check((_lib or lib()).tcu_mx4_dequant(pq, ldq, ps, lds, py, ldy, rows, cols, elem,
+                                           _stream_of(dev, stream_ptr)), where)
+
+
+def tcu_mx4_work(M: int, K: int, N: int) -> int:
+    """Bytes of work of tcu_mx4_gemm and tcu_mx4_linear (-1: a size out of range)."""
+    return (_lib or lib()).tcu_mx4_work(M, K, N)
+
+
+def tcu_mx4_gemm(A, lda: int, ascale, ldas: int, B, ldb: int, bscale, ldbs: int, C, ldc: int, work,
+                 M: int, K: int, N: int, flags: int = 0, stream_ptr: int | None = None) -> None:
+    """C (M x N) = [C +] A (M x K) @ B (N x K)^T, A and B in 4 bits."""
+    where, t = "tcu_mx4_gemm", C.dtype
+    elem = _elem_code(where, t)
+    L = _lib or lib()
+    dev, (pc, pa, pas, pb, pbs, pwork) = _addresses(
+        where, ((C, t, M, N, ldc),) + _mx4(A, lda, ascale, ldas, M, K) +
+        _mx4(B, ldb, bscale, ldbs, N, K), (), work, L.tcu_mx4_work(M, K, N))
+    _check(L.tcu_mx4_gemm(pa, lda, pas, ldas, pb, ldb, pbs, ldbs, pc, ldc, pwork, M, K, N, flags,
+                          elem, _stream_of(dev, stream_ptr)), where)
+
+
+def tcu_mx4_linear(X, ldx: int, W, ldw: int, wscale, ldws: int, Y, ldy: int, work, M: int, K: int,
+                   N: int, flags: int = 0, stream_ptr: int | None = None) -> None:
+    """Y (M x N) = [Y +] q(X) @ W^T: X (M x K) 16-bit, brought to 4 bits along its rows; W
+    (N x K) in 4 bits; Y float32 or X's type."""
+    where, t = "tcu_mx4_linear", X.dtype
+    xelem, elem = _elem_code(where, t), _elem_code(where, Y.dtype)
+    L = _lib or lib()
+    dev, (px, py, pw, pws, pwork) = _addresses(
+        where, ((X, t, M, K, ldx), (Y, Y.dtype, M, N, ldy)) + _mx4(W, ldw, wscale, ldws, N, K),
+        (), work, L.tcu_mx4_work(M, K, N))
+    _check(L.tcu_mx4_linear(px, ldx, pw, ldw, pws, ldws, py, ldy, pwork, M, K, N, flags, xelem,
+                            elem, _stream_of(dev, stream_ptr)), where)
+
+
+# -------------------------------------------- norms of queries and keys with rotation
+TCU_ROPE_ADJACENT = 1
+TCU_MAX_HEAD_DIM = 1024
+TCU_MAX_HEADS = 65536
+
+
+def _heads(where, operands, dtype, vectors, work, nbytes):
+    """Checks of operands (tensor, tokens, heads, dim) of one type, any pitches of tokens
+    and heads, and of vectors and work as _addresses.  Returns the device, three
+    arguments for each operand and the vectors' addresses, work's last."""
+    out, dev = [], _NO_DEVICE
+    for t, *shape in operands:
+        if t is None:
+            out += (None, 0, 0)
+            continue
+        d = t.get_device()
+        if d != dev:
+            dev = _first_device(where, dev, d)
+        if t.dtype != dtype:
+            raise ValueError(f"{where}: expected {dtype}, got {t.dtype}")
+        if list(t.shape) != shape:
+            raise ValueError(f"{where}: expected {shape}, got {tuple(t.shape)}")
+        ld, hd, one = t.stride()
+        if one != 1 and shape[2] > 1 and t.numel():
+            raise ValueError(f"{where}: strides {t.stride()} of heads that are not contiguous")
+        out += (t.data_ptr() or None, ld, hd)
+    vdev, ptrs = _addresses(where, (), vectors, work, nbytes)
+    if dev not in (_NO_DEVICE, vdev):
+        raise ValueError(f"{where}: all tensors must be on the same HIP device")
+    return vdev, out, ptrs
+
+
+def _qk_vectors(wq, wk, freq, pos, dtype, tokens, dim, rot):
+    return ((wq, dtype, dim), (wk, dtype, dim), (freq, _F32, rot // 2), (pos, _I32, tokens))
+
+
+def tcu_qk_norm(q, k, wq, wk, freq, pos, yq, yk, tokens: int, hq: int, hk: int, dim: int, rot: int,
+                eps: float, flags: int = 0, stream_ptr: int | None = None) -> None:
+    """Every head's RMS norm (weights wq and wk) with its first rot elements turned in pairs
+    by the angles pos[t] * freq[i].  q and yq: tokens x hq x dim, k and yk: tokens x hk x
+    dim, of any pitches of tokens and heads (the tensors' strides); yq may be q and yk k.
+    freq: rot / 2 float32; pos: tokens int32; flags: 0 or TCU_ROPE_ADJACENT."""
+    where = "tcu_qk_norm"
+    t = (k if q is None else q).dtype
+    elem = _elem_code(where, t)
+    dev, p, (pwq, pwk, pf, pp) = _heads(
+        where, ((q, tokens, hq, dim), (k, tokens, hk, dim), (yq, tokens, hq, dim),
+                (yk, tokens, hk, dim)), t, _qk_vectors(wq, wk, freq, pos, t, tokens, dim, rot),
+        None, 0)
+    _check((_lib or lib()).tcu_qk_norm(*p[:6], pwq, pwk, pf, pp, *p[6:], tokens, hq, hk, dim, rot,
+                                       eps, flags, elem, _stream_of(dev, stream_ptr)), where)
+
+
+def tcu_qk_norm_grad_work(tokens: int, hq: int, hk: int, dim: int) -> int:
+    """Bytes of tcu_qk_norm_grad's work (-1: a size out of range)."""
+    return (_lib or lib()).tcu_qk_norm_grad_work(tokens, hq, hk, dim)
+
+
+def tcu_qk_norm_grad(dyq, dyk, q, k, wq, wk, freq, pos, dq, dk, dwq, dwk, work, tokens: int,
+                     hq: int, hk: int, dim: int, rot: int, eps: float, flags: int = 0,
+                     stream_ptr: int | None = None) -> None:
+    """The gradients of tcu_qk_norm: dq and dk (shapes and type of q and k), dwq and dwk
+    (dim float32 each), from the gradients dyq and dyk of its outputs."""
+    where = "tcu_qk_norm_grad"
+    t = (k if q is None else q).dtype
+    elem = _elem_code(where, t)
+    L = _lib or lib()
+    dev, p, (pwq, pwk, pf, pp, pdwq, pdwk, pwork) = _heads(
+        where, ((dyq, tokens, hq, dim), (dyk, tokens, hk, dim), (q, tokens, hq, dim),
+                (k, tokens, hk, dim), (dq, tokens, hq, dim), (dk, tokens, hk, dim)), t,
+        _qk_vectors(wq, wk, freq, pos, t, tokens, dim, rot) + ((dwq, _F32, dim), (dwk, _F32, dim)),
+        work, L.tcu_qk_norm_grad_work(tokens, hq, hk, dim))
+    _check(L.tcu_qk_norm_grad(*p[:12], pwq, pwk, pf, pp, *p[12:], pdwq, pdwk, pwork, tokens, hq,
+                              hk, dim, rot, eps, flags, elem, _stream_of(dev, stream_ptr)), where)
 
 
 # --------------------------------------------------------- cost accounting
