@@ -510,8 +510,8 @@ int64_t tcu_clip_grads_work(void);
  * layer above.  Results are the same on every call. */
 #define TCU_MX4_ROW_WORDS(cols) (((int64_t)(cols) + 127) / 128)
 #define TCU_MX4_ROW_BYTES(cols) (64 * TCU_MX4_ROW_WORDS(cols))
-#define TCU_MAX_MX4_PITCH ((int64_t)1 << 29)
-#define TCU_MAX_MX4_DIM ((int64_t)1 << 28)
+#define TCU_MAX_MX4_PITCH ((int64_t)1 << 26)
+#define TCU_MAX_MX4_DIM ((int64_t)1 << 27)
 
 /* x (rows x cols, pitch ldx) in 4 bits, along its rows (q, scale) or along its columns
  * (qt, tscale: the matrix x^T, cols x rows) or both in one pass; a pair that is NULL is

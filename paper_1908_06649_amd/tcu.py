@@ -732,8 +732,8 @@ def tcu_clip_grads(grads, outs, max_norm: float, result, work,
 
 
 # ------------------------------------------------------------- products in 4 bits
-TCU_MAX_MX4_PITCH = 1 << 29
-TCU_MAX_MX4_DIM = 1 << 28
+TCU_MAX_MX4_PITCH = 1 << 26
+TCU_MAX_MX4_DIM = 1 << 27
 
 
 def tcu_mx4_row_words(cols: int) -> int:
