@@ -20,24 +20,32 @@ __device__ __forceinline__ unsigned scale_byte(unsigned max_bits) {
   return max_bits >= kNotFinite ? 255u : e > 2u ? e - 2u : 0u;
 }
 
+// Whether a lane's block needs the slow conversion: its values or its scale may lie below
+// binary32's normal numbers, which the conversion takes.
+__device__ __forceinline__ bool scale_low(unsigned max_bits) {
+  return max_bits != 0u && max_bits < 34u << 23;
+}
+
 // Eight values of a block as codes, the first in the lowest bits: rounded to nearest
-// even and clamped to 6.  Values near binary32's smallest are brought up together
-// with their scale first (the conversion takes normal numbers).
+// even and clamped to 6.  kLow: values are brought up by 2^32 together with their scale.
+template <bool kLow>
 __device__ __forceinline__ unsigned codes8(const float (&x)[8], unsigned byte) {
-  if (byte == 255u) return 0u;
-  const bool low = byte < 32u;
-  const float scale = bitcast<float>((low ? byte + 32u : byte) << 23);
+  const float up = kLow && byte < 32u ? 0x1p32f : 1.f;
+  const unsigned e = kLow && byte < 32u ? byte + 32u : byte;
+  const float scale = bitcast<float>((e > 1u ? e : 1u) << 23);   // (a block of zeros: any)
+  float y[8];
+#pragma unroll
+  for (int i = 0; i < 8; ++i) y[i] = kLow ? x[i] * up : x[i];
   unsigned c = 0;
-  if (__builtin_expect(low, 0)) {
-    c = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(c, x[0] * 0x1p32f, x[1] * 0x1p32f, scale, 0);
-    c = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(c, x[2] * 0x1p32f, x[3] * 0x1p32f, scale, 1);
-    c = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(c, x[4] * 0x1p32f, x[5] * 0x1p32f, scale, 2);
-    return __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(c, x[6] * 0x1p32f, x[7] * 0x1p32f, scale, 3);
-  }
-  c = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(c, x[0], x[1], scale, 0);
-  c = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(c, x[2], x[3], scale, 1);
-  c = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(c, x[4], x[5], scale, 2);
-  return __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(c, x[6], x[7], scale, 3);
+  c = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(c, y[0], y[1], scale, 0);
+  c = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(c, y[2], y[3], scale, 1);
+  c = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(c, y[4], y[5], scale, 2);
+  c = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(c, y[6], y[7], scale, 3);
+  return byte == 255u ? 0u : c;
+}
+// any_low: whether any lane of the wave has a low block (uniform).
+__device__ __forceinline__ unsigned codes8(const float (&x)[8], unsigned byte, bool any_low) {
+  return __builtin_expect(any_low, 0) ? codes8<true>(x, byte) : codes8<false>(x, byte);
 }
 
 // Lanes of a quad, and of a row of 16 lanes, exchanged in registers.

@@ -8,6 +8,7 @@
 //   * mx4_few_kernel: few rows, bound by B's bytes: a workgroup takes 16 rows of B,
 //     its waves share the contracted index, and their sums are added in LDS.
 #include <algorithm>
+#include <cmath>
 
 #include "tcu_mx4_dev.h"
 
@@ -89,18 +90,19 @@ __device__ __forceinline__ void dma_lds4_saddr(const void *gbase, unsigned voff,
 // more power: 6.0 against 6.4 PFLOP/s from registers; 295 us without the stream across
 // tiles, 80 of 340 bands of stores exposed); the order that the compiler chose (256);
 // bands of 2 or 8 rows of tiles (258, 256); four waves of 128 x 128 (spills).
-template <int ELEM, int FM, int FN, int WM, int WN>
-__global__ __launch_bounds__(64 * WM * WN) void mx4_tile_kernel(TileArgs ta) {
+template <int ELEM, int FM, int FN, int WM, int WN, int KG>
+__global__ __launch_bounds__(64 * WM * WN * KG) void mx4_tile_kernel(TileArgs ta) {
   constexpr int BM = 16 * FM * WM, BN = 16 * FN * WN, kWaves = WM * WN;
-  constexpr int kRows = (BM + BN) / kWaves, kCopies = kRows / 8, kAll = kCopies + 2;
+  constexpr int kRows = (BM + BN) / kWaves, R = 2, kCopies = kRows / 8, kAll = kCopies + 2;
   static_assert(kRows == 64 && BM % 64 == 0, "a wave copies 64 rows of one operand");
   constexpr int kCodes = (BM + BN) * 128;
   // (a group's scale words, and 16 more so that both groups' reads fill all banks)
   constexpr int kWords = (BM + BN + 16) * 4, kBuffer = kCodes + 2 * kWords;
-  __shared__ __attribute__((aligned(128))) unsigned char lds[2 * kBuffer];
+  __shared__ __attribute__((aligned(128))) unsigned char lds[R * KG * kBuffer];
   const Mx4GemmArgs &a = ta.g;
   const int lane = threadIdx.x & 63;
-  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int kg = __builtin_amdgcn_readfirstlane(threadIdx.x / (64 * kWaves));
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6) - kg * kWaves;
   const int g = lane >> 4, r16 = lane & 15, half = lane >> 5;
   const int wm = wave / WN, wn = wave % WN;
   const int tiles = ta.tiles_m * ta.tiles_n, items = tiles * ta.splits;
@@ -110,6 +112,7 @@ __global__ __launch_bounds__(64 * WM * WN) void mx4_tile_kernel(TileArgs ta) {
   struct Item {
     int64_t m, n;
     int first, last, split;
+    __device__ int rounds() const { return (last - first + KG - 1) / KG; }
   };
   auto place = [&](int id) {
     // round by round of the grid: consecutive workgroups go round the 8 XCDs, each of
@@ -141,15 +144,20 @@ __global__ __launch_bounds__(64 * WM * WN) void mx4_tile_kernel(TileArgs ta) {
   const int chunk = (lane & 7) ^ (lane >> 4);   // of the even copies; the odd ones: ^ 4
   const unsigned char *src;
   unsigned off[kCopies], word_off;
-  const unsigned *const words = is_a ? a.as : a.bs;
+  const unsigned *words;
   const int64_t words_pitch = is_a ? a.ldas : a.ldbs;
+  int stage, last;   // the group's stage that is copied next, the end of its item's
   auto aim = [&](const Item &it) {
+    stage = it.first + kg;
+    last = it.last;
+    const int at = min(stage, last - 1);
     const int64_t rows = is_a ? a.M : a.N, ld = is_a ? a.lda : a.ldb;
     const int64_t top = is_a ? it.m + wave * 64 : it.n + (wave - BM / 64) * 64;
     // rows past the edge: the last one again
     const int64_t base = min(top, rows - 1);
     const int left = (int)min(rows - 1 - base, (int64_t)63), l8 = lane >> 3;
-    src = (is_a ? a.A : a.B) + base * ld;
+    src = (is_a ? a.A : a.B) + base * ld + (int64_t)at * 128;
+    words = (is_a ? a.as : a.bs) + (int64_t)(2 * at) * words_pitch;
 #pragma unroll
     for (int i = 0; i < kCopies; ++i) {
       const int r = is_a ? 8 * i + l8
@@ -159,23 +167,32 @@ __global__ __launch_bounds__(64 * WM * WN) void mx4_tile_kernel(TileArgs ta) {
     const int r = is_a ? lane : (lane & 32) + 8 * ((lane >> 2) & 3) + 4 * ((lane >> 4) & 1) + (lane & 3);
     word_off = 4u * (unsigned)(base + min(r, left));
   };
-  const unsigned lds0 = lds_addr(lds);
-  // copies [from, upto) of a stage: codes, then the first and the second group's words
-  auto issue = [&](int stage, int buf, int from, int upto) {
-    const bool whole = 2 * stage + 1 < groups;
+  unsigned char *const ring = lds + kg * kBuffer;   // buffer r at r KG buffers
+  const unsigned lds0 = lds_addr(ring);
+  // copies [from, upto) of the next stage: codes, then the first and the second group's
+  // words
+  auto issue = [&](int buf, int from, int upto) {
     // the second half of the last stage may be missing: its scales are cleared when they
     // are read, and the first half's codes stand in for it
+    const bool whole = stage < groups >> 1;
     const unsigned back0 = !whole && chunk >= 4 ? 64u : 0u;
     const unsigned back1 = !whole && chunk < 4 ? 64u : 0u;
-    const unsigned to = lds0 + buf * kBuffer;
+    const unsigned to = lds0 + buf * KG * kBuffer;
 #pragma unroll
     for (int i = from; i < upto; ++i) {
       if (i < kCopies)
-        dma_lds16_saddr(src + (int64_t)stage * 128, off[i] - (i & 1 ? back1 : back0),
-                        to + (wave * kCopies + i) * 1024);
+        dma_lds16_saddr(src, off[i] - (i & 1 ? back1 : back0), to + (wave * kCopies + i) * 1024);
       else
-        dma_lds4_saddr(words + (int64_t)(2 * stage + (i > kCopies && whole)) * words_pitch,
-                       word_off, to + kCodes + (i - kCopies) * kWords + wave * 256);
+        dma_lds4_saddr(i > kCopies && whole ? words + words_pitch : words, word_off,
+                       to + kCodes + (i - kCopies) * kWords + wave * 256);
+    }
+  };
+  // (past the range's end its last stage again, whose scales are then not taken)
+  auto step_on = [&]() {
+    stage += KG;
+    if (KG == 1 || stage < last) {
+      src += 128 * KG;
+      words += 2 * KG * words_pitch;
     }
   };
 
@@ -185,14 +202,15 @@ __global__ __launch_bounds__(64 * WM * WN) void mx4_tile_kernel(TileArgs ta) {
   const unsigned at0 = ((2 * g) ^ (r16 >> 1)) * 16, at1 = ((2 * g + 1) ^ (r16 >> 1)) * 16;
   const unsigned row_a = (wm * 16 * FM + r16) * 128, row_b = (BM + wn * 16 * FN + r16) * 128;
   auto read_x = [&](int i, int s, int buf) {
-    x[i] = *(const u32x4 *)(lds + buf * kBuffer + (row_a + (s ? at1 : at0)) + i * 2048);
+    x[i] = *(const u32x4 *)(ring + buf * KG * kBuffer + (row_a + (s ? at1 : at0)) + i * 2048);
   };
   auto read_w = [&](int j, int s, int buf) {
-    w[s][j] = *(const u32x4 *)(lds + buf * kBuffer + (row_b + (s ? at1 : at0)) + j * 2048);
+    w[s][j] = *(const u32x4 *)(ring + buf * KG * kBuffer + (row_b + (s ? at1 : at0)) + j * 2048);
   };
-  auto read_scales = [&](int buf, bool whole) {
-    const unsigned char *p = lds + buf * kBuffer + kCodes + half * kWords + r16 * 4;
-    const unsigned keep = whole || half == 0 ? ~0u : 0u;
+  auto read_scales = [&](int buf, int stage, int end) {
+    const unsigned char *p = ring + buf * KG * kBuffer + kCodes + half * kWords + r16 * 4;
+    const int there = KG > 1 && stage >= end ? 0 : min(groups - 2 * stage, 2);   // groups
+    const unsigned keep = half < there ? ~0u : 0u;
 #pragma unroll
     for (int i = 0; i < FM; ++i)
       next_a[i] = (*(const unsigned *)(p + (wm * FM + i) * 64) & keep) >> (16 * (g & 1));
@@ -227,28 +245,31 @@ __global__ __launch_bounds__(64 * WM * WN) void mx4_tile_kernel(TileArgs ta) {
   int id = blockIdx.x, next_id = id;   // items: multiplied, and copied
   Item now = place(id);
   aim(now);
-  int t = now.first, ahead = now.first, end = now.last;   // stages: multiplied, to copy, its item's end
-  // past an item's last stage the next one's first (after the last item: its own again,
+  int left = now.rounds(), to_copy = left;   // rounds of the items: to multiply, to copy
+  // past an item's last round the next one's first (after the last item: its own again,
   // which nothing reads)
   auto advance = [&]() {
-    if (ahead < end) return;
+    if (to_copy > 0) return;
     if (next_id + (int)gridDim.x < items) next_id += gridDim.x;
     const Item it = place(next_id);
     aim(it);
-    ahead = it.first;
-    end = it.last;
+    to_copy = it.rounds();
   };
-  issue(ahead++, 0, 0, kAll);
+  issue(0, 0, kAll);
+  step_on();
+  --to_copy;
   advance();
-  int coming = ahead;   // the stage after the one in registers
-  issue(ahead++, 1, 0, kAll);
-  // (the second stage may be on its way)
+  int coming = stage;   // the stage after it
+  issue(1, 0, kAll);
+  step_on();
+  --to_copy;
+  // (the second round may be on its way)
   asm volatile("s_waitcnt vmcnt(%0)\n\ts_barrier" ::"i"(kAll) : "memory");
 #pragma unroll
   for (int j = 0; j < FN; ++j) read_w(j, 0, 0);
 #pragma unroll
   for (int i = 0; i < FM; ++i) read_x(i, 0, 0);
-  read_scales(0, 2 * t + 1 < groups);
+  read_scales(0, now.first + kg, now.last);
   take_scales();
   clear();
   // 16-byte stores of a wave's part of a whole tile, at the least
@@ -275,7 +296,7 @@ __global__ __launch_bounds__(64 * WM * WN) void mx4_tile_kernel(TileArgs ta) {
       asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
     asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory");
     const int other = buf ^ 1;
-    read_scales(other, 2 * coming + 1 < groups);
+    read_scales(other, coming, now.last);   // (only one item's ranges end inside a round)
     read_x(0, 0, other);
     read_w(0, 0, other);
     if (FN > FM) read_w(FN - 1, 0, other);
@@ -285,7 +306,7 @@ __global__ __launch_bounds__(64 * WM * WN) void mx4_tile_kernel(TileArgs ta) {
       multiply(step1, i);
       read_x(i, 0, other);
       if (i < FN) read_w(i, 0, other);
-      issue(ahead, buf, (i - 1) * kPer, i * kPer < kAll ? i * kPer : kAll);
+      issue(buf, (i - 1) * kPer, i * kPer < kAll ? i * kPer : kAll);
     }
     take_scales();
     // reads between the products, none of them waited for
@@ -301,9 +322,11 @@ __global__ __launch_bounds__(64 * WM * WN) void mx4_tile_kernel(TileArgs ta) {
       }
     }
     buf = other;
-    coming = ahead++;
+    coming = stage;
+    step_on();
+    --to_copy;
     stored = false;
-    if (++t < now.last) continue;
+    if (--left > 0) continue;
     // lane: row r16 of a block, eight columns of each pair of blocks
     const int64_t cm = now.m + wm * 16 * FM, cn = now.n + wn * 16 * FN;
     const bool inside = cm + 16 * FM <= a.M && cn + 16 * FN <= a.N;
@@ -313,15 +336,40 @@ __global__ __launch_bounds__(64 * WM * WN) void mx4_tile_kernel(TileArgs ta) {
                                  : (unsigned char *)a.C;
     const int64_t ldc = ELEM == kPart ? a.N : a.ldc;
     const bool accum = ELEM != kPart && a.accum;
+    f32x4 *const sums = (f32x4 *)lds;
+    if constexpr (KG > 1) {
+      // (its only item: nothing is on its way to the ring or read from it any more)
+      asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)\n\ts_barrier" ::: "memory");
+#pragma unroll
+      for (int i = 0; i < FM; ++i)
+#pragma unroll
+        for (int j = 0; j < FN; ++j)
+          sums[(((kg * kWaves + wave) * FM + i) * FN + j) * 64 + lane] = acc[i][j];
+      __syncthreads();
+    }
 #pragma unroll
     for (int i = 0; i < FM; ++i) {
+      if (KG > 1 && i / (FM / KG) != kg) continue;   // a group's share of the rows
       const int64_t m = cm + i * 16 + r16;
 #pragma unroll
       for (int p = 0; p < FN / 2; ++p) {
         const int64_t n = cn + 32 * p + 8 * g;
         float v[8];
+        if constexpr (KG == 1) {
 #pragma unroll
-        for (int e = 0; e < 8; ++e) v[e] = acc[i][2 * p + (e >> 2)][e & 3];
+          for (int e = 0; e < 8; ++e) v[e] = acc[i][2 * p + (e >> 2)][e & 3];
+        } else {
+          // the groups' sums, in their order
+#pragma unroll
+          for (int j = 0; j < 2; ++j) {
+            f32x4 u = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+            for (int k = 0; k < KG; ++k)
+              u += sums[(((k * kWaves + wave) * FM + i) * FN + 2 * p + j) * 64 + lane];
+#pragma unroll
+            for (int e = 0; e < 4; ++e) v[4 * j + e] = u[e];
+          }
+        }
         unsigned char *c = C + (m * ldc + n) * ES;
         if (inside && !accum) {
           store8<OE>(c, v, 8);
@@ -338,11 +386,11 @@ __global__ __launch_bounds__(64 * WM * WN) void mx4_tile_kernel(TileArgs ta) {
       }
     }
     id += gridDim.x;
-    if (id >= items) break;
+    if (KG > 1 || id >= items) break;
     // (an edge may have stored less than the next wait allows for)
     stored = inside && !accum;
     now = place(id);
-    t = now.first;
+    left = now.rounds();
     clear();
   }
   // the copies that nothing reads have landed
@@ -385,7 +433,7 @@ __global__ __launch_bounds__(256) void mx4_join_kernel(Mx4GemmArgs a, int splits
   }
 }
 
-template <int ELEM, int FM, int FN, int WM, int WN>
+template <int ELEM, int FM, int FN, int WM, int WN, int KG>
 hipError_t launch_tiles(const Mx4GemmArgs &a, int splits, hipStream_t stream, int num_cus) {
   constexpr int BM = 16 * FM * WM, BN = 16 * FN * WN;
   const int stages = (int)((mx4_groups(a.K) + 1) / 2);
@@ -393,10 +441,12 @@ hipError_t launch_tiles(const Mx4GemmArgs &a, int splits, hipStream_t stream, in
              (stages + splits - 1) / splits};
   t.splits = (stages + t.stages_per_split - 1) / t.stages_per_split;   // none empty
   // as many workgroups as the compute units' LDS holds
-  constexpr int kPerCu = BM + BN == 512 ? 1 : BM + BN == 256 ? 2 : 4;
+  constexpr int kPerCu = (160 << 10) / (2 * KG * ((BM + BN) * 136 + 128));
   const int64_t items = (int64_t)t.tiles_m * t.tiles_n * t.splits;
-  mx4_tile_kernel<ELEM, FM, FN, WM, WN>
-      <<<(unsigned)std::min<int64_t>(items, (int64_t)kPerCu * num_cus), 64 * WM * WN, 0, stream>>>(t);
+  // (groups of waves that share the contracted index take one item a workgroup)
+  mx4_tile_kernel<ELEM, FM, FN, WM, WN, KG>
+      <<<(unsigned)(KG > 1 ? items : std::min<int64_t>(items, (int64_t)kPerCu * num_cus)),
+         64 * WM * WN * KG, 0, stream>>>(t);
   return hipGetLastError();
 }
 
@@ -409,85 +459,112 @@ struct FewArgs {
   int64_t ldx;
 };
 
-// XE: the left operand's element type, or -1: in 4 bits already.  MF: blocks of 16 rows.
-template <int ELEM, int XE, int MF>
+// Up to four rows: four lanes each (row r16 / 4) hold eight values of a block, and bring
+// them together in registers; each row is then four columns of the products.
+template <int XE, bool kWhole>
+__device__ __forceinline__ u32x4 quad_codes(const unsigned char *row, int64_t col, int64_t K,
+                                            unsigned &byte) {
+  const int64_t at = col + (threadIdx.x & 3) * 8;
+  Raw8<XE> raw = Raw8<XE>{};
+  if (kWhole || at < K) raw = load8<XE>(row + at * 2, kWhole ? 8 : (int)min((int64_t)8, K - at));
+  float v[8];
+  unpack8<XE>(raw, v);
+  unsigned most = 0;
+#pragma unroll
+  for (int e = 0; e < 8; ++e) most = umax(most, abs_bits(v[e]));
+  most = quad_max(most);
+  byte = scale_byte(most);
+  const unsigned c = codes8(v, byte, __any(scale_low(most)));
+  return u32x4{dpp<0x00>(c), dpp<0x55>(c), dpp<0xAA>(c), dpp<0xFF>(c)};
+}
+
+// XE: the left operand's element type (of up to four rows), or -1: in 4 bits already.
+// MF: blocks of 16 rows; NB: blocks of 16 rows of B.  A wave takes pairs of groups of 128
+// values: whole lines.
+template <int ELEM, int XE, int MF, int NB>
 __global__ __launch_bounds__(64 * kFewWaves) void mx4_few_kernel(FewArgs fa) {
   const Mx4GemmArgs &a = fa.g;
-  __shared__ float sums[kFewWaves][MF * 256];
-  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+  __shared__ f32x4 sums[kFewWaves][NB][MF * 64];
+  const int lane = threadIdx.x & 63;
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int r16 = lane & 15, g = lane >> 4;
-  const int64_t n0 = (int64_t)blockIdx.x * 16;
+  const int64_t n0 = (int64_t)blockIdx.x * (16 * NB);
   const int groups = (int)mx4_groups(a.K);
-  const int64_t n = min(n0 + r16, a.N - 1);
-  const unsigned char *pb = a.B + n * a.ldb + g * 16;
-  const unsigned *ps = a.bs + n;
-  f32x4 acc[MF];
+  const unsigned char *pb[NB], *px[MF];
+  const unsigned *ps[NB], *pxs[MF];
 #pragma unroll
-  for (int f = 0; f < MF; ++f) acc[f] = f32x4{0.f, 0.f, 0.f, 0.f};
-  constexpr int U = 2;   // groups in flight
-  for (int t = wave; t < groups; t += kFewWaves * U) {
-    u32x4 w[U], x[U][MF];
-    unsigned ws[U], xs[U][MF];
+  for (int b = 0; b < NB; ++b) {
+    const int64_t n = min(n0 + b * 16 + r16, a.N - 1);
+    pb[b] = a.B + n * a.ldb + g * 16;
+    ps[b] = a.bs + n;
+  }
+#pragma unroll
+  for (int f = 0; f < MF; ++f) {
+    const int64_t m = min((int64_t)(f * 16 + (XE < 0 ? r16 : r16 >> 2)), a.M - 1);
+    px[f] = XE < 0 ? a.A + m * a.lda + g * 16 : fa.X + m * fa.ldx * 2;
+    pxs[f] = a.as + m;
+  }
+  f32x4 acc[MF][NB];
+#pragma unroll
+  for (int f = 0; f < MF; ++f)
+#pragma unroll
+    for (int b = 0; b < NB; ++b) acc[f][b] = f32x4{0.f, 0.f, 0.f, 0.f};
+  constexpr int U = 2;   // groups in flight (4: the same)
+  for (int t = wave * U; t < groups; t += kFewWaves * U) {
+    u32x4 w[U][NB], x[U][MF];
+    unsigned ws[U][NB], xs[U][MF];
 #pragma unroll
     for (int u = 0; u < U; ++u) {
-      const int k = t + u * kFewWaves;
-      const bool in = k < groups;
-      w[u] = in ? *(const u32x4 *)(pb + (int64_t)k * 64) : u32x4{0u, 0u, 0u, 0u};
-      ws[u] = in ? ps[(int64_t)k * a.ldbs] : 0u;
+      // (past the end: the last group with no scale)
+      const int k = min(t + u, groups - 1);
+#pragma unroll
+      for (int b = 0; b < NB; ++b) {
+        w[u][b] = *(const u32x4 *)(pb[b] + (int64_t)k * 64);
+        ws[u][b] = ps[b][(int64_t)k * a.ldbs];
+      }
     }
 #pragma unroll
     for (int u = 0; u < U; ++u) {
-      const int k = t + u * kFewWaves;
-      const bool in = k < groups;
+      const int k = min(t + u, groups - 1);
+      const bool in = t + u < groups;
 #pragma unroll
       for (int f = 0; f < MF; ++f) {
-        const int64_t m = min((int64_t)(f * 16 + r16), a.M - 1);
         if constexpr (XE < 0) {
-          x[u][f] = in ? *(const u32x4 *)(a.A + m * a.lda + (int64_t)k * 64 + g * 16)
-                       : u32x4{0u, 0u, 0u, 0u};
-          xs[u][f] = (in ? a.as[(int64_t)k * a.ldas + m] : 0u) >> (8 * g);
+          x[u][f] = *(const u32x4 *)(px[f] + (int64_t)k * 64);
+          xs[u][f] = pxs[f][(int64_t)k * a.ldas] >> (8 * g);
         } else {
-          // a lane's block of 32 values of its row, by itself
           const int64_t col = (int64_t)k * 128 + g * 32;
-          const unsigned char *p = fa.X + (m * fa.ldx + col) * 2;
-          Raw8<XE> raw[4];
-#pragma unroll
-          for (int d = 0; d < 4; ++d) {
-            const int64_t left = a.K - col - 8 * d;
-            raw[d] = Raw8<XE>{};
-            if (left > 0) raw[d] = load8<XE>(p + 16 * d, (int)min((int64_t)8, left));
-          }
-          float v[4][8];
-          unsigned most = 0;
-#pragma unroll
-          for (int d = 0; d < 4; ++d) {
-            unpack8<XE>(raw[d], v[d]);
-#pragma unroll
-            for (int e = 0; e < 8; ++e) most = umax(most, abs_bits(v[d][e]));
-          }
-          xs[u][f] = scale_byte(most);
-#pragma unroll
-          for (int d = 0; d < 4; ++d) x[u][f][d] = codes8(v[d], xs[u][f]);
+          x[u][f] = (int64_t)(k + 1) * 128 <= a.K
+                        ? quad_codes<XE, true>(px[f], col, a.K, xs[u][f])
+                        : quad_codes<XE, false>(px[f], col, a.K, xs[u][f]);
         }
+        if (!in) xs[u][f] = 0u;
       }
+#pragma unroll
+      for (int b = 0; b < NB; ++b) ws[u][b] = in ? ws[u][b] >> (8 * g) : 0u;
     }
 #pragma unroll
     for (int u = 0; u < U; ++u)
 #pragma unroll
       for (int f = 0; f < MF; ++f)
-        acc[f] = mfma_k128<0>(w[u], x[u][f], acc[f], ws[u] >> (8 * g), xs[u][f]);
+#pragma unroll
+        for (int b = 0; b < NB; ++b)
+          acc[f][b] = mfma_k128<0>(w[u][b], x[u][f], acc[f][b], ws[u][b], xs[u][f]);
   }
   // lane: columns 4 g .. of row r16 of a block
 #pragma unroll
-  for (int f = 0; f < MF; ++f) *(f32x4 *)&sums[wave][(f * 16 + r16) * 16 + 4 * g] = acc[f];
+  for (int f = 0; f < MF; ++f)
+#pragma unroll
+    for (int b = 0; b < NB; ++b) sums[wave][b][(f * 16 + r16) * 4 + g] = acc[f][b];
   __syncthreads();
   // four columns of a row a thread, the waves' sums in their order
-  const int t = threadIdx.x;
-  if (t < MF * 64) {
+  for (int t = threadIdx.x; t < NB * MF * 64; t += 64 * kFewWaves) {
+    const int b = t / (MF * 64), i = t % (MF * 64);
     f32x4 v = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-    for (int i = 0; i < kFewWaves; ++i) v += *(const f32x4 *)&sums[i][t * 4];
-    const int64_t m = t >> 2, c = n0 + (t & 3) * 4;
+    for (int k = 0; k < kFewWaves; ++k) v += sums[k][b][i];
+    if (XE >= 0 && (i >> 2 & 3) != 0) continue;
+    const int64_t m = XE < 0 ? i >> 2 : i >> 4, c = n0 + b * 16 + (i & 3) * 4;
     const int valid = (int)min((int64_t)4, a.N - c);
     if (m < a.M && valid > 0)
       store4<ELEM>((unsigned char *)a.C + (m * a.ldc + c) * elem_bytes<ELEM>, v, valid, a.accum);
@@ -504,13 +581,27 @@ hipError_t launch_few_rows(const FewArgs &args, hipStream_t stream) {
     f.g.B += n * f.g.ldb;
     f.g.bs += n;
     f.g.C = (unsigned char *)f.g.C + n * elem_bytes<ELEM>;
-    const unsigned blocks = (unsigned)((f.g.N + 15) / 16);
-    if (f.g.M <= 16)
-      mx4_few_kernel<ELEM, XE, 1><<<blocks, threads, 0, stream>>>(f);
-    else if (f.g.M <= 32)
-      mx4_few_kernel<ELEM, XE, 2><<<blocks, threads, 0, stream>>>(f);
+    const auto go = [&](auto mf, auto nb) {
+      constexpr int MF = decltype(mf)::value, NB = decltype(nb)::value;
+      mx4_few_kernel<ELEM, XE, MF, NB>
+          <<<(unsigned)((f.g.N + 16 * NB - 1) / (16 * NB)), threads, 0, stream>>>(f);
+    };
+    const auto rows = [&](auto nb) {
+      if (XE >= 0 || f.g.M <= 16)
+        go(std::integral_constant<int, 1>{}, nb);
+      else if (f.g.M <= 32)
+        go(std::integral_constant<int, 2>{}, nb);
+      else
+        go(std::integral_constant<int, 4>{}, nb);
+    };
+    // Two blocks of B's rows share what is read of the left operand, where workgroups are
+    // left for the chip (us, N = K = 8192, one block / two: 16 rows 11.9 / 10.9, 32 16.0 /
+    // 13.9, one 16-bit row 12.8 / 10.5, one row in 4 bits 9.9 / 11.1; 16 x 4096 x 4096 4.5 /
+    // 6.8).
+    if (f.g.N >= 8192 && (XE >= 0 || f.g.M > 8))
+      rows(std::integral_constant<int, 2>{});
     else
-      mx4_few_kernel<ELEM, XE, 4><<<blocks, threads, 0, stream>>>(f);
+      rows(std::integral_constant<int, 1>{});
     const hipError_t e = hipGetLastError();
     if (e != hipSuccess) return e;
   }
@@ -518,52 +609,110 @@ hipError_t launch_few_rows(const FewArgs &args, hipStream_t stream) {
 }
 
 // ------------------------------------------------------------------------ plan
+// The few-row kernel's time in microseconds (us, that / measured, B from memory: 16 x 4096 x
+// 4096 4.8 / 4.5, 32 x 8192 x 8192 13.9 / 13.9, 64 x 1024 x 4096 4.0 / 4.4, 64 x 4096 x 4096 7.9
+// / 8.3, 64 x 8192 x 4096 13.3 / 15.2).  The tiles' time below is fitted on B in the caches;
+// from memory they take longer, the fewer rows share it (32 x 8192 x 8192 12.9 and 15.9).
 constexpr int64_t kFewMax = 64;
-
-// Where C has few tiles, ranges of the contracted index, each of at least four stages.
-constexpr int kMaxCus = 256;
-int splits_of(int64_t tiles, int64_t K, int num_cus) {
-  const int64_t stages = (mx4_groups(K) + 1) / 2;
-  return (int)std::max<int64_t>(1, std::min<int64_t>({std::min(num_cus, kMaxCus) / std::max<int64_t>(tiles, 1),
-                                                      stages / 4, 16}));
+double few_us(int64_t M, int64_t K, int64_t N) {
+  const double strips = N >= 8192 ? N / 4200.0 : std::max(1.0, N / 3500.0);
+  return 2.4 + K / 1024.0 * (0.3 + 0.0135 * M) * strips;
 }
-int64_t tiles_of(int64_t M, int64_t N, int64_t bm, int64_t bn) {
-  return ((M + bm - 1) / bm) * ((N + bn - 1) / bn);
+double cold_us(int64_t K, int64_t N) { return K * N * 0.5 * 8e-8; }
+// Rows that a linear layer's few-row kernel brings to 4 bits itself: above, a workgroup's
+// own conversions cost more than their launch (4096 x 4096: 4 rows 4.9 us against 4.2 + 3.9).
+constexpr int64_t kFewOwn = 4, kFewOwnK = 32768;
+
+// The tile kernel's variants and what their time in microseconds is made of: a call, a
+// round of stages on a compute unit that has room (`alone`) and where all are full (for
+// each item of a compute unit), the stores of an item.  Fitted to 96 products of 16 to
+// 4096 rows, K 512, 2048 and 8192: 6 % off in the mean; the variant it picks is 0.6 % slower
+// than the fastest.
+struct Variant {
+  int tile, groups, per_cu;
+  double call, alone, full, item;
+};
+constexpr Variant kVariants[] = {{256, 1, 1, 1.3, 1.28, 1.79, 7.6}, {128, 1, 2, 2.4, 1.10, 0.95, 2.4},
+                                 {128, 2, 1, 1.6, 0.83, 1.16, 5.6}, {64, 1, 4, 2.4, 0.70, 0.29, 1.6},
+                                 {64, 2, 2, 1.0, 0.65, 0.53, 4.0},  {64, 4, 1, 1.9, 0.70, 0.94, 4.0}};
+
+int64_t tiles_of(int64_t M, int64_t N, int64_t tile) {
+  return ((M + tile - 1) / tile) * ((N + tile - 1) / tile);
+}
+double tiles_us(const Variant &v, int64_t M, int64_t N, int64_t stages, int num_cus) {
+  const double items = (double)tiles_of(M, N, v.tile), full = items / num_cus;
+  const double batches = std::ceil(std::ceil(full) / v.per_cu);
+  return v.call + std::ceil((double)stages / v.groups) * std::max(batches * v.alone, full * v.full) +
+         batches * v.item;
 }
 
+// Ranges of the contracted index where C has few tiles and it is long: the last variant
+// for each, their sums added by a second launch (us: 100 x 65536 x 64 15.2, 512 x
+// 65536 x 512 27; uncut 46 and 93 by the times below).
+constexpr int64_t kRangeValues = (int64_t)1 << 22;   // of all ranges' sums, at most
+int ranges_of(int64_t M, int64_t N, int64_t stages, int num_cus, double &us) {
+  int best = 1;
+  for (int s = 2; s <= 16 && s * M * N <= kRangeValues && stages / s >= 16; s *= 2) {
+    const double t = tiles_us(kVariants[5], M * s, N, (stages + s - 1) / s, num_cus) + 3.0 +
+                     s * M * N * 2e-6;
+    if (t < us) {
+      us = t;
+      best = s;
+    }
+  }
+  return best;
+}
+
+template <int ELEM>
+hipError_t tiles(int variant, const Mx4GemmArgs &a, int splits, hipStream_t stream, int num_cus) {
+  switch (variant) {
+    case 0: return launch_tiles<ELEM, 8, 4, 2, 4, 1>(a, splits, stream, num_cus);
+    case 1: return launch_tiles<ELEM, 4, 4, 2, 2, 1>(a, splits, stream, num_cus);
+    case 2: return launch_tiles<ELEM, 4, 4, 2, 2, 2>(a, splits, stream, num_cus);
+    case 3: return launch_tiles<ELEM, 4, 2, 1, 2, 1>(a, splits, stream, num_cus);
+    case 4: return launch_tiles<ELEM, 4, 2, 1, 2, 2>(a, splits, stream, num_cus);
+    default: return launch_tiles<ELEM, 4, 2, 1, 2, 4>(a, splits, stream, num_cus);
+  }
+}
+
+template <int ELEM>
+hipError_t join(const Mx4GemmArgs &a, int splits, hipStream_t stream, int num_cus) {
+  const int64_t blocks = std::min<int64_t>((a.M * a.N + 1023) / 1024, 4 * num_cus);
+  mx4_join_kernel<ELEM><<<(unsigned)blocks, 256, 0, stream>>>(a, splits);
+  return hipGetLastError();
+}
 
 template <int ELEM>
 hipError_t gemm(const Mx4GemmArgs &a, hipStream_t stream, int num_cus) {
-  const int64_t blocks = std::min<int64_t>((a.M * a.N + 1023) / 1024, 4 * num_cus);
-  if (a.K == 0) {   // zeros: the sums of no ranges
-    mx4_join_kernel<ELEM><<<(unsigned)blocks, 256, 0, stream>>>(a, 0);
-    return hipGetLastError();
+  if (a.K == 0) return join<ELEM>(a, 0, stream, num_cus);   // zeros: the sums of no ranges
+  const int64_t stages = (mx4_groups(a.K) + 1) / 2;
+  int best = 0;
+  double us = 1e300;
+  for (int i = 0; i < 6; ++i) {
+    const double t = tiles_us(kVariants[i], a.M, a.N, stages, num_cus);
+    if (t < us) {
+      us = t;
+      best = i;
+    }
   }
-  if (a.M <= kFewMax) return launch_few_rows<ELEM, -1>(FewArgs{a, nullptr, 0}, stream);
-  if (tiles_of(a.M, a.N, 256, 256) >= num_cus)
-    return launch_tiles<ELEM, 8, 4, 2, 4>(a, 1, stream, num_cus);
-  const int64_t tiles = tiles_of(a.M, a.N, 128, 128);
-  if (tiles < num_cus && tiles_of(a.M, a.N, 64, 64) <= 4 * num_cus && mx4_groups(a.K) < 32)
-    return launch_tiles<ELEM, 4, 2, 1, 2>(a, 1, stream, num_cus);
-  const int splits = splits_of(tiles, a.K, num_cus);
-  if (splits == 1) return launch_tiles<ELEM, 4, 4, 2, 2>(a, 1, stream, num_cus);
-  const hipError_t e = launch_tiles<kPart, 4, 4, 2, 2>(a, splits, stream, num_cus);
+  const int splits = ranges_of(a.M, a.N, stages, num_cus, us);
+  if (a.M <= kFewMax && few_us(a.M, a.K, a.N) < us + cold_us(a.K, a.N))
+    return launch_few_rows<ELEM, -1>(FewArgs{a, nullptr, 0}, stream);
+  if (splits == 1) return tiles<ELEM>(best, a, 1, stream, num_cus);
+  const hipError_t e = launch_tiles<kPart, 4, 2, 1, 2, 4>(a, splits, stream, num_cus);
   if (e != hipSuccess) return e;
-  const int stages = (int)((mx4_groups(a.K) + 1) / 2), per = (stages + splits - 1) / splits;
-  mx4_join_kernel<ELEM><<<(unsigned)blocks, 256, 0, stream>>>(a, (stages + per - 1) / per);
-  return hipGetLastError();
+  const int per = (int)((stages + splits - 1) / splits);
+  return join<ELEM>(a, (int)((stages + per - 1) / per), stream, num_cus);
 }
 
 int64_t up16(int64_t n) { return (n + 15) / 16 * 16; }
 
 }  // namespace
 
-// X in 4 bits and its scales, then the ranges' sums: up to 16 ranges, and of few
-// tiles up to one a compute unit.
+// X in 4 bits and its scales, then the ranges' sums.
 int64_t mx4_work_bytes(int64_t M, int64_t K, int64_t N) {
   const int64_t x = M * mx4_row_bytes(K) + up16(4 * mx4_groups(K) * M);
-  constexpr int64_t kMost = (int64_t)kMaxCus * 128 * 128;
-  return x + (M * N < kMost / 16 ? 16 * M * N : kMost) * 4;
+  return x + (M * N < kRangeValues / 16 ? 16 * M * N : kRangeValues) * 4;
 }
 
 hipError_t launch_mx4_gemm(int elem, const Mx4GemmArgs &a, hipStream_t stream, int num_cus) {
@@ -577,7 +726,7 @@ hipError_t launch_mx4_gemm(int elem, const Mx4GemmArgs &a, hipStream_t stream, i
 hipError_t launch_mx4_linear(int xelem, const void *X, int64_t ldx, int elem,
                              const Mx4GemmArgs &args, hipStream_t stream, int num_cus) {
   Mx4GemmArgs a = args;
-  if (a.M <= 4) {
+  if (a.M <= kFewOwn && a.K > 0 && a.K <= kFewOwnK) {
     const FewArgs f{a, (const unsigned char *)X, ldx};
     if (xelem == TCU_ELEM_F16)
       return elem == TCU_ELEM_F32 ? launch_few_rows<TCU_ELEM_F32, TCU_ELEM_F16>(f, stream)
