@@ -28,39 +28,46 @@ constexpr int kWaves = 4;
 
 // V elements as stored, at any element-aligned address.
 template <int ELEM, int V>
-__device__ __forceinline__ void load_run(const unsigned char *p, float (&x)[V]) {
-  constexpr int ES = elem_bytes<ELEM>;
-  if constexpr (V == 8) {
-    const Raw8<ELEM> r = load8<ELEM>(p, 8);
-    unpack8<ELEM>(r, x);
-  } else if constexpr (V * ES >= 4) {
-    unsigned w[V * ES / 4];
-    if constexpr (V * ES == 16) {
-      const u32x4 v = load16_any(p);
+struct Run {
+  static constexpr int kBytes = V * elem_bytes<ELEM>, kWords = kBytes < 4 ? 1 : kBytes / 4;
+  unsigned w[kWords];
+};
+template <int ELEM, int V>
+__device__ __forceinline__ Run<ELEM, V> load_run(const unsigned char *p) {
+  Run<ELEM, V> r;
+  constexpr int B = Run<ELEM, V>::kBytes;
+  if constexpr (B >= 16) {
 #pragma unroll
-      for (int i = 0; i < 4; ++i) w[i] = v[i];
-    } else if constexpr (V * ES == 8) {
-      typedef u32x2 u32x2_any __attribute__((aligned(1)));
-      const u32x2 v = *(const u32x2_any *)p;
-      w[0] = v[0];
-      w[1] = v[1];
-    } else {
-      w[0] = load4_any(p);
-    }
+    for (int i = 0; i < B / 16; ++i) {
+      const u32x4 v = load16_any(p + 16 * i);
 #pragma unroll
-    for (int e = 0; e < V; ++e) {
-      if constexpr (ELEM == TCU_ELEM_F32) {
-        x[e] = bitcast<float>(w[e]);
-      } else {
-        const unsigned half = (w[e >> 1] >> (16 * (e & 1))) & 0xffffu;
-        if constexpr (ELEM == TCU_ELEM_F16)
-          x[e] = (float)bitcast<_Float16>((unsigned short)half);
-        else
-          x[e] = bf16_to_f32(half);
-      }
+      for (int d = 0; d < 4; ++d) r.w[4 * i + d] = v[d];
     }
+  } else if constexpr (B == 8) {
+    typedef u32x2 u32x2_any __attribute__((aligned(1)));
+    const u32x2 v = *(const u32x2_any *)p;
+    r.w[0] = v[0];
+    r.w[1] = v[1];
+  } else if constexpr (B == 4) {
+    r.w[0] = load4_any(p);
   } else {
-    x[0] = elem_to_f32<ELEM>(p);
+    r.w[0] = *(const unsigned short *)p;
+  }
+  return r;
+}
+template <int ELEM, int V>
+__device__ __forceinline__ void unpack(const Run<ELEM, V> &r, float (&x)[V]) {
+#pragma unroll
+  for (int e = 0; e < V; ++e) {
+    if constexpr (ELEM == TCU_ELEM_F32) {
+      x[e] = bitcast<float>(r.w[e]);
+    } else {
+      const unsigned half = (r.w[e >> 1] >> (16 * (e & 1))) & 0xffffu;
+      if constexpr (ELEM == TCU_ELEM_F16)
+        x[e] = (float)bitcast<_Float16>((unsigned short)half);
+      else
+        x[e] = bf16_to_f32(half);
+    }
   }
 }
 
@@ -74,11 +81,9 @@ __device__ __forceinline__ void store_run(unsigned char *p, const float (&x)[V])
 #pragma unroll
     for (int e = 0; e < 8; ++e) v[e] = e < V ? x[e] : 0.f;
     const Raw8<ELEM> r = pack8<ELEM>(v);
-    if constexpr (V == 8) {
+    if constexpr (V * ES >= 16) {
 #pragma unroll
-      for (int i = 0; i < ES / 2; ++i) store16_any(p + 16 * i, r.v[i]);
-    } else if constexpr (V * ES == 16) {
-      store16_any(p, r.v[0]);
+      for (int i = 0; i < V * ES / 16; ++i) store16_any(p + 16 * i, r.v[i]);
     } else if constexpr (V * ES == 8) {
       typedef u32x2 u32x2_any __attribute__((aligned(1)));
       *(u32x2_any *)p = u32x2{r.v[0][0], r.v[0][1]};
@@ -150,8 +155,19 @@ __device__ __forceinline__ void turn(float (&lo)[V], float (&hi)[V], const float
   }
 }
 
+// The sum over L lanes, a power of two, for each of them.  (L is the same for all lanes of
+// a launch: the steps not taken are branches.)
+template <int kCtrl>
+__device__ __forceinline__ float add_dpp(float v) {
+  return v + bitcast<float>(__builtin_amdgcn_mov_dpp(bitcast<int>(v), kCtrl, 0xf, 0xf, true));
+}
 __device__ __forceinline__ float group_sum(float v, int L) {
-  for (int m = 1; m < L; m <<= 1) v += __shfl_xor(v, m);
+  if (L > 1) v = add_dpp<0xB1>(v);    // lanes 1 0 3 2 of a quad
+  if (L > 2) v = add_dpp<0x4E>(v);    // lanes 2 3 0 1
+  if (L > 4) v = add_dpp<0x141>(v);   // 8 lanes mirrored: the other quad
+  if (L > 8) v = add_dpp<0x140>(v);   // 16 lanes mirrored: the other eight
+  if (L > 16) v += __shfl_xor(v, 16);
+  if (L > 32) v += __shfl_xor(v, 32);
   return v;
 }
 
@@ -161,16 +177,20 @@ __device__ __forceinline__ float rstd_of(float sum_sq, int dim, float eps) {
   return v == 0.f ? 0.f : 1.f / sqrtf(v);
 }
 
-// A token's pairs of one lane: slots lane % L + 64 i (kP > 1: L is 64).
+// A token's pairs of one lane: slots lane % L + 64 i (kP > 1: L is 64).  The next heads'
+// values are on their way while a wave's heads are worked on.
 template <int ELEM, int V, int kP, bool kGrad>
 __global__ __launch_bounds__(64 * kWaves) void heads_kernel(QkNormArgs a, int L, int64_t token_tasks,
                                                           int head_tasks, int heads_per_task) {
   constexpr int ES = elem_bytes<ELEM>;
-  __shared__ float tables[kWaves][2][kAngles];
-  __shared__ float sums[kGrad ? kWaves : 1][2][kGrad ? TCU_MAX_HEAD_DIM : 1];
+  // tables of angles, or the gradient's sums of 16 lanes and more: kWaves x 64 / max(L, 16)
+  // x 2 dim values, dim at most 2 V kP L
+  constexpr int kTables = kWaves * 2 * kAngles, kSums = kGrad ? kWaves * 256 * V * kP : 0;
+  __shared__ float lds[kTables > kSums ? kTables : kSums];
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
   const int j0 = lane & (L - 1), sub = lane / L, at_once = 64 / L;
   const int H = a.heads[0] + a.heads[1];
+  float *const cosines = lds + wave * 2 * kAngles, *const sines = cosines + kAngles;
 
   Slot slot[kP];
 #pragma unroll
@@ -185,17 +205,51 @@ __global__ __launch_bounds__(64 * kWaves) void heads_kernel(QkNormArgs a, int L,
         for (int e = 0; e < V; ++e) dw[s][i][0][e] = dw[s][i][1][e] = 0.f;
   }
 
-  const int64_t tasks = token_tasks * head_tasks;
-  for (int64_t task = (int64_t)blockIdx.x * kWaves + wave; task < tasks;
-       task += (int64_t)gridDim.x * kWaves) {
-    const int64_t token = task / head_tasks;
-    const int h0 = (int)(task - token * head_tasks) * heads_per_task;
+  typedef Run<ELEM, V> R;
+  R rx[kP][2], rw[kP][2], rd[kGrad ? kP : 1][2];
+  // head h's values of x, its weights' and the gradient's (lanes without one: zeros)
+  auto fetch = [&](int64_t token, int h, int end) {
+    const int which = h >= a.heads[0] ? 1 : 0;
+    const int64_t hh = which ? h - a.heads[0] : h;
+    const Heads hx = which ? a.x[1] : a.x[0];
+    const unsigned char *px = (const unsigned char *)hx.p + (token * hx.ld + hh * hx.hd) * ES;
+    const unsigned char *pw = (const unsigned char *)(which ? a.w[1] : a.w[0]);
+    const Heads hd = which ? a.dy[1] : a.dy[0];
+    const unsigned char *pd = (const unsigned char *)hd.p + (token * hd.ld + hh * hd.hd) * ES;
+#pragma unroll
+    for (int i = 0; i < kP; ++i) {
+#pragma unroll
+      for (int r = 0; r < 2; ++r) {
+        rx[i][r] = rw[i][r] = R{};
+        if constexpr (kGrad) rd[i][r] = R{};
+      }
+      if (h < end && slot[i].in) {
+        rx[i][0] = load_run<ELEM, V>(px + slot[i].lo * ES);
+        rw[i][0] = load_run<ELEM, V>(pw + slot[i].lo * ES);
+        if constexpr (kGrad) rd[i][0] = load_run<ELEM, V>(pd + slot[i].lo * ES);
+        if (slot[i].two) {
+          rx[i][1] = load_run<ELEM, V>(px + slot[i].hi * ES);
+          rw[i][1] = load_run<ELEM, V>(pw + slot[i].hi * ES);
+          if constexpr (kGrad) rd[i][1] = load_run<ELEM, V>(pd + slot[i].hi * ES);
+        }
+      }
+    }
+  };
+
+  const int64_t tasks = token_tasks * head_tasks, stride = (int64_t)gridDim.x * kWaves;
+  int64_t task = (int64_t)blockIdx.x * kWaves + wave;
+  int64_t token = task / head_tasks;
+  int h0 = (int)(task - token * head_tasks) * heads_per_task;
+  if (task < tasks) fetch(token, h0 + sub, min(H, h0 + heads_per_task));
+  while (task < tasks) {
     const int h1 = min(H, h0 + heads_per_task);
+    const int64_t next_task = task + stride;
+    const int64_t next_token = next_task / head_tasks;
+    const int next_h0 = (int)(next_task - next_token * head_tasks) * heads_per_task;
     float c[kP][V], s[kP][V];
     if (a.rot > 0) {
       const int pos = a.pos[token];
-      for (int i = lane; i < a.rot / 2; i += 64)
-        angle_of(pos, a.freq[i], tables[wave][0][i], tables[wave][1][i]);
+      for (int i = lane; i < a.rot / 2; i += 64) angle_of(pos, a.freq[i], cosines[i], sines[i]);
       // the wave's own values: in order, once they are written
       asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
     }
@@ -204,8 +258,8 @@ __global__ __launch_bounds__(64 * kWaves) void heads_kernel(QkNormArgs a, int L,
 #pragma unroll
       for (int e = 0; e < V; ++e) {
         const int at = (j0 + 64 * i) * V + e;
-        c[i][e] = slot[i].turned ? tables[wave][0][at] : 1.f;
-        s[i][e] = slot[i].turned ? tables[wave][1][at] : 0.f;
+        c[i][e] = slot[i].turned ? cosines[at] : 1.f;
+        s[i][e] = slot[i].turned ? sines[at] : 0.f;
       }
     asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");   // read before the next token's are written
 
@@ -214,36 +268,24 @@ __global__ __launch_bounds__(64 * kWaves) void heads_kernel(QkNormArgs a, int L,
       const bool live = h < h1;
       const int which = h >= a.heads[0] && live ? 1 : 0;
       const int64_t hh = which ? h - a.heads[0] : h;
-      const Heads hx = which ? a.x[1] : a.x[0];
-      const unsigned char *px = (const unsigned char *)hx.p + (token * hx.ld + hh * hx.hd) * ES;
-      const unsigned char *pw = (const unsigned char *)(which ? a.w[1] : a.w[0]);
       float x[kP][2][V], w[kP][2][V], d[kP][2][V];
       float sq = 0.f;
 #pragma unroll
       for (int i = 0; i < kP; ++i) {
 #pragma unroll
-        for (int e = 0; e < V; ++e) x[i][0][e] = x[i][1][e] = w[i][0][e] = w[i][1][e] = 0.f;
-        if (live && slot[i].in) {
-          load_run<ELEM, V>(px + slot[i].lo * ES, x[i][0]);
-          load_run<ELEM, V>(pw + slot[i].lo * ES, w[i][0]);
-          if (slot[i].two) {
-            load_run<ELEM, V>(px + slot[i].hi * ES, x[i][1]);
-            load_run<ELEM, V>(pw + slot[i].hi * ES, w[i][1]);
-          }
-        }
-        if constexpr (kGrad) {
+        for (int r = 0; r < 2; ++r) {
+          unpack<ELEM, V>(rx[i][r], x[i][r]);
+          unpack<ELEM, V>(rw[i][r], w[i][r]);
+          if constexpr (kGrad) unpack<ELEM, V>(rd[i][r], d[i][r]);
 #pragma unroll
-          for (int e = 0; e < V; ++e) d[i][0][e] = d[i][1][e] = 0.f;
-          const Heads hd = which ? a.dy[1] : a.dy[0];
-          const unsigned char *pd = (const unsigned char *)hd.p + (token * hd.ld + hh * hd.hd) * ES;
-          if (live && slot[i].in) {
-            load_run<ELEM, V>(pd + slot[i].lo * ES, d[i][0]);
-            if (slot[i].two) load_run<ELEM, V>(pd + slot[i].hi * ES, d[i][1]);
-          }
+          for (int e = 0; e < V; ++e) sq += x[i][r][e] * x[i][r][e];
         }
-#pragma unroll
-        for (int e = 0; e < V; ++e) sq += x[i][0][e] * x[i][0][e] + x[i][1][e] * x[i][1][e];
       }
+      // (in place, nobody's outputs are another's inputs)
+      if (hb + at_once < h1)
+        fetch(token, h + at_once, h1);
+      else if (next_task < tasks)
+        fetch(next_token, next_h0 + sub, min(H, next_h0 + heads_per_task));
       const float rstd = rstd_of(group_sum(sq, L), a.dim, a.eps);
       const Heads hy = which ? a.y[1] : a.y[0];
       unsigned char *py = (unsigned char *)hy.p + (token * hy.ld + hh * hy.hd) * ES;
@@ -257,21 +299,37 @@ __global__ __launch_bounds__(64 * kWaves) void heads_kernel(QkNormArgs a, int L,
           if (slot[i].turned) turn<V>(x[i][0], x[i][1], c[i], s[i], a.adjacent, 1.f);
         }
       } else {
+        // (no head's values in the other weights' sums, also where they are not finite)
+        const bool all_q = h1 <= a.heads[0] || hb + at_once <= a.heads[0];
+        const bool all_k = hb >= a.heads[0];
         float gn = 0.f;
 #pragma unroll
         for (int i = 0; i < kP; ++i) {
           if (slot[i].turned) turn<V>(d[i][0], d[i][1], c[i], s[i], a.adjacent, -1.f);
 #pragma unroll
-          for (int r = 0; r < 2; ++r)
+          for (int r = 0; r < 2; ++r) {
+            float t[V];
 #pragma unroll
             for (int e = 0; e < V; ++e) {
               x[i][r][e] *= rstd;
-              const float t = d[i][r][e] * x[i][r][e];
-              dw[0][i][r][e] += which ? 0.f : t;
-              dw[1][i][r][e] += which ? t : 0.f;
+              t[e] = d[i][r][e] * x[i][r][e];
               d[i][r][e] *= w[i][r][e];
               gn += d[i][r][e] * x[i][r][e];
             }
+            if (all_q) {
+#pragma unroll
+              for (int e = 0; e < V; ++e) dw[0][i][r][e] += t[e];
+            } else if (all_k) {
+#pragma unroll
+              for (int e = 0; e < V; ++e) dw[1][i][r][e] += t[e];
+            } else {
+#pragma unroll
+              for (int e = 0; e < V; ++e) {
+                dw[0][i][r][e] += which ? 0.f : t[e];
+                dw[1][i][r][e] += which ? t[e] : 0.f;
+              }
+            }
+          }
         }
         const float mean = group_sum(gn, L) / (float)a.dim;
 #pragma unroll
@@ -289,10 +347,16 @@ __global__ __launch_bounds__(64 * kWaves) void heads_kernel(QkNormArgs a, int L,
         }
       }
     }
+    task = next_task;
+    token = next_token;
+    h0 = next_h0;
   }
 
   if constexpr (kGrad) {
-    // the wave's lanes of one slot, then the waves
+    // a wave's lanes of one slot: those of 16 in registers, the rest and the waves in LDS
+    const int rows = L >= 64 ? 1 : L == 32 ? 2 : 4, span = L > 16 ? L : 16;
+    float *const mine = lds + (wave * rows + lane / span) * 2 * a.dim;
+    __syncthreads();   // the tables are read
 #pragma unroll
     for (int s = 0; s < 2; ++s)
 #pragma unroll
@@ -302,35 +366,38 @@ __global__ __launch_bounds__(64 * kWaves) void heads_kernel(QkNormArgs a, int L,
 #pragma unroll
           for (int e = 0; e < V; ++e) {
             float v = dw[s][i][r][e];
-            for (int m = L; m < 64; m <<= 1) v += __shfl_xor(v, m);
+            if (L <= 1) v = add_dpp<0x121>(v);   // 16 lanes turned by 1, 2, 4 and 8
+            if (L <= 2) v = add_dpp<0x122>(v);
+            if (L <= 4) v = add_dpp<0x124>(v);
+            if (L <= 8) v = add_dpp<0x128>(v);
             const int at = (r ? slot[i].hi : slot[i].lo) + e;
-            if (sub == 0 && (r ? slot[i].two : slot[i].in)) sums[wave][s][at] = v;
+            if (lane % span < L && (r ? slot[i].two : slot[i].in)) mine[s * a.dim + at] = v;
           }
     __syncthreads();
     for (int i = threadIdx.x; i < 2 * a.dim; i += 64 * kWaves) {
-      const int s = i >= a.dim, at = i - s * a.dim;
       float v = 0.f;
-#pragma unroll
-      for (int k = 0; k < kWaves; ++k) v += sums[k][s][at];
+      for (int k = 0; k < kWaves * rows; ++k) v += lds[k * 2 * a.dim + i];
       a.parts[(int64_t)blockIdx.x * 2 * a.dim + i] = v;
     }
   }
 }
 
-// dw: the parts' sums, 16 threads to a column, each in their order.
-__global__ __launch_bounds__(256) void head_dw_kernel(QkNormArgs a, int parts) {
-  __shared__ float sums[16][17];
+// dw: the parts' sums, 64 threads to a column, each in their order.
+__global__ __launch_bounds__(1024) void head_dw_kernel(QkNormArgs a, int parts) {
+  __shared__ float sums[64][17];
   const int col = threadIdx.x & 15, seg = threadIdx.x >> 4;
   const int i = blockIdx.x * 16 + col;
   float v = 0.f;
-  if (i < 2 * a.dim)
-    for (int p = seg; p < parts; p += 16) v += a.parts[(int64_t)p * 2 * a.dim + i];
+  if (i < 2 * a.dim) {
+#pragma unroll 4
+    for (int p = seg; p < parts; p += 64) v += a.parts[(int64_t)p * 2 * a.dim + i];
+  }
   sums[seg][col] = v;
   __syncthreads();
   if (seg == 0 && i < 2 * a.dim) {
     v = 0.f;
 #pragma unroll
-    for (int s = 0; s < 16; ++s) v += sums[s][col];
+    for (int s = 0; s < 64; ++s) v += sums[s][col];
     const int s = i >= a.dim;
     float *dw = s ? a.dw[1] : a.dw[0];
     if (dw) dw[i - s * a.dim] = v;
@@ -357,7 +424,7 @@ hipError_t launch(const QkNormArgs &a, hipStream_t stream, int num_cus) {
       a, L, a.tokens, tasks_h, per_task);
   hipError_t e = hipGetLastError();
   if (e != hipSuccess || !kGrad) return e;
-  head_dw_kernel<<<(unsigned)((2 * a.dim + 15) / 16), 256, 0, stream>>>(a, (int)blocks);
+  head_dw_kernel<<<(unsigned)((2 * a.dim + 15) / 16), 1024, 0, stream>>>(a, (int)blocks);
   return hipGetLastError();
 }
 
