@@ -8,14 +8,19 @@
 // memory: every value is read once, held in registers and written once.
 //   * A head is L lanes', a power of two; a lane holds V pairs as two runs of V
 //     elements: where the pairs are half the rotated part apart the runs are, and where
-//     they are adjacent both runs hold whole pairs.  V is 8 where the sizes allow whole
-//     vectors, down to 1 for any size; heads that need more than 64 lanes of one pair
-//     have kP pairs a lane.
-//   * A wave takes a token and as many of its heads at once as fit, queries and keys in
-//     one sequence; the angles are formed once a token, one lane each, in binary64 (a
-//     far position's angle has no digits left in binary32), and shared through LDS.
+//     they are adjacent both runs hold whole pairs.  V is 8, whole vectors: where a part is
+//     no whole number of them its last slot begins earlier, and what it shares with the slot
+//     before it is left out of the sums and stored twice with the same value.  Heads
+//     whose parts are shorter than two vectors have V = 1, and kP slots a lane if they
+//     need more than 64.
+//   * A wave takes a few tokens, or a part of one token's heads where tokens are few, and as
+//     many heads at once as fit, queries and keys in one sequence; the angles are formed
+//     once a token, one lane each, in binary64 (a far position's angle has no digits left
+//     in binary32), and shared through LDS.
 //   * The weights' gradients are summed in registers over a workgroup's tokens, and the
 //     workgroups' parts by a second launch, in their order.
+// 16384 tokens of 72 heads of 128 bf16 124 us, 4.9 TB/s; gradients of 8192 tokens of 40 heads 52
+// + 4.8 us, 4.7 TB/s; a copy 5.0.
 #include <algorithm>
 
 #include "tcu_elem.h"
@@ -93,25 +98,33 @@ __device__ __forceinline__ void store_run(unsigned char *p, const float (&x)[V])
   }
 }
 
-// Slot j's two runs, and whether they are rotated.  An odd head's last slot has no
-// second run (one pair a slot).
+// Slot j's two runs, and whether they are rotated.  An odd head's last slot has no second
+// run (V = 1); the first `skip` values of a run are another slot's too (V = 8).
 struct Slot {
-  int lo, hi;
+  int lo, hi, skip_lo, skip_hi, at;   // at: the first pair's angle
   bool in, two, turned;
 };
 template <int V>
 __device__ __forceinline__ Slot slot_of(int j, int dim, int rot, bool adjacent) {
   Slot s;
-  const int turned = rot / (2 * V);
+  const int turned = (rot / 2 + V - 1) / V, rest = (dim - rot + 2 * V - 1) / (2 * V);
   s.turned = j < turned;
-  if (s.turned) {
-    s.lo = adjacent ? 2 * V * j : V * j;
-    s.hi = adjacent ? s.lo + V : s.lo + rot / 2;
+  s.in = j < turned + rest;
+  s.skip_lo = s.skip_hi = 0;
+  if (s.turned && !adjacent) {
+    s.at = V > 1 ? min(V * j, rot / 2 - V) : j;
+    s.lo = s.at;
+    s.hi = s.lo + rot / 2;
+    s.skip_lo = s.skip_hi = V * j - s.at;
   } else {
-    s.lo = rot + 2 * V * (j - turned);
+    // 2 V neighbouring elements
+    const int first = s.turned ? 2 * V * j : rot + 2 * V * (j - turned);
+    s.lo = V > 1 ? min(first, (s.turned ? rot : dim) - 2 * V) : first;
     s.hi = s.lo + V;
+    s.at = s.lo / 2;
+    s.skip_lo = min(first - s.lo, V);
+    s.skip_hi = first - s.lo - s.skip_lo;
   }
-  s.in = s.lo < dim;
   s.two = s.hi < dim;
   return s;
 }
@@ -177,24 +190,36 @@ __device__ __forceinline__ float rstd_of(float sum_sq, int dim, float eps) {
   return v == 0.f ? 0.f : 1.f / sqrtf(v);
 }
 
-// A token's pairs of one lane: slots lane % L + 64 i (kP > 1: L is 64).  The next heads'
-// values are on their way while a wave's heads are worked on.
-template <int ELEM, int V, int kP, bool kGrad>
-__global__ __launch_bounds__(64 * kWaves) void heads_kernel(QkNormArgs a, int L, int64_t token_tasks,
-                                                          int head_tasks, int heads_per_task) {
+// A wave's task: `tokens` tokens, or one token's part of `heads` heads, of `parts` (tokens =
+// 1).  The next task is `step` such groups of tokens and `rest` parts further.  A wave's
+// next heads are at_once further: skip_tokens tokens and skip_heads heads.
+struct Tasks {
+  int64_t step;
+  int tokens, parts, heads, rest, skip_tokens, skip_heads;
+};
+
+// A wave's pairs of one lane: slots lane % L + 64 i (kP > 1: L is 64).  The next heads'
+// values are on their way while a wave's heads are worked on.  kShared: slots may share
+// values.
+template <int ELEM, int V, int kP, bool kGrad, bool kShared>
+__global__ __launch_bounds__(64 * kWaves, kP > 1 ? 1 : kGrad ? 2 : 4) void heads_kernel(QkNormArgs a, int L, Tasks by) {
   constexpr int ES = elem_bytes<ELEM>;
   // tables of angles, or the gradient's sums of 16 lanes and more: kWaves x 64 / max(L, 16)
   // x 2 dim values, dim at most 2 V kP L
   constexpr int kTables = kWaves * 2 * kAngles, kSums = kGrad ? kWaves * 256 * V * kP : 0;
-  __shared__ float lds[kTables > kSums ? kTables : kSums];
+  __shared__ __attribute__((aligned(16))) float lds[kTables > kSums ? kTables : kSums];
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-  const int j0 = lane & (L - 1), sub = lane / L, at_once = 64 / L;
-  const int H = a.heads[0] + a.heads[1];
+  const int j0 = lane & (L - 1), sub = lane / L;
+  const int H = a.heads[0] + a.heads[1], half = a.rot / 2;
   float *const cosines = lds + wave * 2 * kAngles, *const sines = cosines + kAngles;
 
   Slot slot[kP];
 #pragma unroll
   for (int i = 0; i < kP; ++i) slot[i] = slot_of<V>(j0 + 64 * i, a.dim, a.rot, a.adjacent);
+  // whether a value is this slot's alone to add
+  auto own = [&](int i, int r, int e) {
+    return !kShared || e >= (r ? slot[i].skip_hi : slot[i].skip_lo);
+  };
   float dw[2][kP][2][V];
   if constexpr (kGrad) {
 #pragma unroll
@@ -206,68 +231,101 @@ __global__ __launch_bounds__(64 * kWaves) void heads_kernel(QkNormArgs a, int L,
   }
 
   typedef Run<ELEM, V> R;
-  R rx[kP][2], rw[kP][2], rd[kGrad ? kP : 1][2];
-  // head h's values of x, its weights' and the gradient's (lanes without one: zeros)
-  auto fetch = [&](int64_t token, int h, int end) {
+  R rx[kP][2], rd[kGrad ? kP : 1][2];
+  // a head's values of x and of the gradient (lanes without one: zeros)
+  auto fetch = [&](int64_t token, int h, bool live) {
     const int which = h >= a.heads[0] ? 1 : 0;
     const int64_t hh = which ? h - a.heads[0] : h;
     const Heads hx = which ? a.x[1] : a.x[0];
     const unsigned char *px = (const unsigned char *)hx.p + (token * hx.ld + hh * hx.hd) * ES;
-    const unsigned char *pw = (const unsigned char *)(which ? a.w[1] : a.w[0]);
     const Heads hd = which ? a.dy[1] : a.dy[0];
     const unsigned char *pd = (const unsigned char *)hd.p + (token * hd.ld + hh * hd.hd) * ES;
 #pragma unroll
     for (int i = 0; i < kP; ++i) {
 #pragma unroll
       for (int r = 0; r < 2; ++r) {
-        rx[i][r] = rw[i][r] = R{};
+        rx[i][r] = R{};
         if constexpr (kGrad) rd[i][r] = R{};
       }
-      if (h < end && slot[i].in) {
+      if (live && slot[i].in) {
         rx[i][0] = load_run<ELEM, V>(px + slot[i].lo * ES);
-        rw[i][0] = load_run<ELEM, V>(pw + slot[i].lo * ES);
         if constexpr (kGrad) rd[i][0] = load_run<ELEM, V>(pd + slot[i].lo * ES);
         if (slot[i].two) {
           rx[i][1] = load_run<ELEM, V>(px + slot[i].hi * ES);
-          rw[i][1] = load_run<ELEM, V>(pw + slot[i].hi * ES);
           if constexpr (kGrad) rd[i][1] = load_run<ELEM, V>(pd + slot[i].hi * ES);
         }
       }
     }
   };
 
-  const int64_t tasks = token_tasks * head_tasks, stride = (int64_t)gridDim.x * kWaves;
-  int64_t task = (int64_t)blockIdx.x * kWaves + wave;
-  int64_t token = task / head_tasks;
-  int h0 = (int)(task - token * head_tasks) * heads_per_task;
-  if (task < tasks) fetch(token, h0 + sub, min(H, h0 + heads_per_task));
-  while (task < tasks) {
-    const int h1 = min(H, h0 + heads_per_task);
-    const int64_t next_task = task + stride;
-    const int64_t next_token = next_task / head_tasks;
-    const int next_h0 = (int)(next_task - next_token * head_tasks) * heads_per_task;
-    float c[kP][V], s[kP][V];
-    if (a.rot > 0) {
-      const int pos = a.pos[token];
-      for (int i = lane; i < a.rot / 2; i += 64) angle_of(pos, a.freq[i], cosines[i], sines[i]);
+  // the task: its first token, how many, and its heads' end; the lane's first head
+  const int first = blockIdx.x * kWaves + wave;
+  int64_t group = first / by.parts;
+  int part = first - (int)group * by.parts;
+  // (of several tokens: the lane's first head in any task)
+  const int tok0 = by.tokens > 1 ? sub / H : 0, head0 = by.tokens > 1 ? sub - tok0 * H : sub;
+  int64_t token = group * by.tokens;
+  int h = part * by.heads + head0;   // the lane's head, of token + tok
+  int tok = tok0, h_end = min(H, (part + 1) * by.heads);
+  int count = (int)min((int64_t)by.tokens, a.tokens - token);
+  // angle `lane` of a task's tokens, whose position is loaded a task ahead
+  const int angle_tok = half > 0 ? lane / half : 0, angle_at = lane - angle_tok * half;
+  const float freq0 = half > 0 ? a.freq[angle_at] : 0.f;
+  int pos = 0;
+  auto fetch_pos = [&](int64_t token, int count) {
+    if (angle_tok < count) pos = a.pos[token + angle_tok];
+  };
+  if (token < a.tokens) {
+    if (half > 0) fetch_pos(token, count);
+    fetch(token + tok, h, tok < count && h < h_end);
+  }
+  while (token < a.tokens) {
+    part += by.rest;
+    const bool carry = part >= by.parts;
+    if (carry) part -= by.parts;
+    group += by.step + carry;
+    const int64_t next_token = group * by.tokens;
+    const int next_h = part * by.heads + head0, next_end = min(H, (part + 1) * by.heads);
+    const int next_count = (int)min((int64_t)by.tokens, a.tokens - next_token);
+    if (half > 0) {
+      for (int i = lane; i < count * half; i += 64) {
+        if (i == lane) {
+          angle_of(pos, freq0, cosines[i], sines[i]);
+        } else {
+          const int t = i / half;
+          angle_of(a.pos[token + t], a.freq[i - t * half], cosines[i], sines[i]);
+        }
+      }
       // the wave's own values: in order, once they are written
       asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+      if (next_token < a.tokens) fetch_pos(next_token, next_count);
     }
-#pragma unroll
-    for (int i = 0; i < kP; ++i)
-#pragma unroll
-      for (int e = 0; e < V; ++e) {
-        const int at = (j0 + 64 * i) * V + e;
-        c[i][e] = slot[i].turned ? cosines[at] : 1.f;
-        s[i][e] = slot[i].turned ? sines[at] : 0.f;
-      }
-    asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");   // read before the next token's are written
 
-    for (int hb = h0; hb < h1; hb += at_once) {
-      const int h = hb + sub;
-      const bool live = h < h1;
-      const int which = h >= a.heads[0] && live ? 1 : 0;
+    while (true) {
+      const bool live = tok < count && h < h_end;
+      const int which = live && h >= a.heads[0] ? 1 : 0;
       const int64_t hh = which ? h - a.heads[0] : h;
+      const int64_t at_token = token + tok;
+      const int table = live ? tok * half : 0;
+      // the next heads: of this task, or the next one's first
+      h += by.skip_heads;
+      tok += by.skip_tokens;
+      if (by.tokens > 1 && h >= H) {
+        h -= H;
+        ++tok;
+      }
+      const bool more = __any(tok < count && h < h_end);
+      // (the weights are in the caches)
+      const unsigned char *pw = (const unsigned char *)(which ? a.w[1] : a.w[0]);
+      R rw[kP][2];
+#pragma unroll
+      for (int i = 0; i < kP; ++i) {
+        rw[i][0] = rw[i][1] = R{};
+        if (live && slot[i].in) {
+          rw[i][0] = load_run<ELEM, V>(pw + slot[i].lo * ES);
+          if (slot[i].two) rw[i][1] = load_run<ELEM, V>(pw + slot[i].hi * ES);
+        }
+      }
       float x[kP][2][V], w[kP][2][V], d[kP][2][V];
       float sq = 0.f;
 #pragma unroll
@@ -278,17 +336,42 @@ __global__ __launch_bounds__(64 * kWaves) void heads_kernel(QkNormArgs a, int L,
           unpack<ELEM, V>(rw[i][r], w[i][r]);
           if constexpr (kGrad) unpack<ELEM, V>(rd[i][r], d[i][r]);
 #pragma unroll
-          for (int e = 0; e < V; ++e) sq += x[i][r][e] * x[i][r][e];
+          for (int e = 0; e < V; ++e)
+            sq += own(i, r, e) ? x[i][r][e] * x[i][r][e] : 0.f;
         }
       }
       // (in place, nobody's outputs are another's inputs)
-      if (hb + at_once < h1)
-        fetch(token, h + at_once, h1);
-      else if (next_task < tasks)
-        fetch(next_token, next_h0 + sub, min(H, next_h0 + heads_per_task));
+      if (more)
+        fetch(token + tok, h, tok < count && h < h_end);
+      else if (next_token < a.tokens)
+        fetch(next_token + tok0, next_h, tok0 < next_count && next_h < next_end);
+      // (read by every lane at once, also by those that turn nothing)
+      float c[kP][V], s[kP][V];
+#pragma unroll
+      for (int i = 0; i < kP; ++i) {
+        const int at = table + (slot[i].turned ? slot[i].at : 0);
+        if constexpr (V == 8 && !kShared) {
+#pragma unroll
+          for (int k = 0; k < 2; ++k) {
+            const f32x4 cv = *(const f32x4 *)(cosines + at + 4 * k);
+            const f32x4 sv = *(const f32x4 *)(sines + at + 4 * k);
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+              c[i][4 * k + e] = cv[e];
+              s[i][4 * k + e] = sv[e];
+            }
+          }
+        } else {
+#pragma unroll
+          for (int e = 0; e < V; ++e) {
+            c[i][e] = cosines[at + e];
+            s[i][e] = sines[at + e];
+          }
+        }
+      }
       const float rstd = rstd_of(group_sum(sq, L), a.dim, a.eps);
       const Heads hy = which ? a.y[1] : a.y[0];
-      unsigned char *py = (unsigned char *)hy.p + (token * hy.ld + hh * hy.hd) * ES;
+      unsigned char *py = (unsigned char *)hy.p + (at_token * hy.ld + hh * hy.hd) * ES;
       if constexpr (!kGrad) {
 #pragma unroll
         for (int i = 0; i < kP; ++i) {
@@ -300,8 +383,7 @@ __global__ __launch_bounds__(64 * kWaves) void heads_kernel(QkNormArgs a, int L,
         }
       } else {
         // (no head's values in the other weights' sums, also where they are not finite)
-        const bool all_q = h1 <= a.heads[0] || hb + at_once <= a.heads[0];
-        const bool all_k = hb >= a.heads[0];
+        const bool any_q = __any(live && !which), any_k = __any(which);
         float gn = 0.f;
 #pragma unroll
         for (int i = 0; i < kP; ++i) {
@@ -314,12 +396,12 @@ __global__ __launch_bounds__(64 * kWaves) void heads_kernel(QkNormArgs a, int L,
               x[i][r][e] *= rstd;
               t[e] = d[i][r][e] * x[i][r][e];
               d[i][r][e] *= w[i][r][e];
-              gn += d[i][r][e] * x[i][r][e];
+              gn += own(i, r, e) ? d[i][r][e] * x[i][r][e] : 0.f;
             }
-            if (all_q) {
+            if (!any_k) {
 #pragma unroll
               for (int e = 0; e < V; ++e) dw[0][i][r][e] += t[e];
-            } else if (all_k) {
+            } else if (!any_q) {
 #pragma unroll
               for (int e = 0; e < V; ++e) dw[1][i][r][e] += t[e];
             } else {
@@ -346,10 +428,14 @@ __global__ __launch_bounds__(64 * kWaves) void heads_kernel(QkNormArgs a, int L,
           if (slot[i].two) store_run<ELEM, V>(py + slot[i].hi * ES, x[i][1]);
         }
       }
+      if (!more) break;
     }
-    task = next_task;
+    asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");   // the angles are read
     token = next_token;
-    h0 = next_h0;
+    count = next_count;
+    h = next_h;
+    h_end = next_end;
+    tok = tok0;
   }
 
   if constexpr (kGrad) {
@@ -371,7 +457,8 @@ __global__ __launch_bounds__(64 * kWaves) void heads_kernel(QkNormArgs a, int L,
             if (L <= 4) v = add_dpp<0x124>(v);
             if (L <= 8) v = add_dpp<0x128>(v);
             const int at = (r ? slot[i].hi : slot[i].lo) + e;
-            if (lane % span < L && (r ? slot[i].two : slot[i].in)) mine[s * a.dim + at] = v;
+            if (lane % span < L && slot[i].in && (r == 0 || slot[i].two) && own(i, r, e))
+              mine[s * a.dim + at] = v;
           }
     __syncthreads();
     for (int i = threadIdx.x; i < 2 * a.dim; i += 64 * kWaves) {
@@ -404,40 +491,69 @@ __global__ __launch_bounds__(1024) void head_dw_kernel(QkNormArgs a, int parts) 
   }
 }
 
-template <int ELEM, int V, int kP, bool kGrad>
+int slots_of(const QkNormArgs &a, int V) {
+  return (a.rot / 2 + V - 1) / V + (a.dim - a.rot + 2 * V - 1) / (2 * V);
+}
+
+template <int ELEM, int V, int kP, bool kGrad, bool kShared>
 hipError_t launch(const QkNormArgs &a, hipStream_t stream, int num_cus) {
-  const int slots = (a.dim + 2 * V - 1) / (2 * V);
+  const int slots = slots_of(a, V);
   int L = 1;
   while (L < slots && L < 64) L <<= 1;
-  const int H = a.heads[0] + a.heads[1], at_once = 64 / L;
+  const int H = a.heads[0] + a.heads[1], at_once = 64 / L, half = a.rot / 2;
   const int rounds = (H + at_once - 1) / at_once;
-  // waves for the whole chip: a token's heads are several waves' where tokens are few
+  // waves for the whole chip: a token's heads are several waves' where tokens are few, and a
+  // wave takes several tokens where they are many and rounds and angles are then fuller
   const int64_t waves = (int64_t)num_cus * (kGrad ? 8 : 16);
-  const int head_tasks =
-      (int)std::max<int64_t>(1, std::min<int64_t>(rounds, waves / std::max<int64_t>(a.tokens, 1)));
-  const int per_task = (rounds + head_tasks - 1) / head_tasks * at_once;
-  const int tasks_h = (H + per_task - 1) / per_task;
-  const int64_t tasks = a.tokens * tasks_h;
+  Tasks by{0, 1, 1, rounds * at_once, 0, 0, at_once};
+  if (a.tokens < waves) {
+    by.parts = (int)std::min<int64_t>(rounds, waves / a.tokens);
+    by.heads = (rounds + by.parts - 1) / by.parts * at_once;
+    by.parts = (H + by.heads - 1) / by.heads;
+  } else {
+    // instructions of a round, of 64 angles and of a task, about; more tokens only where that
+    // saves a twentieth (us, 20000 tokens, bf16, one token / the rule: 18 heads of 64 26.8 / 20.0,
+    // of 80, 40 of them turned, 40.4 / 31.1; 16 heads of 128 28.4, four tokens 31.9)
+    double least = 1e300;
+    for (int n = 1; n <= 8 && n * waves <= a.tokens && n * half <= kAngles; ++n) {
+      const int r = (n * H + at_once - 1) / at_once, angles = (n * half + 63) / 64;
+      const double each = (r * 250.0 + angles * 150.0 + 100.0) / n;
+      if (each < 0.95 * least) {
+        least = each;
+        by.tokens = n;
+      }
+    }
+    if (by.tokens > 1) {
+      by.heads = H;
+      by.skip_tokens = at_once / H;
+      by.skip_heads = at_once % H;
+    }
+  }
+  const int64_t groups = (a.tokens + by.tokens - 1) / by.tokens;
+  const int64_t tasks = groups * by.parts;
   int64_t blocks = (tasks + kWaves - 1) / kWaves;
   blocks = std::min<int64_t>(blocks, kGrad ? kHeadParts : 8 * (int64_t)num_cus);
-  heads_kernel<ELEM, V, kP, kGrad><<<(unsigned)blocks, 64 * kWaves, 0, stream>>>(
-      a, L, a.tokens, tasks_h, per_task);
+  by.step = blocks * kWaves / by.parts;
+  by.rest = (int)(blocks * kWaves % by.parts);
+  heads_kernel<ELEM, V, kP, kGrad, kShared><<<(unsigned)blocks, 64 * kWaves, 0, stream>>>(a, L, by);
   hipError_t e = hipGetLastError();
   if (e != hipSuccess || !kGrad) return e;
   head_dw_kernel<<<(unsigned)((2 * a.dim + 15) / 16), 1024, 0, stream>>>(a, (int)blocks);
   return hipGetLastError();
 }
 
-// The widest runs that a head's rotated and other parts are whole numbers of.
+// Whole vectors where each part of a head has room for a slot (us, 2000 tokens of 9 heads of
+// 100 elements, 50 of them turned, by vectors / by pairs: 6.7 / 9.7, gradients
+// 15.4 / 20.1).
 template <int ELEM, bool kGrad>
 hipError_t pick(const QkNormArgs &a, hipStream_t stream, int num_cus) {
   const int rest = a.dim - a.rot;
-  const auto fits = [&](int v) { return a.rot % (2 * v) == 0 && rest % (2 * v) == 0; };
-  if (fits(8)) return launch<ELEM, 8, 1, kGrad>(a, stream, num_cus);
-  if (fits(4) && a.dim <= 512) return launch<ELEM, 4, 1, kGrad>(a, stream, num_cus);
-  if (fits(2) && a.dim <= 256) return launch<ELEM, 2, 1, kGrad>(a, stream, num_cus);
-  if (a.dim <= 128) return launch<ELEM, 1, 1, kGrad>(a, stream, num_cus);
-  return launch<ELEM, 1, 8, kGrad>(a, stream, num_cus);
+  if (a.rot % 16 == 0 && rest % 16 == 0)
+    return launch<ELEM, 8, 1, kGrad, false>(a, stream, num_cus);
+  if ((a.rot == 0 || a.rot >= 16) && (rest == 0 || rest >= 16) && slots_of(a, 8) <= 64)
+    return launch<ELEM, 8, 1, kGrad, true>(a, stream, num_cus);
+  if (slots_of(a, 1) <= 64) return launch<ELEM, 1, 1, kGrad, false>(a, stream, num_cus);
+  return launch<ELEM, 1, 8, kGrad, false>(a, stream, num_cus);
 }
 
 __global__ void zero_dw_kernel(QkNormArgs a) {
