@@ -228,12 +228,11 @@ __global__ __launch_bounds__(256) void dequant_kernel(Mx4DequantArgs a, int64_t 
   }
 }
 
-// Workgroups of a launch count in 2^31 here and threads in 32 bits: more tiles of
-// rows than that are launched in turn.
+// Threads of a launch count in 32 bits: more tiles of rows than that are launched in turn.
 template <typename F>
 hipError_t by_rows(int64_t rows, int64_t row_tile, int64_t col_tiles, F launch) {
   if (col_tiles == 0) return hipSuccess;
-  const int64_t most = std::max<int64_t>(1, ((int64_t)1 << 23) / col_tiles);
+  const int64_t most = std::max<int64_t>(1, ((int64_t)1 << 22) / col_tiles);
   for (int64_t r = 0; r < rows; r += most * row_tile) {
     const int64_t n = std::min(rows - r, most * row_tile);
     launch(r, n, (unsigned)((n + row_tile - 1) / row_tile * col_tiles));

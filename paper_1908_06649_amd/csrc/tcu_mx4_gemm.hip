@@ -641,6 +641,7 @@ int64_t tiles_of(int64_t M, int64_t N, int64_t tile) {
 }
 double tiles_us(const Variant &v, int64_t M, int64_t N, int64_t stages, int num_cus) {
   const double items = (double)tiles_of(M, N, v.tile), full = items / num_cus;
+  if (v.groups > 1 && items > (1 << 22)) return 1e300;   // one item a workgroup of 512 threads
   const double batches = std::ceil(std::ceil(full) / v.per_cu);
   return v.call + std::ceil((double)stages / v.groups) * std::max(batches * v.alone, full * v.full) +
          batches * v.item;

@@ -856,8 +856,8 @@ def tcu_qk_norm(q, k, wq, wk, freq, pos, yq, yk, tokens: int, hq: int, hk: int, 
     if q is not None and k is not None and rot:
         # everything as it should be: one flat condition (a call 9.3 -> 8.2 us)
         a, b, c, d, dev = q.stride(), k.stride(), yq.stride(), yk.stride(), q.get_device()
-        if dev >= 0 and a[-1] == b[-1] == c[-1] == d[-1] == 1 and \
-                q.shape == sq and yq.shape == sq and k.shape == sk and yk.shape == sk and \
+        if dev >= 0 and q.shape == sq and yq.shape == sq and k.shape == sk and \
+                yk.shape == sk and a[2] == b[2] == c[2] == d[2] == 1 and \
                 t == k.dtype == yq.dtype == yk.dtype == wq.dtype == wk.dtype and \
                 freq.dtype == _F32 and pos.dtype == _I32 and \
                 dev == k.get_device() == yq.get_device() == yk.get_device() == \
@@ -898,9 +898,9 @@ def tcu_qk_norm_grad(dyq, dyk, q, k, wq, wk, freq, pos, dq, dk, dwq, dwk, work, 
         # as in tcu_qk_norm (a call 15.3 -> 13.7 us)
         a, b, c, d, dev = q.stride(), k.stride(), dyq.stride(), dyk.stride(), q.get_device()
         e, f = dq.stride(), dk.stride()
-        if dev >= 0 and a[-1] == b[-1] == c[-1] == d[-1] == e[-1] == f[-1] == 1 and \
-                q.shape == sq and dyq.shape == sq and dq.shape == sq and \
+        if dev >= 0 and q.shape == sq and dyq.shape == sq and dq.shape == sq and \
                 k.shape == sk and dyk.shape == sk and dk.shape == sk and \
+                a[2] == b[2] == c[2] == d[2] == e[2] == f[2] == 1 and \
                 t == k.dtype == dyq.dtype == dyk.dtype == dq.dtype == dk.dtype == wq.dtype == \
                 wk.dtype and \
                 freq.dtype == dwq.dtype == dwk.dtype == _F32 and pos.dtype == _I32 and \
