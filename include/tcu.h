@@ -566,8 +566,12 @@ int64_t tcu_mx4_work(int64_t M, int64_t K, int64_t N);
  * formed in binary32 and rounded once; the angles are formed so that they are right to
  * binary32 at any int32 position.  Head h of token t begins at t * ld + h * hd of its
  * operand (pitches in elements, no alignment asked of them): token by token (hd < ld, as
- * views of packed queries, keys and values) or head by head (ld < hd).  yq may be exactly q and yk exactly k.
- * A head of zeros has y = 0, also for eps = 0 (as tcu_rms_norm).
+ * views of packed queries, keys and values) or head by head (ld < hd).  yq may be exactly
+ * q and yk exactly k.
+ * A head of zeros has y = 0 (and a gradient of 0), also for eps = 0: there every head whose
+ * squares' mean is 0 in binary32.  A value that is not finite stays in its head; a finite
+ * head whose squares' sum passes binary32's range is taken as one of infinite norm: y = 0
+ * (all as tcu_rms_norm).
  *   0 <= tokens <= TCU_MAX_RECT_DIM; 0 <= hq, hk <= TCU_MAX_HEADS (operands of no
  *   heads may be NULL); 1 <= dim <= TCU_MAX_HEAD_DIM; 0 <= rot <= dim, even (rot = 0:
  *   freq and pos may be NULL); eps >= 0, finite; elem: a tcu_elem, of q, k, wq, wk, yq

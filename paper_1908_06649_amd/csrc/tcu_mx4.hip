@@ -4,8 +4,9 @@
 //   0, 1/2, 1, 3/2, 2, 3, 4, 6, clamped to 6;  scale byte e + 127
 //
 // Both are bound by memory: x is read once, also where it is written along its rows
-// and along its columns (8192 x 8192 bf16: along the rows 25 us, both ways 36.6, 5.6 TB/s,
-// back 30).  Along the rows a lane holds eight values, four lanes a block, 16 a group of
+// and along its columns (8192 x 8192 bf16, us from memory / where x is still in the last cache:
+// along the rows 30.6 / 25.7, both ways 45.8 / 34.8, 4.5 / 5.9 TB/s, back 37.7 / 30.8; a copy
+// from memory 5.0 TB/s).  Along the rows a lane holds eight values, four lanes a block, 16 a group of
 // 128 with its word of four scales; a workgroup takes 8 rows of 512 columns.  Along the
 // columns a tile of 128 x 128 goes through LDS, where a lane takes 16 rows of two columns.
 #include <algorithm>
@@ -71,6 +72,8 @@ template <int ELEM>
 constexpr int kTilePitch = kTile *elem_bytes<ELEM> + 4;
 constexpr int kCodePitch = 80;
 
+// (Tiles in runs of an XCD, two rows of them at a time so that neighbours' half lines meet
+// in its L2: the same time, 46.0 us.)
 template <int ELEM, bool kRows>
 __global__ __launch_bounds__(512) void quant_both_kernel(Mx4QuantArgs a, int64_t col_tiles) {
   constexpr int ES = elem_bytes<ELEM>, kPitch = kTilePitch<ELEM>;

@@ -83,13 +83,15 @@ __device__ __forceinline__ void dma_lds4_saddr(const void *gbase, unsigned voff,
 // next stage's first fragments, and the copy of the stage after it is issued into the
 // buffer that has been read.
 //
-// 8192 x 8192 x 8192 of random codes, bf16 out: 248 us in steady state (4.4 PFLOP/s), 192
-// (5.4) on zeros, which the power limit does not slow; products from registers alone 174
-// (6.0).  LDS is busy 2250 cycles of a stage's 3700 (reads 1735, copies 512), the matrix
-// cores 2048.  Tried: blocks of 32 x 32 over 64 values (each instruction the same work,
-// more power: 6.0 against 6.4 PFLOP/s from registers; 295 us without the stream across
-// tiles, 80 of 340 bands of stores exposed); the order that the compiler chose (256);
-// bands of 2 or 8 rows of tiles (258, 256); four waves of 128 x 128 (spills).
+// 8192 x 8192 x 8192, bf16 out, us in steady state: 248 to 258 on random codes (4.4 PFLOP/s; by
+// the card), 189 (5.8) on zeros; the matrix cores alone, from registers, 174 and 118.  Random
+// codes are bound by power, zeros by the order of reads and products: of a stage's 3600
+// cycles LDS is busy 2250 (reads 1735, copies 512) and the matrix cores 2048.  The copies
+// are not waited for: without their wait the time is the same.  Tried, same product:
+// products of 32 x 32 over 64 values (each instruction the same work at more power: 182 from
+// registers); the order that the compiler chose (256 against 248); bands of 2 or 8 rows of
+// tiles (258, 256); a stage's copies issued at once or in two parts (262 against 258, on
+// zeros 198 against 189); four waves of 128 x 128 (their registers spill).
 template <int ELEM, int FM, int FN, int WM, int WN, int KG>
 __global__ __launch_bounds__(64 * WM * WN * KG) void mx4_tile_kernel(TileArgs ta) {
   constexpr int BM = 16 * FM * WM, BN = 16 * FN * WN, kWaves = WM * WN;
@@ -480,7 +482,8 @@ __device__ __forceinline__ u32x4 quad_codes(const unsigned char *row, int64_t co
 
 // XE: the left operand's element type (of up to four rows), or -1: in 4 bits already.
 // MF: blocks of 16 rows; NB: blocks of 16 rows of B.  A wave takes pairs of groups of 128
-// values: whole lines.
+// values: whole lines.  Bound by B's bytes and the latency of a wave's first: us from memory,
+// 1 x 4096 x 4096 4.9 (B 8.9 MB), 16 x 8192 x 8192 10.4 (B 35.7 MB, 3.4 TB/s with launch and end).
 template <int ELEM, int XE, int MF, int NB>
 __global__ __launch_bounds__(64 * kFewWaves) void mx4_few_kernel(FewArgs fa) {
   const Mx4GemmArgs &a = fa.g;
