@@ -143,3 +143,37 @@ def test_the_general_checks_pass_the_same_arguments(library, name, monkeypatch):
     # the same but for freq, pos and rot
     different = [i for i, (x, y) in enumerate(zip(flat[1], args)) if x != y]
     assert len(args) == len(flat[1]) and len(different) == 3
+
+
+@pytest.mark.parametrize("name", CALLS)
+def test_absent_operands_are_the_librarys_to_refuse(library, name):
+    """An operand that is None arrives as a null pointer; scratch that is needed and None, and an
+    operand whose type the call takes for its own, are refused before."""
+    operands, call = CALLS[name]
+    for i in range(len(operands)):
+        t = [Fake(t, 0, 4096 * (j + 1)) for j, t in enumerate(operands)]
+        t[i] = None
+        try:
+            call(*t)
+        except (ValueError, AttributeError):
+            assert operands[i].shape == WORK[0] or operands[i].dtype in (BF16, F32)
+            assert library.calls == []
+            continue
+        called, args = library.calls.pop()
+        assert called == name and 4096 * (i + 1) not in args and None in args
+
+
+@pytest.mark.parametrize("name,i", [("tcu_mx4_quant", 2), ("tcu_mx4_quant", 4),
+                                    ("tcu_mx4_dequant", 0), ("tcu_mx4_linear", 1),
+                                    ("tcu_mx4_linear", 2), ("tcu_qk_norm", 2), ("tcu_qk_norm", 4),
+                                    ("tcu_qk_norm", 5), ("tcu_qk_norm", 7),
+                                    ("tcu_qk_norm_grad", 1), ("tcu_qk_norm_grad", 9),
+                                    ("tcu_qk_norm_grad", 11)])
+def test_a_missing_operand_is_an_error_of_the_library(library, name, i):
+    """Scales without codes, weights, tables or outputs that are missing arrive as null."""
+    operands, call = CALLS[name]
+    t = [Fake(t, 0, 4096 * (j + 1)) for j, t in enumerate(operands)]
+    t[i] = None
+    call(*t)
+    (called, args), = library.calls
+    assert called == name and None in args
