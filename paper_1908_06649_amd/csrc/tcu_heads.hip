@@ -204,8 +204,8 @@ struct Tasks {
 template <int ELEM, int V, int kP, bool kGrad, bool kShared>
 __global__ __launch_bounds__(64 * kWaves, kP > 1 ? 1 : kGrad ? 2 : 4) void heads_kernel(QkNormArgs a, int L, Tasks by) {
   constexpr int ES = elem_bytes<ELEM>;
-  // tables of angles, or the gradient's sums of 16 lanes and more: kWaves x 64 / max(L, 16)
-  // x 2 dim values, dim at most 2 V kP L
+  // tables of angles, or the gradient's sums: kWaves x 64 / L x 2 dim values, dim at most
+  // 2 V kP L
   constexpr int kTables = kWaves * 2 * kAngles, kSums = kGrad ? kWaves * 256 * V * kP : 0;
   __shared__ __attribute__((aligned(16))) float lds[kTables > kSums ? kTables : kSums];
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
@@ -439,32 +439,57 @@ __global__ __launch_bounds__(64 * kWaves, kP > 1 ? 1 : kGrad ? 2 : 4) void heads
   }
 
   if constexpr (kGrad) {
-    // a wave's lanes of one slot: those of 16 in registers, the rest and the waves in LDS
-    const int rows = L >= 64 ? 1 : L == 32 ? 2 : 4, span = L > 16 ? L : 16;
-    float *const mine = lds + (wave * rows + lane / span) * 2 * a.dim;
+    // every lane's sums to LDS as they are, heads' rows one after the other: few instructions
+    // (a kernel of few tokens waits for each of its own code's lines)
+    const int rows = 64 / L;
+    float *const mine = lds + (wave * rows + sub) * 2 * a.dim;
     __syncthreads();   // the tables are read
 #pragma unroll
     for (int s = 0; s < 2; ++s)
 #pragma unroll
       for (int i = 0; i < kP; ++i)
 #pragma unroll
-        for (int r = 0; r < 2; ++r)
+        for (int r = 0; r < 2; ++r) {
+          const int at = r ? slot[i].hi : slot[i].lo;
+          if (!slot[i].in || (r == 1 && !slot[i].two)) continue;
+          if constexpr (V == 8 && !kShared) {
 #pragma unroll
-          for (int e = 0; e < V; ++e) {
-            float v = dw[s][i][r][e];
-            if (L <= 1) v = add_dpp<0x121>(v);   // 16 lanes turned by 1, 2, 4 and 8
-            if (L <= 2) v = add_dpp<0x122>(v);
-            if (L <= 4) v = add_dpp<0x124>(v);
-            if (L <= 8) v = add_dpp<0x128>(v);
-            const int at = (r ? slot[i].hi : slot[i].lo) + e;
-            if (lane % span < L && slot[i].in && (r == 0 || slot[i].two) && own(i, r, e))
-              mine[s * a.dim + at] = v;
+            for (int k = 0; k < 2; ++k) {
+              const float *v = dw[s][i][r] + 4 * k;
+              *(f32x4 *)(mine + s * a.dim + at + 4 * k) = f32x4{v[0], v[1], v[2], v[3]};
+            }
+          } else {
+#pragma unroll
+            for (int e = 0; e < V; ++e)
+              if (own(i, r, e)) mine[s * a.dim + at + e] = dw[s][i][r][e];
           }
+        }
     __syncthreads();
-    for (int i = threadIdx.x; i < 2 * a.dim; i += 64 * kWaves) {
-      float v = 0.f;
-      for (int k = 0; k < kWaves * rows; ++k) v += lds[k * 2 * a.dim + i];
-      a.parts[(int64_t)blockIdx.x * 2 * a.dim + i] = v;
+    // the rows in `segs` pieces, a thread a column of one, and the pieces in their order
+    const int cols = 2 * a.dim, all = kWaves * rows;
+    const int segs = max(1, 64 * kWaves / cols), each = (all + segs - 1) / segs;
+    const int seg = (int)threadIdx.x / cols, col = (int)threadIdx.x - seg * cols;
+    float v = 0.f;
+    if (segs > 1) {
+      if (seg < segs) {
+#pragma unroll 8
+        for (int k = seg * each; k < min(all, (seg + 1) * each); ++k) v += lds[k * cols + col];
+      }
+      __syncthreads();   // the rows are read
+      lds[threadIdx.x] = v;
+      __syncthreads();
+      if (seg == 0) {
+        v = 0.f;
+        for (int k = 0; k < segs; ++k) v += lds[k * cols + col];
+        a.parts[(int64_t)blockIdx.x * cols + col] = v;
+      }
+      return;
+    }
+    for (int i = threadIdx.x; i < cols; i += 64 * kWaves) {
+      v = 0.f;
+#pragma unroll 8
+      for (int k = 0; k < all; ++k) v += lds[k * cols + i];
+      a.parts[(int64_t)blockIdx.x * cols + i] = v;
     }
   }
 }
