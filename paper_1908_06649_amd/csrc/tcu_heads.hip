@@ -536,13 +536,17 @@ hipError_t launch(const QkNormArgs &a, hipStream_t stream, int num_cus) {
     by.heads = (rounds + by.parts - 1) / by.parts * at_once;
     by.parts = (H + by.heads - 1) / by.heads;
   } else {
-    // instructions of a round, of 64 angles and of a task, about; more tokens only where that
-    // saves a twentieth (us, 20000 tokens, bf16, one token / the rule: 18 heads of 64 26.8 / 20.0,
-    // of 80, 40 of them turned, 40.4 / 31.1; 16 heads of 128 28.4, four tokens 31.9)
+    // instructions of a round, of 64 angles and of a task, about, times the tasks of a wave:
+    // between their mean and the most that one has.  More tokens only where that saves a
+    // twentieth (us, bf16, one token / the rule: 20000 tokens of 18 heads of 64 26.8 / 20.0, of
+    // 80, 40 of them turned, 40.4 / 31.1; 16 heads of 128 28.4, four tokens 31.9; rounded tasks
+    // counted / the mean alone, 6000 tokens of 3 heads of 64 5.0 / 7.1, of 20 10.1 / 11.8).
     double least = 1e300;
-    for (int n = 1; n <= 8 && n * waves <= a.tokens && n * half <= kAngles; ++n) {
+    for (int n = 1; n <= 8 && n * half <= kAngles; ++n) {
       const int r = (n * H + at_once - 1) / at_once, angles = (n * half + 63) / 64;
-      const double each = (r * 250.0 + angles * 150.0 + 100.0) / n;
+      const int64_t groups = (a.tokens + n - 1) / n, most = (groups + waves - 1) / waves;
+      const double mean = std::max(1.0, (double)groups / waves);
+      const double each = 0.5 * (most + mean) * (r * 250.0 + angles * 150.0 + 100.0);
       if (each < 0.95 * least) {
         least = each;
         by.tokens = n;
