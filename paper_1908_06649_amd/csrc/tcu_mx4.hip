@@ -16,18 +16,48 @@
 namespace tcu {
 namespace {
 
+// The tile of a workgroup.  Workgroups go round the 8 XCDs: where rows of x begin inside
+// lines, neighbouring tiles share lines, and an XCD takes a run of tiles (`runs`), in bands
+// of kBand rows of them and column by column, so that these lines meet in its L2; where
+// rows are whole lines, in order (us from memory, in order / in runs: 8191 x 8191 bf16 along
+// the rows 57.4 / 35.7, both ways 65.5 / 49.1; 8192 x 8192 30.8 / 34.0 and 45.8 / 46.0.  Back, whose
+// stores are these rows, 48.9 / 46.0 and smaller ones slower: always in order).
+template <int kBand>
+__device__ __forceinline__ void place_tile(bool runs, unsigned row_tiles, unsigned col_tiles,
+                                           int64_t &row, int64_t &col) {
+  unsigned v = blockIdx.x;
+  if (!runs) {
+    row = v / col_tiles;
+    col = v % col_tiles;
+    return;
+  }
+  const unsigned body = gridDim.x & ~7u;
+  if (v < body) v = (v & 7) * (body >> 3) + (v >> 3);
+  const unsigned band = v / (kBand * col_tiles), in_band = v - band * kBand * col_tiles;
+  const unsigned rows = min((unsigned)kBand, row_tiles - kBand * band);
+  row = kBand * band + in_band % rows;
+  col = in_band / rows;
+}
+// Whether rows of pitch ld bytes from p on begin inside lines.
+bool inside_lines(const void *p, int64_t ld) {
+  return (((uintptr_t)p | (uintptr_t)ld) & 127) != 0;
+}
+
 // ------------------------------------------------------------- along the rows
 // Two rows a wave (us, two / eight, bf16: 64 x 4096 2.6 / 4.1, 1024 x 4096 3.4 / 4.4, 8192 x 8192
 // 24.8 / 29.7; back 2.9 / 5.2, 4.8 / 6.3, 29.8 / 31.3).
 constexpr int kMine = 2, kRowTile = 4 * kMine, kColTile = 512;
 
 template <int ELEM>
-__global__ __launch_bounds__(256) void quant_rows_kernel(Mx4QuantArgs a, int64_t col_tiles) {
+__global__ __launch_bounds__(256) void quant_rows_kernel(Mx4QuantArgs a, unsigned col_tiles,
+                                                         bool runs) {
   constexpr int ES = elem_bytes<ELEM>;
   __shared__ unsigned words[4][kRowTile];
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-  const int64_t r0 = (int64_t)blockIdx.x / col_tiles * kRowTile;
-  const int64_t c0 = (int64_t)blockIdx.x % col_tiles * kColTile;
+  int64_t r0, c0;
+  place_tile<4>(runs, (unsigned)((a.rows + kRowTile - 1) / kRowTile), col_tiles, r0, c0);
+  r0 *= kRowTile;
+  c0 *= kColTile;
   const int64_t col = c0 + lane * 8;
   const int64_t groups = mx4_groups(a.cols);
   const int valid = (int)min((int64_t)8, max((int64_t)0, a.cols - col));
@@ -72,18 +102,19 @@ template <int ELEM>
 constexpr int kTilePitch = kTile *elem_bytes<ELEM> + 4;
 constexpr int kCodePitch = 80;
 
-// (Tiles in runs of an XCD, two rows of them at a time so that neighbours' half lines meet
-// in its L2: the same time, 46.0 us.)
 template <int ELEM, bool kRows>
-__global__ __launch_bounds__(512) void quant_both_kernel(Mx4QuantArgs a, int64_t col_tiles) {
+__global__ __launch_bounds__(512) void quant_both_kernel(Mx4QuantArgs a, unsigned col_tiles,
+                                                         bool runs) {
   constexpr int ES = elem_bytes<ELEM>, kPitch = kTilePitch<ELEM>;
   __shared__ __attribute__((aligned(16))) unsigned char tile[kTile * kPitch];
   __shared__ unsigned words[kTile];
   __shared__ __attribute__((aligned(16))) unsigned char codes[kTile * kCodePitch];
   __shared__ unsigned char bytes[kTile * 4];
   const int t = threadIdx.x, lane = t & 63, wave = t >> 6;
-  const int64_t r0 = (int64_t)blockIdx.x / col_tiles * kTile;
-  const int64_t c0 = (int64_t)blockIdx.x % col_tiles * kTile;
+  int64_t r0, c0;
+  place_tile<2>(runs, (unsigned)((a.rows + kTile - 1) / kTile), col_tiles, r0, c0);
+  r0 *= kTile;
+  c0 *= kTile;
   {
     // 16 lanes a row, 32 rows at a time
     const int64_t col = c0 + (t & 15) * 8;
@@ -186,11 +217,11 @@ template <int ELEM>
 constexpr int kBackValues = 16 / elem_bytes<ELEM>;
 
 template <int ELEM>
-__global__ __launch_bounds__(256) void dequant_kernel(Mx4DequantArgs a, int64_t col_tiles) {
+__global__ __launch_bounds__(256) void dequant_kernel(Mx4DequantArgs a, unsigned col_tiles) {
   constexpr int ES = elem_bytes<ELEM>, V = kBackValues<ELEM>;
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-  const int64_t r0 = (int64_t)blockIdx.x / col_tiles * kRowTile;
-  const int64_t col = (int64_t)blockIdx.x % col_tiles * (64 * V) + lane * V;
+  const int64_t r0 = (int64_t)(blockIdx.x / col_tiles) * kRowTile;
+  const int64_t col = (int64_t)(blockIdx.x % col_tiles) * (64 * V) + lane * V;
   const int valid = (int)min((int64_t)V, a.cols - col);
   if (valid <= 0) return;
   unsigned c[kMine], byte[kMine];
@@ -252,6 +283,7 @@ hipError_t quant(const Mx4QuantArgs &a, hipStream_t stream) {
   return by_rows(a.rows, a.qt ? kTile : kRowTile, col_tiles, [&](int64_t r, int64_t n, unsigned blocks) {
     Mx4QuantArgs p = a;
     p.x = (const unsigned char *)a.x + r * a.ldx * elem_bytes<ELEM>;
+    const bool runs = inside_lines(p.x, a.ldx * elem_bytes<ELEM>);
     p.rows = n;
     if (a.q) {
       p.q += r * a.ldq;
@@ -262,11 +294,11 @@ hipError_t quant(const Mx4QuantArgs &a, hipStream_t stream) {
       p.ts += r / 128 * a.ldts;
     }
     if (a.qt && a.q)
-      quant_both_kernel<ELEM, true><<<blocks, 512, 0, stream>>>(p, col_tiles);
+      quant_both_kernel<ELEM, true><<<blocks, 512, 0, stream>>>(p, (unsigned)col_tiles, runs);
     else if (a.qt)
-      quant_both_kernel<ELEM, false><<<blocks, 512, 0, stream>>>(p, col_tiles);
+      quant_both_kernel<ELEM, false><<<blocks, 512, 0, stream>>>(p, (unsigned)col_tiles, runs);
     else
-      quant_rows_kernel<ELEM><<<blocks, 256, 0, stream>>>(p, col_tiles);
+      quant_rows_kernel<ELEM><<<blocks, 256, 0, stream>>>(p, (unsigned)col_tiles, runs);
   });
 }
 
@@ -280,7 +312,7 @@ hipError_t dequant(const Mx4DequantArgs &a, hipStream_t stream) {
     p.s += r;
     p.y = (unsigned char *)a.y + r * a.ldy * elem_bytes<ELEM>;
     p.rows = n;
-    dequant_kernel<ELEM><<<blocks, 256, 0, stream>>>(p, col_tiles);
+    dequant_kernel<ELEM><<<blocks, 256, 0, stream>>>(p, (unsigned)col_tiles);
   });
 }
 
