@@ -19,7 +19,7 @@
 //     in binary32), and shared through LDS.
 //   * The weights' gradients are summed in registers over a workgroup's tokens, and the
 //     workgroups' parts by a second launch, in their order.
-// 16384 tokens of 72 heads of 128 bf16 124 us, 4.9 TB/s; gradients of 8192 tokens of 40 heads 52
+// 16384 tokens of 72 heads of 128 bf16 124 us, 4.9 TB/s; gradients of 8192 tokens of 40 heads 54
 // + 4.8 us, 4.7 TB/s; a copy 5.0.
 #include <algorithm>
 
@@ -200,9 +200,11 @@ struct Tasks {
 
 // A wave's pairs of one lane: slots lane % L + 64 i (kP > 1: L is 64).  The next heads'
 // values are on their way while a wave's heads are worked on.  kShared: slots may share
-// values.
+// values.  Gradients: two waves on a SIMD (three, for 16-bit types, spill: 59 sizes 9 %
+// slower in the mean).
 template <int ELEM, int V, int kP, bool kGrad, bool kShared>
-__global__ __launch_bounds__(64 * kWaves, kP > 1 ? 1 : kGrad ? 2 : 4) void heads_kernel(QkNormArgs a, int L, Tasks by) {
+__global__ __launch_bounds__(64 * kWaves, kP > 1 ? 1 : kGrad ? 2 : 4) void heads_kernel(
+    QkNormArgs a, int L, Tasks by) {
   constexpr int ES = elem_bytes<ELEM>;
   // tables of angles, or the gradient's sums: kWaves x 64 / L x 2 dim values, dim at most
   // 2 V kP L
