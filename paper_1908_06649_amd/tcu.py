@@ -817,9 +817,24 @@ def tcu_mx4_gemm(A, lda: int, ascale, ldas: int, B, ldb: int, bscale, ldbs: int,
     where, t = "tcu_mx4_gemm", C.dtype
     elem = _elem_code(where, t)
     L = _lib or lib()
+    # as in tcu_mx4_quant (a small layer's step, three calls of each: 42.9 -> 40.3 us)
+    dev, g, nbytes = C.get_device(), (K + 127) // 128, L.tcu_mx4_work(M, K, N)
+    if A is not None and ascale is not None and B is not None and bscale is not None and \
+            work is not None and dev >= 0 and C.shape == (M, N) and C.stride() == (ldc, 1) and \
+            A.shape == (M, 64 * g) and A.stride() == (lda, 1) and ascale.shape == (g, M) and \
+            ascale.stride() == (ldas, 1) and B.shape == (N, 64 * g) and B.stride() == (ldb, 1) and \
+            bscale.shape == (g, N) and bscale.stride() == (ldbs, 1) and \
+            A.dtype == B.dtype == _U8 and ascale.dtype == bscale.dtype == _I32 and \
+            work.is_contiguous() and 0 <= nbytes <= work.nbytes and \
+            dev == A.get_device() == ascale.get_device() == B.get_device() == \
+            bscale.get_device() == work.get_device() == _current_device():
+        _check(L.tcu_mx4_gemm(A.data_ptr(), lda, ascale.data_ptr(), ldas, B.data_ptr(), ldb,
+                              bscale.data_ptr(), ldbs, C.data_ptr(), ldc, work.data_ptr(), M, K, N,
+                              flags, elem, _stream_of(dev, stream_ptr)), where)
+        return
     dev, (pc, pa, pas, pb, pbs, *pwork) = _addresses(
         where, ((C, t, M, N, ldc),) + _mx4(A, lda, ascale, ldas, M, K) +
-        _mx4(B, ldb, bscale, ldbs, N, K), (), work, L.tcu_mx4_work(M, K, N))
+        _mx4(B, ldb, bscale, ldbs, N, K), (), work, nbytes)
     _check(L.tcu_mx4_gemm(pa, lda, pas, ldas, pb, ldb, pbs, ldbs, pc, ldc, *(pwork or (None,)), M,
                           K, N, flags, elem, _stream_of(dev, stream_ptr)), where)
 

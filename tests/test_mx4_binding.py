@@ -165,7 +165,8 @@ def test_absent_operands_are_the_librarys_to_refuse(library, name):
 
 @pytest.mark.parametrize("name,i", [("tcu_mx4_quant", 2), ("tcu_mx4_quant", 4),
                                     ("tcu_mx4_dequant", 0), ("tcu_mx4_linear", 1),
-                                    ("tcu_mx4_linear", 2), ("tcu_qk_norm", 2), ("tcu_qk_norm", 4),
+                                    ("tcu_mx4_linear", 2), ("tcu_mx4_gemm", 0), ("tcu_mx4_gemm", 3),
+                                    ("tcu_qk_norm", 2), ("tcu_qk_norm", 4),
                                     ("tcu_qk_norm", 5), ("tcu_qk_norm", 7),
                                     ("tcu_qk_norm_grad", 1), ("tcu_qk_norm_grad", 9),
                                     ("tcu_qk_norm_grad", 11)])

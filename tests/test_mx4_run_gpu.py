@@ -3,6 +3,7 @@ projection of queries, keys and values in 4 bits, the heads' norms with rotation
 back -- eager, on another stream, captured and replayed, with pointer checks on, and with
 graphs that have scratch of their own."""
 import ctypes
+import threading
 
 import numpy as np
 import pytest
@@ -180,6 +181,37 @@ def test_another_stream():
         layer.run()
     stream.synchronize()
     assert all(torch.equal(layer.o[k], want[k]) for k in want)
+
+
+def test_two_host_threads():
+    """Two threads, a layer and a stream each, at once."""
+    layers = [Layer(30, 256, 2, 2, 64, 3), Layer(50, 384, 3, 1, 80, 4)]
+    want = []
+    for layer in layers:
+        layer.run()
+        want.append(layer.snapshot())
+    failures = []
+
+    def go(layer, w):
+        try:
+            stream = torch.cuda.Stream()
+            with torch.cuda.stream(stream):
+                for _ in range(20):
+                    for t in layer.o.values():
+                        t.fill_(float("nan"))
+                    layer.run()
+                    stream.synchronize()
+                    assert all(torch.equal(layer.o[k], w[k]) for k in w)
+        except BaseException as e:   # (asserted in the test's own thread)
+            failures.append(e)
+
+    threads = [threading.Thread(target=go, args=a) for a in zip(layers, want)]
+    torch.cuda.synchronize()
+    for t in threads:
+        t.start()
+    for t in threads:
+        t.join()
+    assert not failures
 
 
 @pytest.mark.parametrize("M,K,N", [(1, 4096, 512), (40, 2048, 300), (300, 3000, 200),
