@@ -200,8 +200,8 @@ struct Tasks {
 
 // A wave's pairs of one lane: slots lane % L + 64 i (kP > 1: L is 64).  The next heads'
 // values are on their way while a wave's heads are worked on.  kShared: slots may share
-// values.  Gradients: two waves on a SIMD (three, for 16-bit types, spill: 59 sizes 9 %
-// slower in the mean).
+// values.  Four waves on a SIMD, gradients two: five and three, for 16-bit types, spill (52
+// sizes 23 % slower in the mean, 59 sizes 9 %).
 template <int ELEM, int V, int kP, bool kGrad, bool kShared>
 __global__ __launch_bounds__(64 * kWaves, kP > 1 ? 1 : kGrad ? 2 : 4) void heads_kernel(
     QkNormArgs a, int L, Tasks by) {
