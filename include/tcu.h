@@ -566,8 +566,12 @@ int64_t tcu_mx4_work(int64_t M, int64_t K, int64_t N);
  * formed in binary32 and rounded once; the angles are formed so that they are right to
  * binary32 at any int32 position.  Head h of token t begins at t * ld + h * hd of its
  * operand (pitches in elements, no alignment asked of them): token by token (hd < ld, as
- * views of packed queries, keys and values) or head by head (ld < hd).  yq may be exactly
- * q and yk exactly k.
+ * views of packed queries, keys and values) or head by head (ld < hd); the smaller pitch
+ * is at least dim, the larger at least what lies between its steps (no broadcast heads).
+ * yq may be exactly q and yk exactly k.  Outputs may lie between other operands' heads
+ * where the larger pitches are equal, or all pitches multiples of the smallest (rows of
+ * each head's query, key and value); otherwise operands that lie in each other's gaps
+ * are refused as overlapping.
  * A head of zeros has y = 0 (and a gradient of 0), also for eps = 0: there every head whose
  * squares' mean is 0 in binary32.  A value that is not finite stays in its head; a finite
  * head whose squares' sum passes binary32's range is taken as one of infinite norm: y = 0

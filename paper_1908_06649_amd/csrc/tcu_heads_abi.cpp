@@ -33,7 +33,7 @@ int check_sizes(const Sizes &s) {
 }
 
 // tokens x heads x dim elements as a view of rows: the outer of the two indices, and
-// the whole extent of the inner one.
+// the extent of the inner one with its runs of `dim`.
 Operand heads_view(const Heads &h, int64_t heads, const Sizes &s, bool out = false) {
   Operand o{h.p, 0, 0, 0, elem_size(s.elem), (int)elem_size(s.elem), out};
   if (s.tokens == 0 || heads == 0) return o;
@@ -46,6 +46,9 @@ Operand heads_view(const Heads &h, int64_t heads, const Sizes &s, bool out = fal
     // (an inner pitch in which the elements do not fit is given as one of too many columns)
     const __int128 extent = (__int128)(inner_n - 1) * inner + s.dim;
     o.cols = inner < s.dim || extent >= kMaxExtent ? kMaxExtent : (int64_t)extent;
+    o.runs = inner_n;
+    o.run = s.dim;
+    o.step = inner;
   }
   o.ld = o.rows > 1 ? outer : o.cols;
   return o;

@@ -17,18 +17,65 @@ inline bool elem_ok(int elem) { return elem >= TCU_ELEM_F32 && elem <= TCU_ELEM_
 inline bool dim_ok(int64_t n) { return n >= 0 && n <= TCU_MAX_RECT_DIM; }
 
 // One operand: rows x cols elements of es bytes with pitch ld, its base at a
-// multiple of `align` bytes.
+// multiple of `align` bytes.  Of a row's columns those of `runs` runs of `run` elements
+// `step` apart, if there are several.
 struct Operand {
   const void *p;
   int64_t rows, cols, ld, es;
   int align = 16;
   bool out = false;
+  int64_t runs = 1, run = 0, step = 0;
   bool empty() const { return rows <= 0 || cols <= 0; }
   int64_t extent() const { return view_extent(rows, cols, ld, es); }
 };
 
 inline bool same_view(const Operand &a, const Operand &b) {
   return a.p == b.p && (a.ld == b.ld || a.rows <= 1) && a.es == b.es;
+}
+
+// Whether two operands whose rows meet share no byte all the same, as rows of runs: in
+// bytes, w of every run, `step` apart, n of a row, rows `ld` apart.  Exact where their rows
+// have one pitch; else found where all pitches are multiples of the smallest.
+inline bool runs_apart(const Operand &a, const Operand &b) {
+  if (a.runs == 1 && b.runs == 1) return false;
+  struct Runs {
+    int64_t rows, ld, n, step, w;
+  };
+  const auto in_bytes = [](const Operand &o) {
+    return Runs{o.rows, o.ld * o.es, o.runs, o.step * o.es, (o.runs > 1 ? o.run : o.cols) * o.es};
+  };
+  Runs x = in_bytes(a), y = in_bytes(b);
+  const int64_t d = (int64_t)(reinterpret_cast<uintptr_t>(b.p) - reinterpret_cast<uintptr_t>(a.p));
+  // every run of x begins at one place modulo the smallest pitch, every run of y d behind it
+  const int64_t pitches[] = {x.rows > 1 ? x.ld : 0, x.n > 1 ? x.step : 0, y.rows > 1 ? y.ld : 0,
+                             y.n > 1 ? y.step : 0};
+  int64_t least = kMaxExtent;
+  for (const int64_t p : pitches)
+    if (p > 0 && p < least) least = p;
+  bool whole = true;
+  for (const int64_t p : pitches) whole = whole && p % least == 0;
+  const int64_t at = (d % least + least) % least;
+  if (whole && at >= x.w && at + y.w <= least) return true;
+  // one pitch of rows: y's first row begins `off` behind row k of x.  (rows of single runs
+  // as far apart as the other's runs are: a single row)
+  const auto one_row = [](Runs &r, const Runs &other) {
+    if (r.n == 1 && r.ld == other.step && r.ld != other.ld) r = Runs{1, other.ld, r.rows, r.ld, r.w};
+  };
+  one_row(x, y);
+  one_row(y, x);
+  const int64_t ld = x.rows > 1 ? x.ld : y.ld;
+  const auto fits = [&](const Runs &r) {
+    return (r.rows == 1 || r.ld == ld) && (r.n - 1) * r.step + r.w <= ld;
+  };
+  if (!fits(x) || !fits(y)) return false;
+  const int64_t off = (d % ld + ld) % ld, k = (d - off) / ld;
+  // (rows of y beside rows of x, and those that begin in the row before)
+  const auto meet = [&](int64_t k, int64_t off) {
+    const void *row = reinterpret_cast<const void *>(reinterpret_cast<uintptr_t>(a.p) + off);
+    return k < x.rows && k + y.rows > 0 &&
+           views_overlap(a.p, x.n, x.w, x.step, row, y.n, y.w, y.step);
+  };
+  return !meet(k, off) && !meet(k + 1, off - ld);
 }
 
 // The checks every operator makes of its operands: pointers, pitches and
@@ -54,7 +101,8 @@ int check_operands(const Operand (&ops)[n],
       if (paired) continue;
       const Operand &a = ops[i], &b = ops[j];
       if (views_overlap(a.p, a.rows, a.cols * a.es, a.ld * a.es, b.p, b.rows, b.cols * b.es,
-                        b.ld * b.es))
+                        b.ld * b.es) &&
+          !runs_apart(a, b))
         return TCU_ERR_OVERLAP;
     }
   }
