@@ -542,9 +542,9 @@ def _addresses(where: str, views, vectors, work, nbytes: int):
         if t.numel() != n or not t.is_contiguous():
             raise ValueError(f"{where}: expected {n} contiguous elements, got {tuple(t.shape)}")
         ptrs.append(t.data_ptr() or None)
+    if nbytes < 0:
+        raise TcuError(TCU_ERR_SHAPE, where)
     if work is not None:
-        if nbytes < 0:
-            raise TcuError(TCU_ERR_SHAPE, where)
         if work.get_device() != dev or not work.is_contiguous() or \
                 work.numel() * work.element_size() < nbytes:
             raise ValueError(f"{where}: work needs {nbytes} contiguous bytes on the same device")
