@@ -31,9 +31,10 @@ namespace {
 
 constexpr int kWaves = 4;
 
-// V elements as stored, at any element-aligned address.
+// V elements as stored, at any element-aligned address: one, or whole vectors.
 template <int ELEM, int V>
 struct Run {
+  static_assert(V == 1 || V == 8);
   static constexpr int kBytes = V * elem_bytes<ELEM>, kWords = kBytes < 4 ? 1 : kBytes / 4;
   unsigned w[kWords];
 };
@@ -48,11 +49,6 @@ __device__ __forceinline__ Run<ELEM, V> load_run(const unsigned char *p) {
 #pragma unroll
       for (int d = 0; d < 4; ++d) r.w[4 * i + d] = v[d];
     }
-  } else if constexpr (B == 8) {
-    typedef u32x2 u32x2_any __attribute__((aligned(1)));
-    const u32x2 v = *(const u32x2_any *)p;
-    r.w[0] = v[0];
-    r.w[1] = v[1];
   } else if constexpr (B == 4) {
     r.w[0] = load4_any(p);
   } else {
@@ -78,23 +74,15 @@ __device__ __forceinline__ void unpack(const Run<ELEM, V> &r, float (&x)[V]) {
 
 template <int ELEM, int V>
 __device__ __forceinline__ void store_run(unsigned char *p, const float (&x)[V]) {
-  constexpr int ES = elem_bytes<ELEM>;
   if constexpr (V == 1) {
     f32_to_elem<ELEM>(p, x[0]);
   } else {
     float v[8];
 #pragma unroll
-    for (int e = 0; e < 8; ++e) v[e] = e < V ? x[e] : 0.f;
+    for (int e = 0; e < 8; ++e) v[e] = x[e];
     const Raw8<ELEM> r = pack8<ELEM>(v);
-    if constexpr (V * ES >= 16) {
 #pragma unroll
-      for (int i = 0; i < V * ES / 16; ++i) store16_any(p + 16 * i, r.v[i]);
-    } else if constexpr (V * ES == 8) {
-      typedef u32x2 u32x2_any __attribute__((aligned(1)));
-      *(u32x2_any *)p = u32x2{r.v[0][0], r.v[0][1]};
-    } else {
-      store4_any(p, r.v[0][0]);
-    }
+    for (int i = 0; i < elem_bytes<ELEM> / 2; ++i) store16_any(p + 16 * i, r.v[i]);
   }
 }
 
