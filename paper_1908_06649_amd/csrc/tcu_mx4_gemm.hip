@@ -575,7 +575,7 @@ __global__ __launch_bounds__(64 * kFewWaves) void mx4_few_kernel(FewArgs fa) {
 }
 
 template <int ELEM, int XE>
-hipError_t launch_few_rows(const FewArgs &args, hipStream_t stream) {
+hipError_t launch_few_rows(const FewArgs &args, hipStream_t stream, int num_cus) {
   const int threads = 64 * kFewWaves;
   constexpr int64_t kCols = (int64_t)1 << 25;   // of a launch
   for (int64_t n = 0; n < args.g.N; n += kCols) {
@@ -597,11 +597,11 @@ hipError_t launch_few_rows(const FewArgs &args, hipStream_t stream) {
       else
         go(std::integral_constant<int, 4>{}, nb);
     };
-    // Two blocks of B's rows share what is read of the left operand, where workgroups are
-    // left for the chip (us, N = K = 8192, one block / two: 16 rows 11.9 / 10.9, 32 16.0 /
-    // 13.9, one 16-bit row 12.8 / 10.5, one row in 4 bits 9.9 / 11.1; 16 x 4096 x 4096 4.5 /
-    // 6.8).
-    if (f.g.N >= 8192 && (XE >= 0 || f.g.M > 8))
+    // Two blocks of B's rows share what is read of the left operand, where a workgroup of
+    // 32 is left for every compute unit (us, 256 of them, N = K = 8192, one block / two: 16
+    // rows 11.9 / 10.9, 32 16.0 / 13.9, one 16-bit row 12.8 / 10.5, one row in 4 bits 9.9 /
+    // 11.1; 16 x 4096 x 4096 4.5 / 6.8).
+    if (f.g.N >= 32 * (int64_t)num_cus && (XE >= 0 || f.g.M > 8))
       rows(std::integral_constant<int, 2>{});
     else
       rows(std::integral_constant<int, 1>{});
@@ -617,8 +617,10 @@ hipError_t launch_few_rows(const FewArgs &args, hipStream_t stream) {
 // / 8.3, 64 x 8192 x 4096 13.3 / 15.2).  The tiles' time below is fitted on B in the caches;
 // from memory they take longer, the fewer rows share it (32 x 8192 x 8192 12.9 and 15.9).
 constexpr int64_t kFewMax = 64;
-double few_us(int64_t M, int64_t K, int64_t N) {
-  const double strips = N >= 8192 ? N / 4200.0 : std::max(1.0, N / 3500.0);
+double few_us(int64_t M, int64_t K, int64_t N, int num_cus) {
+  const double cus = num_cus / 256.0;
+  const double strips =
+      N >= 32 * (int64_t)num_cus ? N / (4200.0 * cus) : std::max(1.0, N / (3500.0 * cus));
   return 2.4 + K / 1024.0 * (0.3 + 0.0135 * M) * strips;
 }
 double cold_us(int64_t K, int64_t N) { return K * N * 0.5 * 8e-8; }
@@ -700,8 +702,8 @@ hipError_t gemm(const Mx4GemmArgs &a, hipStream_t stream, int num_cus) {
     }
   }
   const int splits = ranges_of(a.M, a.N, stages, num_cus, us);
-  if (a.M <= kFewMax && few_us(a.M, a.K, a.N) < us + cold_us(a.K, a.N))
-    return launch_few_rows<ELEM, -1>(FewArgs{a, nullptr, 0}, stream);
+  if (a.M <= kFewMax && few_us(a.M, a.K, a.N, num_cus) < us + cold_us(a.K, a.N))
+    return launch_few_rows<ELEM, -1>(FewArgs{a, nullptr, 0}, stream, num_cus);
   if (splits == 1) return tiles<ELEM>(best, a, 1, stream, num_cus);
   const hipError_t e = launch_tiles<kPart, 4, 2, 1, 2, 4>(a, splits, stream, num_cus);
   if (e != hipSuccess) return e;
@@ -733,10 +735,10 @@ hipError_t launch_mx4_linear(int xelem, const void *X, int64_t ldx, int elem,
   if (a.M <= kFewOwn && a.K > 0 && a.K <= kFewOwnK) {
     const FewArgs f{a, (const unsigned char *)X, ldx};
     if (xelem == TCU_ELEM_F16)
-      return elem == TCU_ELEM_F32 ? launch_few_rows<TCU_ELEM_F32, TCU_ELEM_F16>(f, stream)
-                                  : launch_few_rows<TCU_ELEM_F16, TCU_ELEM_F16>(f, stream);
-    return elem == TCU_ELEM_F32 ? launch_few_rows<TCU_ELEM_F32, TCU_ELEM_BF16>(f, stream)
-                                : launch_few_rows<TCU_ELEM_BF16, TCU_ELEM_BF16>(f, stream);
+      return elem == TCU_ELEM_F32 ? launch_few_rows<TCU_ELEM_F32, TCU_ELEM_F16>(f, stream, num_cus)
+                                  : launch_few_rows<TCU_ELEM_F16, TCU_ELEM_F16>(f, stream, num_cus);
+    return elem == TCU_ELEM_F32 ? launch_few_rows<TCU_ELEM_F32, TCU_ELEM_BF16>(f, stream, num_cus)
+                                : launch_few_rows<TCU_ELEM_BF16, TCU_ELEM_BF16>(f, stream, num_cus);
   }
   unsigned char *w = (unsigned char *)a.work;
   const int64_t row = mx4_row_bytes(a.K);
