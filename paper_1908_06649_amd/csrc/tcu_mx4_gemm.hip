@@ -83,13 +83,16 @@ __device__ __forceinline__ void dma_lds4_saddr(const void *gbase, unsigned voff,
 // next stage's first fragments, and the copy of the stage after it is issued into the
 // buffer that has been read.
 //
-// 8192 x 8192 x 8192, bf16 out, us in steady state: 248 to 258 on random codes (4.4 PFLOP/s; by
-// the card), 189 (5.8) on zeros; the matrix cores alone, from registers, 174 and 118.  Random
-// codes are bound by power, zeros by the order of reads and products: of a stage's 3600
-// cycles LDS is busy 2250 (reads 1735, copies 512) and the matrix cores 2048.  The copies
-// are not waited for: without their wait the time is the same.  Tried, same product:
-// products of 32 x 32 over 64 values (each instruction the same work at more power: 182 from
-// registers); the order that the compiler chose (256 against 248); bands of 2 or 8 rows of
+// 8192 x 8192 x 8192, bf16 out, us in steady state: 240 to 258 on random codes (4.3 to 4.6
+// PFLOP/s, by the card), 187 (5.9) on zeros, in the same 0.47 million cycles: power keeps the
+// clock at 1.95 GHz on random codes, 2.46 on zeros.  The matrix cores are busy in 56 % of
+// them, so the order of reads and products bounds both: of a stage's 3650 cycles LDS is busy
+// 2250 (reads 1735, copies 512) and the matrix cores 2048.  The same instructions from
+// registers: 153 on random codes (busy 95 %, 1.82 GHz), 114 on zeros; a better order would so
+// give part of its cycles back to the clock.  The copies are not waited for: without
+// their wait the time is the same.  Tried, same product:
+// products of 32 x 32 over 64 values (each instruction the same work at more power: from
+// registers 5 % slower); the order that the compiler chose (256 against 248); bands of 2 or 8 rows of
 // tiles (258, 256); a stage's copies issued at once or in two parts (262 against 258, on
 // zeros 198 against 189); four waves of 128 x 128 (their registers spill).
 template <int ELEM, int FM, int FN, int WM, int WN, int KG>
@@ -482,8 +485,9 @@ __device__ __forceinline__ u32x4 quad_codes(const unsigned char *row, int64_t co
 
 // XE: the left operand's element type (of up to four rows), or -1: in 4 bits already.
 // MF: blocks of 16 rows; NB: blocks of 16 rows of B.  A wave takes pairs of groups of 128
-// values: whole lines.  Bound by B's bytes and the latency of a wave's first: us from memory,
-// 1 x 4096 x 4096 4.9 (B 8.9 MB), 16 x 8192 x 8192 10.4 (B 35.7 MB, 3.4 TB/s with launch and end).
+// values: whole lines.  Bound by B's bytes and the latency of a wave's first (us in a row of
+// launches, B from memory / in the last cache: a 16-bit row 1 x 4096 x 4096 5.3 / 4.2, B 8.9
+// MB; 16 x 8192 x 8192 11.7 / 9.2, B 35.7 MB, 3.1 / 3.9 TB/s with launch and end).
 template <int ELEM, int XE, int MF, int NB>
 __global__ __launch_bounds__(64 * kFewWaves) void mx4_few_kernel(FewArgs fa) {
   const Mx4GemmArgs &a = fa.g;
@@ -612,10 +616,11 @@ hipError_t launch_few_rows(const FewArgs &args, hipStream_t stream, int num_cus)
 }
 
 // ------------------------------------------------------------------------ plan
-// The few-row kernel's time in microseconds (us, that / measured, B from memory: 16 x 4096 x
-// 4096 4.8 / 4.5, 32 x 8192 x 8192 13.9 / 13.9, 64 x 1024 x 4096 4.0 / 4.4, 64 x 4096 x 4096 7.9
-// / 8.3, 64 x 8192 x 4096 13.3 / 15.2).  The tiles' time below is fitted on B in the caches;
-// from memory they take longer, the fewer rows share it (32 x 8192 x 8192 12.9 and 15.9).
+// The few-row kernel's time in microseconds (us, that / measured on two cards, B from memory:
+// 16 x 4096 x 4096 4.8 / 4.5 and 5.0, 32 x 8192 x 8192 13.8 / 13.9 and 14.6, 64 x 1024 x 4096
+// 3.8 / 4.4 and 5.1, 64 x 4096 x 4096 7.8 / 8.3 and 8.7, 64 x 8192 x 4096 13.3 / 15.2).  The
+// tiles' time below is fitted on B in the caches; from memory they take longer, the fewer
+// rows share it (32 x 8192 x 8192 12.9 and 15.9).
 constexpr int64_t kFewMax = 64;
 double few_us(int64_t M, int64_t K, int64_t N, int num_cus) {
   const double cus = num_cus / 256.0;
@@ -624,9 +629,12 @@ double few_us(int64_t M, int64_t K, int64_t N, int num_cus) {
   return 2.4 + K / 1024.0 * (0.3 + 0.0135 * M) * strips;
 }
 double cold_us(int64_t K, int64_t N) { return K * N * 0.5 * 8e-8; }
-// Rows that a linear layer's few-row kernel brings to 4 bits itself: above, a workgroup's
-// own conversions cost more than their launch (4096 x 4096: 4 rows 4.9 us against 4.2 + 3.9).
-constexpr int64_t kFewOwn = 4, kFewOwnK = 32768;
+// What a linear layer's few-row kernel brings to 4 bits itself: up to four rows, of which
+// its quads of lanes hold one each (more have no such form), and of K values up to where every
+// workgroup's own conversions cost what a launch does (us from memory, own / two launches:
+// 1 x 4096 x 4096 5.3 / 6.7, 4 x 4096 x 4096 5.4 / 6.9, 4 x 8192 x 8192 11.7 / 13.1, 4 x 16384 x
+// 4096 13.4 / 13.3, 4 x 32768 x 4096 22.9 / 20.9, 4 x 32768 x 1024 19.5 / 17.5).
+constexpr int64_t kFewOwn = 4, kFewOwnK = 16384;
 
 // The tile kernel's variants and what their time in microseconds is made of: a call, a
 // round of stages on a compute unit that has room (`alone`) and where all are full (for
