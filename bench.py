@@ -69,7 +69,7 @@ METRIC = ("TFLOP/s (or TOP/s) and % MFMA peak for tcu_gemm; "
           "GB/s and % HBM peak for tcu_mm_tall")
 HEADLINE = "gemm_bf16_N8192_s32"
 # MI355X published peaks (dense): matrix cores by input type, and HBM3E.
-PEAK = {"f16": 2500.0, "bf16": 2500.0, "i8": 5000.0}   # TFLOP/s or TOP/s
+PEAK = {"f16": 2500.0, "bf16": 2500.0, "i8": 5000.0, "mx4": 10000.0}   # TFLOP/s or TOP/s
 HBM_PEAK_GBS = 8000.0
 CSRC = os.path.join(ROOT, "paper_1908_06649_amd", "csrc")
 PROFILES = os.path.join(ROOT, "profiles")
@@ -603,9 +603,10 @@ def mfma_probe(iters: int = 100000, reps: int = 3) -> None:
     """The matrix cores' sustained rate on this chip with nothing else
     running (libtcu_probe.so: the product's persistent grid, one workgroup of
     8 waves per CU, each wave issuing the product's 32-instruction phase from
-    registers `iters` times), for bfloat16 and int8 operands drawn at random
-    as in the workloads and for constant operands: the power-limited ceiling
-    the products are measured against.  Prints one JSON line."""
+    registers `iters` times), for bfloat16, int8 and 4-bit operands drawn at
+    random (4 bits: every code alike) and for constant operands (4 bits: ones,
+    and zeros): the power-limited ceiling the products are measured against.
+    Prints one JSON line."""
     import ctypes
     import torch
     from paper_1908_06649_amd import build as hip_build
@@ -622,11 +623,13 @@ def mfma_probe(iters: int = 100000, reps: int = 3) -> None:
     res = {"probe": "matrix-core ceiling", "blocks": blocks, "waves_per_block": 8,
            "instructions_per_wave": 32 * iters}
     st = torch.cuda.current_stream()
+    ones = {"bf16": 0x3F803F80, "i8": 0x01010101, "mx4": 0x22222222}
+    depth = {"bf16": 32, "i8": 64, "mx4": 128}      # of an instruction
     for name, dt, peak in (("bf16", tcu.TCU_BF16_F32, PEAK["bf16"]),
-                           ("i8", tcu.TCU_I8_I32, PEAK["i8"])):
-        for kind in ("random", "constant"):
-            if kind == "constant":
-                ops = torch.full((words,), 0x3F803F80 if name == "bf16" else 0x01010101,
+                           ("i8", tcu.TCU_I8_I32, PEAK["i8"]), ("mx4", 100, PEAK["mx4"])):
+        for kind in ("random", "constant") + (("zero",) if name == "mx4" else ()):
+            if kind != "random":
+                ops = torch.full((words,), ones[name] if kind == "constant" else 0,
                                  dtype=torch.int32, device="cuda")
             elif name == "bf16":
                 ops = torch.randn(words * 2, generator=g, device="cuda").to(torch.bfloat16)
@@ -651,8 +654,7 @@ def mfma_probe(iters: int = 100000, reps: int = 3) -> None:
             e1.record(st)
             torch.cuda.synchronize()
             ms = e0.elapsed_time(e1) / reps
-            flops = blocks * 8 * 32 * iters * (16 * 16 * 32 * 2 if name == "bf16" else
-                                               16 * 16 * 64 * 2)
+            flops = blocks * 8 * 32 * iters * 16 * 16 * depth[name] * 2
             rate = flops / (ms * 1e-3) / 1e12
             res[f"{name}_{kind}"] = {"ms": ms, "T_per_s": rate, "frac_of_peak": rate / peak}
     res["overlap"] = overlap_probe(lib, blocks, st)

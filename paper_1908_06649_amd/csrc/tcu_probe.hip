@@ -7,9 +7,9 @@
 // operands of one of the product's phases -- 8 data and 4 weights
 // fragments, 16 bytes per lane each -- once from memory, then issues `iters`
 // rounds of the product's 32 matrix-core instructions on them from
-// registers (16x16x32 bfloat16 into binary32, or 16x16x64 int8 into int32),
-// and finally writes one sum of its accumulators per lane so that no work
-// is dead.  No LDS, no further memory traffic, no barriers: the rate is
+// registers (16x16x32 bfloat16 into binary32, 16x16x64 int8 into int32, or
+// 16x16x128 in 4 bits, all scales 1, into binary32), and finally writes one
+// sum of its accumulators per lane so that no work is dead.  No LDS, no further memory traffic, no barriers: the rate is
 // bounded by the matrix cores and the chip's clock under the power limit,
 // which depends on the operand values (the host passes random or constant
 // data).
@@ -31,6 +31,17 @@ namespace tcu {
 namespace {
 
 constexpr int kFM = 8, kFN = 4;   // the product's wave sub-tile: 32 blocks of 16 x 16
+
+// The probe's type of operands in 4 bits, beside the library's dtypes.
+constexpr int kMx4 = 100;
+
+__device__ __forceinline__ f32x4 mfma_mx4_k128(u32x4 w, u32x4 x, f32x4 d) {
+  typedef int i32x8 __attribute__((ext_vector_type(8)));
+  const i32x8 a = {(int)w[0], (int)w[1], (int)w[2], (int)w[3], 0, 0, 0, 0};
+  const i32x8 b = {(int)x[0], (int)x[1], (int)x[2], (int)x[3], 0, 0, 0, 0};
+  return __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(a, b, d, 4, 4, 0, 0x7f7f7f7f, 0,
+                                                          0x7f7f7f7f);
+}
 
 template <int DT>
 __global__ __attribute__((amdgpu_flat_work_group_size(512, 512), amdgpu_waves_per_eu(2, 2))) void
@@ -54,7 +65,9 @@ mfma_probe_kernel(const u32x4 *__restrict__ ops, int64_t iters, unsigned *__rest
     for (int fn = 0; fn < kFN; ++fn)
 #pragma unroll
       for (int fm = 0; fm < kFM; ++fm) {
-        if constexpr (kI8)
+        if constexpr (DT == kMx4)
+          acc[fn][fm] = mfma_mx4_k128(wf[fn], xf[fm], acc[fn][fm]);
+        else if constexpr (kI8)
           acc[fn][fm] = mfma_i8_k64(wf[fn], xf[fm], acc[fn][fm]);
         else
           acc[fn][fm] = mfma_k32(DT, wf[fn], xf[fm], acc[fn][fm]);
@@ -301,7 +314,7 @@ hipError_t launch_overlap(int nv, const u32x4 *ops, int64_t iters, unsigned *out
 }  // namespace tcu
 
 // ops: blocks * 512 * 12 16-byte operand words (device); out: blocks * 512
-// words (device).  dtype: TCU_BF16_F32 or TCU_I8_I32.  Asynchronous on
+// words (device).  dtype: TCU_BF16_F32, TCU_I8_I32 or 100 (4 bits).  Asynchronous on
 // `stream`.  Returns 0, or -1 for bad arguments, -6 for a launch error.
 // Every wave issues 32 * iters matrix-core instructions.
 extern "C" __attribute__((visibility("default"))) int tcu_probe_mfma(int dtype, const void *ops,
@@ -315,6 +328,9 @@ extern "C" __attribute__((visibility("default"))) int tcu_probe_mfma(int dtype, 
                        (hipStream_t)stream, o, iters, u);
   else if (dtype == TCU_I8_I32)
     hipLaunchKernelGGL((tcu::mfma_probe_kernel<TCU_I8_I32>), dim3(blocks), dim3(512), 0,
+                       (hipStream_t)stream, o, iters, u);
+  else if (dtype == tcu::kMx4)
+    hipLaunchKernelGGL((tcu::mfma_probe_kernel<tcu::kMx4>), dim3(blocks), dim3(512), 0,
                        (hipStream_t)stream, o, iters, u);
   else
     return -1;
