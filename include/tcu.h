@@ -573,7 +573,7 @@ int64_t tcu_mx4_work(int64_t M, int64_t K, int64_t N);
  * each head's query, key and value); otherwise operands that lie in each other's gaps
  * are refused as overlapping.
  * A head of zeros has y = 0 (and a gradient of 0), also for eps = 0: there every head whose
- * squares' mean is 0 in binary32.  A value that is not finite stays in its head; a finite
+ * squares' mean is 0 in binary32 (squares below its normal numbers have fewer digits).  A value that is not finite stays in its head; a finite
  * head whose squares' sum passes binary32's range is taken as one of infinite norm: y = 0
  * (all as tcu_rms_norm).
  *   0 <= tokens <= TCU_MAX_RECT_DIM; 0 <= hq, hk <= TCU_MAX_HEADS (operands of no

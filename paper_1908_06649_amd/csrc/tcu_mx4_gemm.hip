@@ -661,8 +661,8 @@ double tiles_us(const Variant &v, int64_t M, int64_t N, int64_t stages, int num_
 }
 
 // Ranges of the contracted index where C has few tiles and it is long: the last variant
-// for each, their sums added by a second launch (us: 100 x 65536 x 64 15.2, 512 x
-// 65536 x 512 27; uncut 46 and 93 by the times below).
+// for each, their sums added by a second launch (us: 100 x 65536 x 64 14 to 15, 512 x
+// 65536 x 512 26 to 27; uncut 46 and 93 by the times above).
 constexpr int64_t kRangeValues = (int64_t)1 << 22;   // of all ranges' sums, at most
 int ranges_of(int64_t M, int64_t N, int64_t stages, int num_cus, double &us) {
   int best = 1;
