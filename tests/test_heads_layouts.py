@@ -113,3 +113,21 @@ def test_against_every_byte():
             assert got in (FREE, OVER)
         seen[want] += 1
     assert min(seen.values()) > 3000
+
+
+def test_vectors_against_every_byte():
+    """A gradient of the weights anywhere about an operand's heads."""
+    rng = random.Random(6)
+    seen = {FREE: 0, OVER: 0}
+    for _ in range(10000):
+        T, hq, dim = rng.randint(1, 5), rng.randint(1, 4), rng.randint(1, 3)
+        ld, hd = nested(rng, T, hq, dim)
+        dw = P[0] + 4 * rng.randint(-8, 40)
+        change = dict(q=P[0], ldq=ld, hdq=hd, dyq=P[1], lddyq=ld, hddyq=hd, dq=P[2], lddq=ld, hddq=hd,
+                      hk=0, k=0, dyk=0, dk=0, wk=0, dwk=0, wq=P[3], dwq=dw, work=P[6], tokens=T, hq=hq,
+                      dim=dim, rot=0)
+        got = getattr(tcu.lib(), QKG)(*{**CALLS[QKG], **change}.values())
+        shared = bytes_of(P[0], ld, hd, T, hq, dim, 2) & set(range(dw, dw + 4 * dim))
+        assert got == OVER if shared else got in (FREE, OVER), change
+        seen[got] += 1
+    assert min(seen.values()) > 2000
